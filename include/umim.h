@@ -612,6 +612,121 @@ umim_status umim_distill_soft_ce(const void *teacher_logits, int32_t n_teacher_r
                                  size_t workspace_bytes, int32_t *dev_status, cudaStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Log probabilities of given tokens, with entropy and the best alternatives
+ * (not part of the method: what a serving program answers with, what the
+ * perplexity over a compressed prompt is summed from, and, run once over the
+ * teacher's logits, the cache that umim_distill_topk_ce reads).  Per row r of
+ * logits x, with T = temperature, m = max_v x_v and
+ * l = ln sum_v exp((x_v - m) / T):
+ *   logprobs[r] = (x_t - m) / T - l          t = token_ids[r]
+ *   entropy[r]  = -sum_v p_v ln p_v          p_v = exp((x_v - m) / T - l)
+ *   stats[r]    = (m, l)                     m / T + l is the log-sum-exp
+ *   top_ids[r], top_logprobs[r]: the n_top largest logits in descending
+ *     order, equal ones in ascending order of their id, and their log
+ *     probabilities.  A logit of -inf is no alternative: entries past a row's
+ *     last one hold -1 and -inf.
+ * Computed in fp32 whatever the logits' type; each logit is read once.
+ * A row whose token is -1 is left out: its logits are not read, logprobs,
+ * entropy and stats are 0, its alternatives -1 and -inf.  A row of -inf only
+ * has logprob -inf, entropy 0 and stats (-inf, 0); a row that holds NaN or
+ * +inf has NaN everywhere and no alternatives (ids -1, log probabilities NaN).
+ * logits        device [n_rows][ld] of `dtype` (umim_dtype), 16-B aligned
+ * vocab, ld     vocabulary size (1 .. 262144) and row stride in elements: a
+ *               multiple of 8 (fp32: 4), at least vocab; the elements from
+ *               vocab up to ld are neither read nor written
+ * n_dev         device int32 [1] or NULL: rows used, min(*n_dev, n_rows);
+ *               what belongs to the rows behind them is left as it was
+ * token_ids     device int32 [n_rows], or NULL: no tokens, every row counts
+ *               (logprobs must then be NULL)
+ * temperature   in [1e-4, 1e4]
+ * n_top         0 .. 128
+ * logprobs, entropy  device fp32 [n_rows] out, or NULL
+ * stats         device fp32 [n_rows][2] out, 8-B aligned, or NULL
+ * top_ids, top_logprobs  device int32 / fp32 [n_rows][n_top] out (n_top > 0)
+ * No workspace.  Device-side errors: UMIM_ERR_INVALID_ARG for a token outside
+ * [-1, vocab) (that row is left out).
+ *
+ * umim_token_logprobs_grad: the gradient of sum_r g_r logprobs[r] + h_r
+ * entropy[r] with respect to the logits,
+ *   (1/T) [ g_r (1[v = t] - p_v) - h_r p_v (ln p_v + entropy[r]) ],
+ * zero on rows that are left out or hold -inf only, NaN on rows whose stats
+ * are NaN.  Each logit is read once, each gradient element written once.
+ * stats, entropy  as umim_token_logprobs wrote them for these logits, tokens
+ *               and this temperature (entropy only where grad_entropy is given)
+ * grad_logprobs, grad_entropy  device fp32 [n_rows]: g and h, or NULL for
+ *               zeros; one of them at least, and grad_logprobs only with
+ *               token_ids
+ * grad          device [n_rows][ld] of `dtype` out, 16-B aligned: elements
+ *               [0, vocab) of the rows used are written.  May be logits
+ *               itself (computed in place); other overlap is not allowed
+ * Other arguments and errors: as umim_token_logprobs.
+ * ------------------------------------------------------------------------ */
+typedef enum umim_dtype { UMIM_DTYPE_BF16 = 0, UMIM_DTYPE_FP16 = 1, UMIM_DTYPE_FP32 = 2 } umim_dtype;
+
+umim_status umim_token_logprobs(const void *logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t ld,
+                                const int32_t *n_dev, const int32_t *token_ids, float temperature, int32_t n_top,
+                                float *logprobs, float *entropy, float *stats, int32_t *top_ids, float *top_logprobs,
+                                int32_t *dev_status, cudaStream_t stream);
+
+umim_status umim_token_logprobs_grad(const void *logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t ld,
+                                     const int32_t *n_dev, const int32_t *token_ids, float temperature,
+                                     const float *stats, const float *entropy, const float *grad_logprobs,
+                                     const float *grad_entropy, void *grad, int32_t *dev_status,
+                                     cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Aligned predictive distillation from the teacher's best alternatives: the
+ * masked distillation loss of App. F where, of each teacher row, only n_top
+ * token ids and log probabilities were kept (umim_token_logprobs writes
+ * them), so that the frozen backbone runs once and 8 n_top bytes a row stand
+ * for its whole row of logits.  Over the N aligned pairs (teacher row t_k, student
+ * row s_k; umim_distill_align), with the teacher's entries (a_i, lambda_i)
+ * and q = softmax(x / T) of the student's row x:
+ *   tail == 0   p = softmax(lambda) over the entries, p_rest = 0
+ *   tail != 0   p_i = exp(lambda_i), p_rest = 1 - sum_i p_i: the rest of the
+ *               vocabulary counts as one outcome (below 2^-20, which is the
+ *               rounding of a list that holds everything, it counts as 0)
+ *   pair loss = -sum_i p_i ln q(a_i) - p_rest ln q_rest,
+ *     q_rest = the sum of q outside the list;  loss = the pair losses' mean
+ * and grad_scale times the loss's gradient with respect to the student logits,
+ * with P = sum_i p_i + p_rest:
+ *   grad_scale / (N T) q_v (P - p_rest / q_rest)     outside the list
+ *   grad_scale / (N T) (P q_v - p_i)                 at v = a_i;
+ * student rows in no pair have a zero gradient.  Computed in fp32.
+ * top_ids, top_logprobs  device int32 / fp32 [n_teacher_rows][n_top]; id -1:
+ *               no entry (a teacher row without entries has a pair loss of 0,
+ *               and its pair's gradient is 0)
+ * n_top         1 .. 128
+ * student_logits, dtype, vocab, ld, temperature  as umim_token_logprobs
+ * teacher_rows, student_rows  device int32 [max_pairs] (e.g. from
+ *               umim_distill_align); each student row at most once
+ * n_pairs       device int32 [1] or NULL: N (NULL: N = max_pairs)
+ * grad_scale    finite; this loss's weight in a sum, or a loss scale (fp16
+ *               gradients of 1 / N and below need one)
+ * loss          device fp32 [1] out
+ * pair_loss     device fp32 [max_pairs] out, or NULL
+ * grad          device [n_student_rows][ld] of `dtype` out, or NULL (loss
+ *               only); elements [0, vocab) of every row written; must not
+ *               overlap the logits
+ * workspace     device, umim_distill_topk_ce_workspace_size() bytes, 256-B
+ *               aligned (no initial contents required)
+ * A student row of -inf only has a pair loss of +inf (0 where nothing is
+ * asked of it) and a zero gradient; NaN or +inf in it make both NaN.
+ * Device-side errors: UMIM_ERR_INVALID_ARG, and nothing written, for N outside
+ * [0, max_pairs], a row outside its array or a student row in two pairs;
+ * UMIM_ERR_INVALID_ARG for an id outside [-1, vocab) or listed twice in its
+ * row (that entry counts as -1; of two equal ids the first counts).
+ * ------------------------------------------------------------------------ */
+size_t umim_distill_topk_ce_workspace_size(int32_t n_student_rows, int32_t max_pairs);
+
+umim_status umim_distill_topk_ce(const int32_t *top_ids, const float *top_logprobs, int32_t n_teacher_rows,
+                                 int32_t n_top, const void *student_logits, int32_t dtype, int32_t n_student_rows,
+                                 int32_t vocab, int64_t ld, const int32_t *teacher_rows, const int32_t *student_rows,
+                                 int32_t max_pairs, const int32_t *n_pairs, float temperature, int32_t tail,
+                                 float grad_scale, float *loss, float *pair_loss, void *grad, void *workspace,
+                                 size_t workspace_bytes, int32_t *dev_status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Decode attention for callers that cannot allocate GPU memory.
  * The paper has no counterpart to this call; it is a convenience of this
  * library.  A serving engine that gives all device memory to its own block

@@ -39,6 +39,10 @@ for indices and moved KV bytes:
                           loss): teacher / student alignment masks packed
                           into pairs, the soft cross-entropy and its
                           gradient with respect to the student logits
+  logprobs.token_logprobs / token_logprobs_grad / topk_ce
+                          log probabilities, entropy and alternatives of rows
+                          of logits, their gradient, and App. F's loss from
+                          the teacher's top log probabilities
 
 bf16 values are represented by their raw bit patterns (numpy uint16) and
 upcast exactly to float64.
@@ -62,8 +66,11 @@ Parity status per function (what pins it is in tests/test_oracle_*.py):
   align / soft_ce   pinned (the paper's alignment example, the compressed-
                     position map, library soft cross-entropy and KL,
                     autograd)
+  token_logprobs, its gradient, topk_ce
+                    pinned (library log-softmax and sort, autograd, the full
+                    soft cross-entropy when every id is listed)
 """
-from . import bf16, spans, merge, rollback, append, attention, compaction, rules, prefill, distill  # noqa: F401
+from . import bf16, spans, merge, rollback, append, attention, compaction, rules, prefill, distill, logprobs  # noqa: F401
 from .merge import merge_spans, merge_span_reference_steps  # noqa: F401
 from .rollback import kv_rollback  # noqa: F401
 from .append import kv_append  # noqa: F401

@@ -21,6 +21,10 @@ points keep the C names:
                           aligned predictive distillation: teacher/student row pairing
                           and the full-vocabulary soft-target cross-entropy with its
                           gradient (App. F, Algorithm 1)
+  umim_distill_topk_ce    the same from the teacher's cached top log probabilities
+  umim_token_logprobs, umim_token_logprobs_grad
+                          log probabilities of given tokens, entropy and the best
+                          alternatives of rows of logits, and the gradient of the first two
 """
 import ctypes
 import struct
@@ -548,6 +552,132 @@ def umim_distill_soft_ce(teacher_logits, student_logits, teacher_rows, student_r
                                       _p(grad if with_grad else None), _p(workspace_buf), workspace_buf.numel(),
                                       _p(dev_status), _stream(stream))
     _check(code, "umim_distill_soft_ce")
+    return loss, pair_loss, (grad if with_grad else None)
+
+
+# ---------------------------------------------------------------------------
+# log probabilities, and distillation from a teacher's top log probabilities
+# ---------------------------------------------------------------------------
+_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}   # umim_dtype
+
+
+def _logit_rows(logits, vocab, what="logits"):
+    """(address, dtype code, rows, vocab, row stride) of rows of logits."""
+    _on_gpu(logits)
+    shape, stride = logits.shape, logits.stride()
+    if logits.dtype not in _DTYPE or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{what} must be bf16, fp16 or fp32 [rows][vocab] with contiguous rows")
+    ld = stride[0]
+    if shape[0] < 2:   # a single row's stride says nothing: any that is allowed
+        vec = 16 // logits.element_size()
+        ld = (shape[1] + vec - 1) // vec * vec
+    vocab = shape[1] if vocab is None else int(vocab)
+    if vocab > shape[1]:
+        raise ValueError(f"{what} have {shape[1]} columns, vocab is {vocab}")
+    return logits.data_ptr(), _DTYPE[logits.dtype], shape[0], vocab, ld
+
+
+def _vector(t, n, dtype, what):
+    """The address of a contiguous device tensor of n elements, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what} must be a contiguous CUDA tensor of {n} x {dtype}")
+    return t.data_ptr()
+
+
+def umim_token_logprobs(logits, token_ids=None, n_top=0, vocab=None, temperature=1.0, n_rows=None, out=None,
+                        dev_status=None, stream=None):
+    """Log probabilities of token_ids [R] (int32; -1 leaves a row out, None: no
+    tokens) under softmax(logits / temperature), logits bf16, fp16 or fp32
+    [R][columns] (vocab defaults to the columns; rows may be strided, a multiple
+    of 16 bytes apart).  n_rows: device int32 [1], the rows used, or None (all).
+    Returns (or fills, when out is given) a dict: logprobs and entropy fp32
+    [R], stats fp32 [R][2] (the row's maximum m, and ln sum exp((x - m) /
+    temperature)), top_ids int32 and top_logprobs fp32 [R][n_top]; logprobs is
+    None without tokens, the last two are None where n_top is 0."""
+    x, dtype, R, V, ld = _logit_rows(logits, vocab)
+    if out is None:
+        f32 = lambda *n: torch.empty(n, dtype=torch.float32, device=logits.device)
+        out = dict(logprobs=None if token_ids is None else f32(R), entropy=f32(R), stats=f32(R, 2),
+                   top_ids=torch.empty((R, n_top), dtype=torch.int32, device=logits.device) if n_top else None,
+                   top_logprobs=f32(R, n_top) if n_top else None)
+    code = lib().umim_token_logprobs(
+        x, dtype, R, V, ld, _vector(n_rows, 1, torch.int32, "n_rows"), _vector(token_ids, R, torch.int32, "token_ids"),
+        float(temperature), n_top, _vector(out.get("logprobs"), R, torch.float32, "logprobs"),
+        _vector(out.get("entropy"), R, torch.float32, "entropy"),
+        _vector(out.get("stats"), 2 * R, torch.float32, "stats"),
+        _vector(out.get("top_ids"), R * n_top, torch.int32, "top_ids"),
+        _vector(out.get("top_logprobs"), R * n_top, torch.float32, "top_logprobs"), _p(dev_status), _stream(stream))
+    _check(code, "umim_token_logprobs")
+    return out
+
+
+def umim_token_logprobs_grad(logits, stats, token_ids=None, grad_logprobs=None, entropy=None, grad_entropy=None,
+                             vocab=None, temperature=1.0, n_rows=None, grad=None, dev_status=None, stream=None):
+    """The gradient with respect to the logits of sum(grad_logprobs * logprobs)
+    + sum(grad_entropy * entropy), from what umim_token_logprobs returned for
+    the same logits, tokens and temperature.  grad (like logits, the same row
+    stride; logits itself for a gradient in place) is returned; columns past
+    vocab are not written."""
+    x, dtype, R, V, ld = _logit_rows(logits, vocab)
+    if grad is None:
+        grad = torch.empty_strided((R, logits.shape[1]), (ld, 1), dtype=logits.dtype, device=logits.device)
+    g_ptr, g_dtype, g_R, _, g_ld = _logit_rows(grad, V, "grad")
+    if g_dtype != dtype or g_R != R or g_ld != ld:
+        raise ValueError("grad must have the logits' type, rows and row stride")
+    code = lib().umim_token_logprobs_grad(
+        x, dtype, R, V, ld, _vector(n_rows, 1, torch.int32, "n_rows"), _vector(token_ids, R, torch.int32, "token_ids"),
+        float(temperature), _vector(stats, 2 * R, torch.float32, "stats"),
+        _vector(entropy, R, torch.float32, "entropy"),
+        _vector(grad_logprobs, R, torch.float32, "grad_logprobs"),
+        _vector(grad_entropy, R, torch.float32, "grad_entropy"), g_ptr, _p(dev_status), _stream(stream))
+    _check(code, "umim_token_logprobs_grad")
+    return grad
+
+
+def umim_distill_topk_ce_workspace_size(n_student_rows, max_pairs):
+    return int(lib().umim_distill_topk_ce_workspace_size(n_student_rows, max_pairs))
+
+
+def umim_distill_topk_ce(top_ids, top_logprobs, student_logits, teacher_rows, student_rows, n_pairs=None, vocab=None,
+                         temperature=1.0, tail=True, grad_scale=1.0, with_grad=True, loss=None, pair_loss=None,
+                         grad=None, workspace_buf=None, dev_status=None, stream=None):
+    """Soft-target cross-entropy over the aligned pairs from the teacher's top
+    log probabilities (top_ids int32, top_logprobs fp32 [R_T][K], as
+    umim_token_logprobs returns them), and grad_scale times its gradient with
+    respect to the student logits (bf16, fp16 or fp32 [R_S][columns]).  tail:
+    what the teacher's list leaves counts as one outcome; otherwise the list is
+    renormalised.  n_pairs: device int32 [1] or None (all of teacher_rows).
+    Returns (loss [1] fp32, pair_loss [max_pairs] fp32, grad like
+    student_logits or None)."""
+    x, dtype, R_S, V, ld = _logit_rows(student_logits, vocab, "student_logits")
+    dev = student_logits.device
+    if top_ids.dim() != 2 or top_ids.shape != top_logprobs.shape:
+        raise ValueError("top_ids and top_logprobs must have the same shape [rows][n_top]")
+    R_T, K = top_ids.shape
+    P = teacher_rows.numel()
+    if loss is None:
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+    if pair_loss is None:
+        pair_loss = torch.empty(max(1, P), dtype=torch.float32, device=dev)
+    g_ptr = None
+    if with_grad:
+        if grad is None:
+            grad = torch.empty_strided((R_S, student_logits.shape[1]), (ld, 1), dtype=student_logits.dtype, device=dev)
+        g_ptr, g_dtype, g_R, _, g_ld = _logit_rows(grad, V, "grad")
+        if g_dtype != dtype or g_R != R_S or g_ld != ld:
+            raise ValueError("grad must have the student logits' type, rows and row stride")
+    if workspace_buf is None:
+        workspace_buf = workspace(umim_distill_topk_ce_workspace_size(R_S, P), dev)
+    code = lib().umim_distill_topk_ce(
+        _vector(top_ids, R_T * K, torch.int32, "top_ids"),
+        _vector(top_logprobs, R_T * K, torch.float32, "top_logprobs"),
+        R_T, K, x, dtype, R_S, V, ld, _vector(teacher_rows, P, torch.int32, "teacher_rows"),
+        _vector(student_rows, P, torch.int32, "student_rows"), P, _vector(n_pairs, 1, torch.int32, "n_pairs"),
+        float(temperature), 1 if tail else 0, float(grad_scale), _vector(loss, 1, torch.float32, "loss"),
+        _p(pair_loss), g_ptr, workspace_buf.data_ptr(), workspace_buf.numel(), _p(dev_status), _stream(stream))
+    _check(code, "umim_distill_topk_ce")
     return loss, pair_loss, (grad if with_grad else None)
 
 

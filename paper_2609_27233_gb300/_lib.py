@@ -76,6 +76,14 @@ SIGNATURES = {
     "umim_distill_soft_ce_workspace_size": (c_size, [c_i32, c_i32]),
     "umim_distill_soft_ce": (ctypes.c_int, [c_ptr, c_i32, c_ptr, c_i32, c_i32, c_i64, c_ptr, c_ptr, c_i32, c_ptr,
                                             ctypes.c_float, c_ptr, c_ptr, c_ptr, c_ptr, c_size, c_ptr, c_ptr]),
+    "umim_token_logprobs": (ctypes.c_int, [c_ptr, c_i32, c_i32, c_i32, c_i64, c_ptr, c_ptr, ctypes.c_float, c_i32,
+                                           c_ptr, c_ptr, c_ptr, c_ptr, c_ptr, c_ptr, c_ptr]),
+    "umim_token_logprobs_grad": (ctypes.c_int, [c_ptr, c_i32, c_i32, c_i32, c_i64, c_ptr, c_ptr, ctypes.c_float,
+                                                c_ptr, c_ptr, c_ptr, c_ptr, c_ptr, c_ptr, c_ptr]),
+    "umim_distill_topk_ce_workspace_size": (c_size, [c_i32, c_i32]),
+    "umim_distill_topk_ce": (ctypes.c_int, [c_ptr, c_ptr, c_i32, c_i32, c_ptr, c_i32, c_i32, c_i32, c_i64, c_ptr,
+                                            c_ptr, c_i32, c_ptr, ctypes.c_float, c_i32, ctypes.c_float, c_ptr, c_ptr,
+                                            c_ptr, c_ptr, c_size, c_ptr, c_ptr]),
     "umim_decode_attention_workspace_size": (c_size, [c_i32, c_i32, c_i32, c_i32]),
     "umim_decode_attention": (ctypes.c_int, [c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_i32,
                                              c_ptr, c_i32, ctypes.c_float, c_ptr, c_ptr, c_size, c_ptr,

@@ -5,7 +5,7 @@
 #include <cstring>
 #include <mutex>
 
-#include "common.cuh"
+#include "logits.cuh"
 
 namespace umim {
 
@@ -68,6 +68,15 @@ int distill_soft_ce_vecs(int64_t V);
 umim_status distill_soft_ce(const void *, int32_t, const void *, int32_t, int32_t, int64_t, const int32_t *,
                             const int32_t *, int32_t, const int32_t *, float, float *, float *, void *, void *,
                             int32_t *, cudaStream_t, int);
+umim_status token_logprobs(const void *, int, int, int, int64_t, const int32_t *, const int32_t *, float, int, float *,
+                           float *, float *, int32_t *, float *, int32_t *, cudaStream_t, int);
+umim_status token_logprobs_grad(const void *, int, int, int, int64_t, const int32_t *, const int32_t *, float,
+                                const float *, const float *, const float *, const float *, void *, int32_t *,
+                                cudaStream_t, int);
+size_t distill_topk_ce_workspace_bytes(int R_S, int max_pairs);
+umim_status distill_topk_ce(const int32_t *, const float *, int, int, const void *, int, int, int, int64_t,
+                            const int32_t *, const int32_t *, int, const int32_t *, float, int, float, float *, float *,
+                            void *, void *, int32_t *, cudaStream_t, int);
 int decode_step_max_batch();
 size_t decode_step_workspace_bytes(int B, int Hkv, int D, int num_sms);
 umim_status decode_layer_step(const void *, int, const umim_paged_kv *, int, int32_t *, int, int32_t *, int,
@@ -105,6 +114,20 @@ bool kv_ok(const umim_paged_kv *kv) {
 bool kv_supported(const umim_paged_kv *kv) {
   return kv->page_size == UMIM_PAGE_SIZE && (kv->head_dim == 64 || kv->head_dim == 128) && kv->n_kv_heads <= 64;
 }
+
+// rows of logits: each starts on a 16-byte vector
+umim_status logits_ok(const void *logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t ld) {
+  if (n_rows < 0 || vocab < 1) return UMIM_ERR_INVALID_ARG;
+  if (dtype != UMIM_DTYPE_BF16 && dtype != UMIM_DTYPE_FP16 && dtype != UMIM_DTYPE_FP32) return UMIM_ERR_INVALID_ARG;
+  const int64_t vec = 16 / (int64_t)dtype_bytes(dtype);
+  if (ld % vec != 0 || ld < vocab) return UMIM_ERR_INVALID_ARG;
+  if (vocab > kMaxLogitVocab) return UMIM_ERR_UNSUPPORTED;
+  if (n_rows > 0 && (!logits || !aligned(logits, 16))) return UMIM_ERR_INVALID_ARG;
+  return UMIM_OK;
+}
+
+// neither the scale 1 / T nor T itself leaves fp32's range
+bool temperature_ok(float t) { return t >= 1e-4f && t <= 1e4f; }
 
 bool merge_supported(int d, int h) {
   return d > 0 && d % 512 == 0 && d <= 8192 && (h == 1 || h == 2 || h == 4 || h == 8);
@@ -391,6 +414,9 @@ const char *umim_debug_site_name(int32_t status) {
       "distill.pair",
       "rules.span_slot",
       "rules.span_token",
+      "distill_topk.teacher_row",
+      "distill_topk.pair",
+      "distill_topk.entry",
   };
   const int site = (status >> 8) & 0xffffff;
   return site < kSiteCount ? names[site] : "";
@@ -402,6 +428,66 @@ umim_status umim_selftest_bounds_check(int32_t *buf, int64_t n, int64_t index, i
   if (!buf || n <= 0) return UMIM_ERR_INVALID_ARG;
   const DeviceScope scope(stream);
   return selftest_bounds_check(buf, n, index, dev_status, stream);
+}
+
+umim_status umim_token_logprobs(const void *logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t ld,
+                                const int32_t *n_dev, const int32_t *token_ids, float temperature, int32_t n_top,
+                                float *logprobs, float *entropy, float *stats, int32_t *top_ids, float *top_logprobs,
+                                int32_t *dev_status, cudaStream_t stream) {
+  const umim_status st = logits_ok(logits, dtype, n_rows, vocab, ld);
+  if (st != UMIM_OK) return st;
+  if (!temperature_ok(temperature) || n_top < 0 || n_top > kMaxTop) return UMIM_ERR_INVALID_ARG;
+  if (logprobs && !token_ids) return UMIM_ERR_INVALID_ARG;
+  if (n_top > 0 && n_rows > 0 && (!top_ids || !top_logprobs)) return UMIM_ERR_INVALID_ARG;
+  if (!aligned(stats, 8)) return UMIM_ERR_INVALID_ARG;
+  if (n_rows == 0) return UMIM_OK;
+  const DeviceScope scope(stream);
+  return token_logprobs(logits, dtype, n_rows, vocab, ld, n_dev, token_ids, temperature, n_top, logprobs, entropy,
+                        stats, top_ids, top_logprobs, dev_status, stream, scope.sms());
+}
+
+umim_status umim_token_logprobs_grad(const void *logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t ld,
+                                     const int32_t *n_dev, const int32_t *token_ids, float temperature,
+                                     const float *stats, const float *entropy, const float *grad_logprobs,
+                                     const float *grad_entropy, void *grad, int32_t *dev_status,
+                                     cudaStream_t stream) {
+  const umim_status st = logits_ok(logits, dtype, n_rows, vocab, ld);
+  if (st != UMIM_OK) return st;
+  if (!temperature_ok(temperature)) return UMIM_ERR_INVALID_ARG;
+  if (!grad_logprobs && !grad_entropy) return UMIM_ERR_INVALID_ARG;
+  if ((grad_logprobs && !token_ids) || (grad_entropy && !entropy)) return UMIM_ERR_INVALID_ARG;
+  if (n_rows == 0) return UMIM_OK;
+  if (!stats || !aligned(stats, 8) || !grad || !aligned(grad, 16)) return UMIM_ERR_INVALID_ARG;
+  const DeviceScope scope(stream);
+  return token_logprobs_grad(logits, dtype, n_rows, vocab, ld, n_dev, token_ids, temperature, stats, entropy,
+                             grad_logprobs, grad_entropy, grad, dev_status, stream, scope.sms());
+}
+
+size_t umim_distill_topk_ce_workspace_size(int32_t n_student_rows, int32_t max_pairs) {
+  if (n_student_rows < 0 || max_pairs < 0) return 0;
+  return distill_topk_ce_workspace_bytes(n_student_rows, max_pairs);
+}
+
+umim_status umim_distill_topk_ce(const int32_t *top_ids, const float *top_logprobs, int32_t n_teacher_rows,
+                                 int32_t n_top, const void *student_logits, int32_t dtype, int32_t n_student_rows,
+                                 int32_t vocab, int64_t ld, const int32_t *teacher_rows, const int32_t *student_rows,
+                                 int32_t max_pairs, const int32_t *n_pairs, float temperature, int32_t tail,
+                                 float grad_scale, float *loss, float *pair_loss, void *grad, void *workspace,
+                                 size_t workspace_bytes, int32_t *dev_status, cudaStream_t stream) {
+  const umim_status st = logits_ok(student_logits, dtype, n_student_rows, vocab, ld);
+  if (st != UMIM_OK) return st;
+  if (n_teacher_rows < 0 || max_pairs < 0 || n_top < 1 || n_top > kMaxTop || !loss) return UMIM_ERR_INVALID_ARG;
+  if (!temperature_ok(temperature) || !std::isfinite(grad_scale)) return UMIM_ERR_INVALID_ARG;
+  if (n_teacher_rows > 0 && (!top_ids || !top_logprobs)) return UMIM_ERR_INVALID_ARG;
+  if (grad && !aligned(grad, 16)) return UMIM_ERR_INVALID_ARG;
+  if (max_pairs > 0 && (!teacher_rows || !student_rows)) return UMIM_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 256) ||
+      workspace_bytes < distill_topk_ce_workspace_bytes(n_student_rows, max_pairs))
+    return UMIM_ERR_WORKSPACE;
+  const DeviceScope scope(stream);
+  return distill_topk_ce(top_ids, top_logprobs, n_teacher_rows, n_top, student_logits, dtype, n_student_rows, vocab,
+                         ld, teacher_rows, student_rows, max_pairs, n_pairs, temperature, tail != 0, grad_scale, loss,
+                         pair_loss, grad, workspace, dev_status, stream, scope.sms());
 }
 
 size_t umim_prefill_attention_workspace_size(int32_t batch, int32_t n_rows, int32_t n_kv_heads, int32_t head_dim) {

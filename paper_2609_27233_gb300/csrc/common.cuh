@@ -73,7 +73,10 @@ enum DebugSite : int32_t {
   kSiteDistillPair = 21,
   kSiteRulesSpanSlot = 22,
   kSiteRulesSpanToken = 23,
-  kSiteCount = 24
+  kSiteTopkTeacherRow = 24,
+  kSiteTopkPair = 25,
+  kSiteTopkEntry = 26,
+  kSiteCount = 27
 };
 
 // true when 0 <= i < n; in the debug build a false result is recorded
