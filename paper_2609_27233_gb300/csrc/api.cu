@@ -417,6 +417,8 @@ const char *umim_debug_site_name(int32_t status) {
       "distill_topk.teacher_row",
       "distill_topk.pair",
       "distill_topk.entry",
+      "logprobs.segment",
+      "logprobs.rank",
   };
   const int site = (status >> 8) & 0xffffff;
   return site < kSiteCount ? names[site] : "";

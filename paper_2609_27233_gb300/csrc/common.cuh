@@ -76,7 +76,9 @@ enum DebugSite : int32_t {
   kSiteTopkTeacherRow = 24,
   kSiteTopkPair = 25,
   kSiteTopkEntry = 26,
-  kSiteCount = 27
+  kSiteLogprobSegment = 27,
+  kSiteLogprobRank = 28,
+  kSiteCount = 29
 };
 
 // true when 0 <= i < n; in the debug build a false result is recorded

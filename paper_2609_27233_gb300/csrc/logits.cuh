@@ -13,15 +13,58 @@ constexpr int kMaxTop = 128;             // alternatives per row, at most
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// The hardware's base-2 exponential (relative error about 2^-22; subnormal results flush to zero).
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// the maximum over the warp; NaN only where every lane holds one
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// sum over the warp by xor butterflies: every lane gets the same bits
+__device__ __forceinline__ float2 warp_sum2(float2 v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    v = __fadd2_rn(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+  return v;
+}
+
 __device__ __forceinline__ float2 half2_to_float2(uint32_t w) {
   return __half22float2(*reinterpret_cast<const __half2 *>(&w));
 }
 
 // The three element types: VEC elements to a 16-byte vector, unpacked to and
-// packed from fp32 (packing rounds to nearest even).
+// packed from fp32 (packing rounds to nearest even).  max_words takes the
+// maximum of the elements of two 32-bit words place by place, word_max that of
+// one word's; both pass a number over a NaN.  order_key maps an element's bits
+// to a number that grows with its value, both zeros to one.
+__device__ __forceinline__ uint32_t order_key16(uint16_t b) {
+  const uint32_t u = b == 0x8000u ? 0u : b;
+  return u & 0x8000u ? 0xffffu - u : u + 0x8000u;
+}
+__device__ __forceinline__ uint16_t from_key16(uint32_t k) {
+  return (uint16_t)(k & 0x8000u ? k - 0x8000u : 0xffffu - k);
+}
+
 struct ElemBf16 {
   using T = uint16_t;
   static constexpr int VEC = 8;
+  static constexpr uint32_t kNegInf2 = 0xff80ff80u;
+  static constexpr T kNegInf = 0xff80;
+  static __device__ __forceinline__ uint32_t max_words(uint32_t x, uint32_t y) {
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(y));
+    return d;
+  }
+  static __device__ __forceinline__ T word_max_bits(uint32_t w) { return (T)max_words(w, w >> 16); }
+  static __device__ __forceinline__ uint32_t order_key(T b) { return order_key16(b); }
+  static __device__ __forceinline__ T from_key(uint32_t k) { return from_key16(k); }
   static __device__ __forceinline__ float2 pair(uint32_t w) {
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
@@ -39,6 +82,16 @@ struct ElemBf16 {
 struct ElemFp16 {
   using T = uint16_t;
   static constexpr int VEC = 8;
+  static constexpr uint32_t kNegInf2 = 0xfc00fc00u;
+  static constexpr T kNegInf = 0xfc00;
+  static __device__ __forceinline__ uint32_t max_words(uint32_t x, uint32_t y) {
+    uint32_t d;
+    asm("max.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(y));
+    return d;
+  }
+  static __device__ __forceinline__ T word_max_bits(uint32_t w) { return (T)max_words(w, w >> 16); }
+  static __device__ __forceinline__ uint32_t order_key(T b) { return order_key16(b); }
+  static __device__ __forceinline__ T from_key(uint32_t k) { return from_key16(k); }
   static __device__ __forceinline__ float2 pair(uint32_t w) { return half2_to_float2(w); }
   static __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     __half2 p = __floats2half2_rn(lo, hi);
@@ -54,9 +107,50 @@ struct ElemFp16 {
 struct ElemFp32 {
   using T = float;
   static constexpr int VEC = 4;
+  static constexpr uint32_t kNegInf2 = 0xff800000u;
+  static constexpr T kNegInf = -INFINITY;
+  static __device__ __forceinline__ uint32_t max_words(uint32_t x, uint32_t y) {
+    return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y)));
+  }
+  static __device__ __forceinline__ T word_max_bits(uint32_t w) { return __uint_as_float(w); }
+  static __device__ __forceinline__ uint32_t order_key(T b) {
+    const uint32_t u = b == 0.f ? 0u : __float_as_uint(b);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+  }
+  static __device__ __forceinline__ T from_key(uint32_t k) {
+    return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+  }
   static __device__ __forceinline__ float to_float(T x) { return x; }
   static __device__ __forceinline__ T from_float(float x) { return x; }
 };
+
+// The vector at element e of a row of V; none at or past V is read, they come out as -inf.
+template <class E>
+__device__ __forceinline__ uint4 load_raw(const typename E::T *row, int e, int V) {
+  if (e + E::VEC <= V) return *reinterpret_cast<const uint4 *>(row + e);
+  uint32_t w[4] = {E::kNegInf2, E::kNegInf2, E::kNegInf2, E::kNegInf2};
+#pragma unroll
+  for (int j = 0; j < E::VEC; ++j)
+    if (e + j < V) {
+      if constexpr (E::VEC == 8) {
+        const uint32_t keep = (j & 1) ? 0x0000ffffu : 0xffff0000u;
+        w[j / 2] = (w[j / 2] & keep) | ((uint32_t)row[e + j] << (16 * (j & 1)));
+      } else {
+        w[j] = __float_as_uint(row[e + j]);
+      }
+    }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// words i and i + 1 of fp32 elements, or both elements of a 16-bit word, as two floats
+template <class E>
+__device__ __forceinline__ float2 pair_of(const uint4 &u, int i) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  if constexpr (E::VEC == 8)
+    return E::pair(w[i]);
+  else
+    return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+}
 
 // the elements of a 16-byte vector as floats, and back
 template <class E>
