@@ -42,7 +42,8 @@ struct GradArgs {
   int64_t ld;
   const int32_t *n_dev;
   const int32_t *tokens;
-  float inv_t;
+  float inv_t, c;            // 1 / T, log2(e) / T
+  int32_t parts;             // CTAs per row
   const float2 *stats;
   const float *entropy, *g, *h;
   void *grad;
@@ -495,43 +496,81 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
   }
 }
 
-// One CTA per row, a vector per thread and step.
+// ---------------------------------------------------------------------------
+// gradient
+// ---------------------------------------------------------------------------
+// Elementwise, bound by its one read and one write of every element.  A CTA takes
+// kGradChunks chunks of a row: 4 vectors a thread, loaded together and ahead of the
+// row's numbers.  With t = log2 p the element is p (A + B t), A = -(g + h H) / T and
+// B = -h ln 2 / T; the token's own is -g expm1(ln p) / T + p (A + g / T + B t), exact
+// where p is so near 1 that 1 - p would be nothing.
+constexpr int kGradChunks = 2;
+
 template <class E>
-__global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(GradArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) token_logprobs_grad_kernel(GradArgs a) {
   griddep_wait();
-  const int r = blockIdx.x, V = a.V;
+  griddep_launch();
+  const int r = blockIdx.x / a.parts, V = a.V;
   if (r >= rows_used(a.n_dev, a.R)) return;
   const typename E::T *row = static_cast<const typename E::T *>(a.logits) + (int64_t)r * a.ld;
   typename E::T *out = static_cast<typename E::T *>(a.grad) + (int64_t)r * a.ld;
+  constexpr int kStep = kThreads * E::VEC, kChunk = kUnroll * kStep;
+  int e0 = (blockIdx.x % a.parts) * (kGradChunks * kChunk) + threadIdx.x * E::VEC;
+  const int last = min(V, (int)(blockIdx.x % a.parts + 1) * (kGradChunks * kChunk));
+
   const int token = a.tokens ? row_token(a.tokens, r, V, a.status, threadIdx.x == 0) : 0;
   const float2 st = a.stats[r];
+  const float g = a.g ? a.g[r] * a.inv_t : 0.f, h = a.h ? a.h[r] * a.inv_t : 0.f;
   const bool zero = token < 0 || st.x == -INFINITY;
-  const float g = a.g ? a.g[r] * a.inv_t : 0.f, h = a.h ? a.h[r] * a.inv_t : 0.f, H = a.h ? a.entropy[r] : 0.f;
-  for (int e = threadIdx.x * E::VEC; e < V; e += kThreads * E::VEC) {
-    float x[E::VEC], d[E::VEC];
-    if (zero) {
-#pragma unroll
-      for (int j = 0; j < E::VEC; ++j) d[j] = 0.f;
-    } else {
-      load_vec<E>(row, e, V, 0.f, x);
-#pragma unroll
-      for (int j = 0; j < E::VEC; ++j) {
-        const float z = (x[j] - st.x) * a.inv_t - st.y, p = expf(z);
-        d[j] = -p * g;
-        if (a.g && e + j == token) d[j] = -expm1f(z) * g;
-        if (!(p == 0.f)) d[j] -= h * p * (z + H);
-      }
-    }
-    store_vec<E>(out, e, V, d);
+  if (zero) {
+    const float z[E::VEC] = {};
+    for (; e0 < last; e0 += kStep) store_vec<E>(out, e0, V, z);
+    return;
   }
-}
-
-template <class Args>
-umim_status launch_rows(void (*kern)(Args), const Args &a, int R, const char *label, cudaStream_t stream) {
-  trace_mark(stream, label);
-  const cudaError_t e = launch_pdl(kern, dim3((unsigned)R), dim3(kThreads), 0, stream, a);
-  trace_mark(stream, nullptr);
-  return e == cudaSuccess ? UMIM_OK : UMIM_ERR_CUDA;
+  const float H = a.h ? a.entropy[r] : 0.f;
+  // a row without a distribution has NaN for m: all of it is
+  const float A = isnan(st.x) ? NAN : -g - h * H, B = -h * kLn2;
+  const float2 A2 = make_float2(A, A), B2 = make_float2(B, B), nm2 = make_float2(-st.x, -st.x);
+  const float2 c2 = make_float2(a.c, a.c), nl2 = make_float2(-st.y * kLog2e, -st.y * kLog2e);
+  for (; e0 < last; e0 += kChunk) {
+    uint4 u[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int e = e0 + k * kStep;
+      if (e + E::VEC <= V)
+        u[k] = __ldcs(reinterpret_cast<const uint4 *>(row + e));
+      else if (e < V)
+        u[k] = load_raw<E>(row, e, V);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int e = e0 + k * kStep;
+      if (e >= last) break;
+      float d[E::VEC];
+#pragma unroll
+      for (int i = 0; i < E::VEC / 2; ++i) {
+        float2 t = __ffma2_rn(__fadd2_rn(pair_of<E>(u[k], i), nm2), c2, nl2);
+        t = make_float2(fmaxf(t.x, -1000.f), fmaxf(t.y, -1000.f));   // of -inf: 0 times it would be no number
+        const float2 v = __fmul2_rn(make_float2(ex2(t.x), ex2(t.y)), __ffma2_rn(t, B2, A2));
+        d[2 * i] = v.x;
+        d[2 * i + 1] = v.y;
+      }
+      if (a.g && (unsigned)(token - e) < (unsigned)E::VEC) {
+        float x[E::VEC];
+        unpack<E>(u[k], x);
+#pragma unroll
+        for (int j = 0; j < E::VEC; ++j)
+          if (e + j == token) {
+            const float z = (x[j] - st.x) * a.inv_t - st.y, t = fmaxf(z * kLog2e, -1000.f);
+            d[j] = -g * expm1f(z) + ex2(t) * fmaf(t, B, A + g);
+          }
+      }
+      if (e + E::VEC <= V)
+        __stcs(reinterpret_cast<uint4 *>(out + e), pack<E>(d));
+      else
+        store_vec<E>(out, e, V, d);
+    }
+  }
 }
 
 }  // namespace
@@ -578,14 +617,18 @@ umim_status token_logprobs(const void *logits, int dtype, int R, int V, int64_t 
 
 umim_status token_logprobs_grad(const void *logits, int dtype, int R, int V, int64_t ld, const int32_t *n_dev,
                                 const int32_t *tokens, float temperature, const float *stats, const float *entropy,
-                                const float *g, const float *h, void *grad, int32_t *dev_status, cudaStream_t stream,
-                                int num_sms) {
-  GradArgs a{logits, R, V, ld, n_dev, tokens, 1.f / temperature, reinterpret_cast<const float2 *>(stats), entropy,
-             g, h, grad, dev_status};
+                                const float *g, const float *h, void *grad, int32_t *dev_status, cudaStream_t stream) {
+  const int vec = 16 / (int)dtype_bytes(dtype);
+  const int parts = ceil_div(V, kGradChunks * kUnroll * kThreads * vec);
+  const GradArgs a{logits, R, V, ld, n_dev, tokens, 1.f / temperature, kLog2e / temperature, parts,
+                   reinterpret_cast<const float2 *>(stats), entropy, g, h, grad, dev_status};
   auto *k = dtype == UMIM_DTYPE_BF16   ? token_logprobs_grad_kernel<ElemBf16>
             : dtype == UMIM_DTYPE_FP16 ? token_logprobs_grad_kernel<ElemFp16>
                                        : token_logprobs_grad_kernel<ElemFp32>;
-  return launch_rows(k, a, R, "logprobs.grad", stream);
+  trace_mark(stream, "logprobs.grad");
+  const cudaError_t e = launch_pdl(k, dim3((unsigned)R * (unsigned)parts), dim3(kThreads), 0, stream, a);
+  trace_mark(stream, nullptr);
+  return e == cudaSuccess ? UMIM_OK : UMIM_ERR_CUDA;
 }
 
 }  // namespace umim
