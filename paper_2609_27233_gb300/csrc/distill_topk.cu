@@ -58,13 +58,6 @@ struct TopkArgs {
   int32_t *status;
 };
 
-__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
-      "l"(src), "r"(bytes), "r"(smem_u32(bar))
-      : "memory");
-}
-
 inline size_t a256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // One CTA: the pair of every student row; the pairs are checked before anything is written.

@@ -20,6 +20,14 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// An asynchronous copy of whole vectors into shared memory; its bytes count on bar.
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+      "l"(src), "r"(bytes), "r"(smem_u32(bar))
+      : "memory");
+}
+
 // the maximum over the warp; NaN only where every lane holds one
 __device__ __forceinline__ float warp_max(float x) {
   float r;
@@ -42,7 +50,9 @@ __device__ __forceinline__ float2 half2_to_float2(uint32_t w) {
 // The three element types: VEC elements to a 16-byte vector, unpacked to and
 // packed from fp32 (packing rounds to nearest even).  max_words takes the
 // maximum of the elements of two 32-bit words place by place, word_max that of
-// one word's; both pass a number over a NaN.  order_key maps an element's bits
+// one word's; both pass a number over a NaN.  finite_words brings a 16-bit word's -inf up
+// to a finite value so far below that it may stand for it (see its type), and
+// keeps NaN.  order_key maps an element's bits
 // to a number that grows with its value, both zeros to one.
 __device__ __forceinline__ uint32_t order_key16(uint16_t b) {
   const uint32_t u = b == 0x8000u ? 0u : b;
@@ -63,6 +73,13 @@ struct ElemBf16 {
     return d;
   }
   static __device__ __forceinline__ T word_max_bits(uint32_t w) { return (T)max_words(w, w >> 16); }
+  // -1e30: beside a maximum of any size that fp32 exponents of differences are taken of
+  static constexpr bool kHasFinite = true;
+  static __device__ __forceinline__ uint32_t finite_words(uint32_t x) {
+    uint32_t d;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(0xf149f149u));
+    return d;
+  }
   static __device__ __forceinline__ uint32_t order_key(T b) { return order_key16(b); }
   static __device__ __forceinline__ T from_key(uint32_t k) { return from_key16(k); }
   static __device__ __forceinline__ float2 pair(uint32_t w) {
@@ -90,6 +107,8 @@ struct ElemFp16 {
     return d;
   }
   static __device__ __forceinline__ T word_max_bits(uint32_t w) { return (T)max_words(w, w >> 16); }
+  // no finite half is far enough below the others
+  static constexpr bool kHasFinite = false;
   static __device__ __forceinline__ uint32_t order_key(T b) { return order_key16(b); }
   static __device__ __forceinline__ T from_key(uint32_t k) { return from_key16(k); }
   static __device__ __forceinline__ float2 pair(uint32_t w) { return half2_to_float2(w); }
@@ -113,6 +132,7 @@ struct ElemFp32 {
     return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y)));
   }
   static __device__ __forceinline__ T word_max_bits(uint32_t w) { return __uint_as_float(w); }
+  static constexpr bool kHasFinite = false;   // a maximum per element, as it costs where it is used
   static __device__ __forceinline__ uint32_t order_key(T b) {
     const uint32_t u = b == 0.f ? 0u : __float_as_uint(b);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
@@ -140,6 +160,11 @@ __device__ __forceinline__ uint4 load_raw(const typename E::T *row, int e, int V
       }
     }
   return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ uint32_t word(const uint4 &u, int i) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  return w[i];
 }
 
 // words i and i + 1 of fp32 elements, or both elements of a 16-bit word, as two floats

@@ -69,7 +69,7 @@ struct Stats {
 };
 __device__ __forceinline__ Stats no_stats() { return Stats{-INFINITY, 0.f, 0.f}; }
 
-// s and w from the reference `from` to `to` >= from.  What underflows goes to 0, a NaN stays one.
+// s and w from their reference to `to`, which is not below it.  What underflows goes to 0, a NaN stays one.
 __device__ __forceinline__ void rebase(Stats &a, float to, float c) {
   if (!(a.m == to)) {
     const float d = (a.m - to) * c, f = ex2(d), s = a.s;
@@ -79,36 +79,47 @@ __device__ __forceinline__ void rebase(Stats &a, float to, float c) {
   }
 }
 
-// the warp's statistics in every lane
-__device__ __forceinline__ Stats warp_stats(Stats a, float c) {
-  rebase(a, warp_max(a.m), c);
+// the warp's statistics in every lane, at its maximum; top: the largest this lane has seen
+__device__ __forceinline__ Stats warp_stats(Stats a, float top, float c) {
+  rebase(a, warp_max(top), c);
   const float2 v = warp_sum2(make_float2(a.s, a.w));
   a.s = v.x;
   a.w = v.y;
   return a;
 }
 
+// 2^t is 0 from t = -150 on; where it is weighed with t, a t of -inf must not make that
+// no number.  (bf16 elements are kept finite two at a time instead, which
+// holds as long as |m c| < 2^24.)
+constexpr float kLeastT = -1000.f;
+
 // One thread's part: four vectors at a time.  t is one FMA, x c + b with
 // b = -m c rounded; the rounding r is common to a chunk and made good on its
-// sums, so that t is as exact for large |m| as (x - m) c.  Where r itself is large,
-// or a -inf is met (0 times -inf is no number), the sums come out as no
-// numbers and the chunk is done again the careful way; only NaN and +inf are
-// left as NaN by that.
+// sums, so that t is as exact for large |m| as (x - m) c.  Where r itself is large
+// (|m c| past 2^24, or no number) the chunk is read again and done the careful
+// way.  NaN and +inf leave s as NaN on both.
+//
+// The reference m follows the maximum only when that has come 2^16 past it:
+// until then the exponentials are as exact, and the sums far from overflowing.
+constexpr float kSlack = 16.f;
+
 template <class E>
 struct Running {
   Stats st = no_stats();
+  float top = -INFINITY;             // the maximum
   float b = 0.f, r = 0.f, rf = 1.f;
 
   // again(k): vector k of the chunk, read a second time
   template <class Again>
   __device__ __forceinline__ void add(const uint4 (&u)[kUnroll], uint32_t max_word, float c, Again again) {
     const float cm = E::to_float(E::word_max_bits(max_word));
-    if (cm > st.m) {
+    top = fmaxf(top, cm);
+    if ((cm - st.m) * c > kSlack) {
       rebase(st, cm, c);
       b = -cm * c;
       r = fmaf(-cm, c, -b);
       rf = ex2(r);
-      if (!(fabsf(r) <= 1.f)) b = NAN;   // |m c| past 2^24, or no number: the careful way
+      if (!(fabsf(r) <= 1.f)) b = NAN;   // the careful way
     }
     const float2 c2 = make_float2(c, c), b2 = make_float2(b, b);
     float2 s0 = make_float2(0.f, 0.f), s1 = s0, w0 = s0, w1 = s0;
@@ -116,8 +127,14 @@ struct Running {
     for (int k = 0; k < kUnroll; ++k)
 #pragma unroll
       for (int i = 0; i < E::VEC / 2; ++i) {
-        const float2 t = __ffma2_rn(pair_of<E>(u[k], i), c2, b2);
+        float2 x;
+        if constexpr (E::kHasFinite)
+          x = E::pair(E::finite_words(word(u[k], i)));
+        else
+          x = pair_of<E>(u[k], i);
+        float2 t = __ffma2_rn(x, c2, b2);
         const float2 e = make_float2(ex2(t.x), ex2(t.y));
+        if constexpr (!E::kHasFinite) t = make_float2(fmaxf(t.x, kLeastT), fmaxf(t.y, kLeastT));
         if (i & 1) {
           s1 = __fadd2_rn(s1, e);
           w1 = __ffma2_rn(e, t, w1);
@@ -129,7 +146,7 @@ struct Running {
     s0 = __fadd2_rn(s0, s1);
     w0 = __fadd2_rn(w0, w1);
     const float s = s0.x + s0.y, w = w0.x + w0.y;
-    if (s < INFINITY && w > -INFINITY) {
+    if (!isnan(b)) {
       st.s = fmaf(rf, s, st.s);
       st.w = fmaf(rf, fmaf(r, s, w), st.w);
     } else {
@@ -147,15 +164,13 @@ struct Running {
       for (int i = 0; i < E::VEC / 2; ++i) {
         const float2 x = pair_of<E>(u, i);
         float t = (x.x - m0) * c;
-        t = t < -1000.f ? -1000.f : t;   // 2^t is 0 from -150 on; a NaN passes
         float e = ex2(t);
         st.s += e;
-        st.w = fmaf(e, t, st.w);
+        st.w = fmaf(e, fmaxf(t, kLeastT), st.w);
         t = (x.y - m0) * c;
-        t = t < -1000.f ? -1000.f : t;
         e = ex2(t);
         st.s += e;
-        st.w = fmaf(e, t, st.w);
+        st.w = fmaf(e, fmaxf(t, kLeastT), st.w);
       }
     }
   }
@@ -166,201 +181,292 @@ struct Running {
 // ---------------------------------------------------------------------------
 // One cluster of C CTAs per row, each on one of C contiguous parts.  A warp
 // takes chunks of 4 x 32 vectors, a lane one vector of each 32: every logit is
-// read once, by 16-byte loads a chunk ahead of their use.
+// read once, by 16-byte loads a chunk ahead of their use.  (Copies of a chunk
+// into buffers of the warp's own, which leave registers for a fifth CTA on an SM,
+// measured slower: 231 against 222 us for 4096 rows of 128256 bf16 with 64
+// alternatives, 17 against 10 us for 128 rows without.)
 //
 // The alternatives need no second pass over the row.  Beside the sums, the
 // maximum of every segment of 32 consecutive elements goes to shared memory.
-// The n largest elements (by value, then by lowest id) lie in the n largest
-// segments (by maximum, then by lowest place): n segments before one that holds an
-// element each have an element before it.  So the segments' maxima are searched
-// for a threshold that n of them reach, and the few segments at or above
-// it are read again (64 or 128 bytes each, from L2).
+// In whatever way the row is divided into groups, the n-th largest of the groups'
+// maxima is a bound for the n best elements.  The groups here are the 256
+// that C threads each have read, whose maxima the threads hold anyway: a few
+// rounds of counting give a threshold that n of them reach, and not many
+// more.  The segments that reach it are read again (64 or 128 bytes each, from L2),
+// and of a row's elements about 256 ln(256 / (256 - n)) pass it (21 for n = 20, 177
+// for 128), which are ranked by counting.
 //
-// The threshold is taken over 256 groups of segments, one a thread, since the
-// n-th largest of the groups' maxima is a bound too: then about
-// 256 ln(256 / (256 - n)) elements pass it (21 for n = 20, 177 for 128), and a
-// thread each ranks them by counting.  Equal values can make them many more;
-// then the same bisections that gave the threshold pick exactly n segments, and
-// exactly n of their elements.
+// Equal values can make them more than 256.  The n best by (value, lowest id) lie in
+// the n best segments by (maximum, lowest place): n segments before one that
+// holds an element each have an element before it.  So bisections, by value and
+// then by place, pick exactly n segments, and of their elements exactly n.
+//
+// The search keeps its shared memory small (13 KB at 128256 bf16): what it takes
+// the L1 cache lacks, through which the loads in flight pass.  With 25 and 48
+// KB a CTA the pass alone took 175 and 189 us for 4096 such rows, against 156.
 //
 // All of it happens in shared memory and registers of the cluster: no
 // workspace, no atomics on global memory, the same bits in every call.
 constexpr int kSegment = 32;
+template <class E>
+__host__ __device__ constexpr int chunk_elems() {   // of a warp's chunk
+  return kUnroll * 32 * E::VEC;
+}
 
+constexpr int kCands = kThreads;     // candidates that are ranked, at most
+constexpr int kListed = 2 * kThreads; // segments that reach the threshold, at most (else the exact way)
+
+// Dynamic shared memory.
 template <class E>
 struct TopShared {
-  typename E::T *seg;      // [segments] maximum of each
-  uint16_t *list;          // [segments] those at or above the threshold
-  uint64_t *cand;          // [32 n] elements at or above it: (key, ~id)
-  uint64_t *merge;         // rank 0: [C][n] every CTA's best, descending
-  static size_t bytes(int slice, int n, int C) {
-    const size_t segs = (size_t)ceil_div(slice, kSegment);
-    return 8 * ((size_t)kSegment * n + (C > 1 ? (size_t)C * n : 0)) + (sizeof(typename E::T) + 2) * segs;
+  uint64_t *merge;         // rank 0 of several: [C][merge_cap(n)] every CTA's candidates
+  typename E::T *seg;      // [segments, up to a whole chunk] maximum of each
+  static __host__ __device__ int padded(int slice) {
+    return ceil_div(slice, chunk_elems<E>()) * (chunk_elems<E>() / kSegment);
   }
-  __device__ TopShared(uint8_t *p, int slice, int n, int C) {
-    const int segs = ceil_div(slice, kSegment);
-    cand = reinterpret_cast<uint64_t *>(p);
-    merge = cand + kSegment * n;
-    seg = reinterpret_cast<typename E::T *>(merge + (C > 1 ? C * n : 0));
-    list = reinterpret_cast<uint16_t *>(seg + segs);
+  // what a CTA tells rank 0: n at most, or the few more that the threshold let pass
+  static __host__ __device__ int merge_cap(int n) { return n > 32 ? n : 32; }
+  static size_t bytes(int slice, int n, int C) {
+    return 8 * (size_t)(C > 1 ? C * merge_cap(n) : 0) + sizeof(typename E::T) * (size_t)padded(slice);
+  }
+  __device__ TopShared(uint8_t *p, int slice, int n, int C) {   // seg starts on 16 bytes: C is even where it counts
+    merge = reinterpret_cast<uint64_t *>(p);
+    seg = reinterpret_cast<typename E::T *>(merge + (C > 1 ? C * merge_cap(n) : 0));
   }
 };
 
-// The largest k in [lo, hi] that at least n entries reach (lo where fewer reach it);
-// count(k): how many do, the same in every thread.
-template <class Count>
-__device__ uint32_t largest_reached(uint32_t lo, uint32_t hi, int n, Count count) {
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo + 1) / 2;
-    if (count(mid) >= n)
-      lo = mid;
-    else
-      hi = mid - 1;
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t key_of(uint64_t e) { return (uint32_t)(e >> 32); }
+__device__ __forceinline__ uint32_t id_of(uint64_t e) { return ~(uint32_t)e; }
+__device__ __forceinline__ uint64_t entry(uint32_t key, uint32_t id) { return ((uint64_t)key << 32) | (uint32_t)~id; }
+
+// The bits of vector word w[j / 2] (16-bit elements) or w[j] that are element j.
+template <class E>
+__device__ __forceinline__ typename E::T element(const uint4 &u, int j) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  if constexpr (E::VEC == 8)
+    return (typename E::T)(w[j / 2] >> (16 * (j & 1)));
+  else
+    return __uint_as_float(w[j]);
+}
+
+// the warp's values in descending order (a bitonic sort)
+__device__ __forceinline__ uint64_t warp_sorted(uint64_t v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      const uint64_t o = __shfl_xor_sync(0xffffffffu, v, j);
+      const bool larger = ((lane & j) == 0) == ((lane & k) == 0);   // this lane keeps the larger one
+      v = (v > o) == larger ? v : o;
+    }
+  return v;
+}
+
+// The place, among all that the CTA's threads take, of the first of the `count` that this
+// thread takes; *total (shared, 0 before) counts them.  One atomic per warp.
+__device__ __forceinline__ int take_places(int count, int *total) {
+  const int lane = threadIdx.x & 31;
+  int sum = count;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int below = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += below;
   }
-  return lo;
+  int base = 0;
+  if (lane == 31 && sum > 0) base = atomicAdd(total, sum);
+  return __shfl_sync(0xffffffffu, base, 31) + sum - count;
 }
 
-// how many of M entries, held by the CTA's threads in turn, satisfy pred
-template <class Pred>
-__device__ int count_entries(int M, Pred pred) {
-  int c = 0;
-  for (int i = threadIdx.x; i - (int)threadIdx.x < M; i += kThreads) c += __syncthreads_count(i < M && pred(i));
-  return c;
-}
-
-// Exactly the n first of M > n entries by (key descending, id ascending), as a key and the
-// largest id that is still in at that key; ids are below `ids`.
+// The n first of the CTA's entries by (key descending, id ascending), of which there are
+// more: a key, and the largest id that is still in at that key.  lo: a key that
+// more than n reach; hi: the largest; ids are below `ids`.  own(pred): how
+// many of this thread's entries satisfy pred(key, id).
 struct Cut {
   uint32_t key, id;
   __device__ bool in(uint32_t k, uint32_t i) const { return k > key || (k == key && i <= id); }
 };
-template <class Key, class Id>
-__device__ Cut cut_at(int M, int n, uint32_t lo, uint32_t hi, uint32_t ids, Key key, Id id) {
+template <class Own>
+__device__ Cut cut_at(int n, uint32_t lo, uint32_t hi, uint32_t ids, Own own) {
+  __shared__ int part[2][kWarps];
+  int turn = 0;
+  const auto count = [&](auto pred) {   // over the CTA
+    const int warp_sum = __reduce_add_sync(0xffffffffu, own(pred));
+    if ((threadIdx.x & 31) == 0) part[turn][threadIdx.x >> 5] = warp_sum;
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) sum += part[turn][i];
+    turn ^= 1;   // the next count's barrier is before these are written again
+    return sum;
+  };
   Cut c;
-  c.key = largest_reached(lo, hi, n, [&](uint32_t k) { return count_entries(M, [&](int i) { return key(i) >= k; }); });
-  const int left = n - count_entries(M, [&](int i) { return key(i) > c.key; });
-  // the smallest id with `left` equal entries at or below it
+  while (lo < hi) {   // the largest key that n reach
+    const uint32_t mid = lo + (hi - lo + 1) / 2;
+    if (count([&](uint32_t k, uint32_t) { return k >= mid; }) >= n)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  c.key = lo;
+  const int left = n - count([&](uint32_t k, uint32_t) { return k > c.key; });
   uint32_t a = 0, b = ids - 1;
-  while (a < b) {
+  while (a < b) {     // the smallest id with `left` equal entries at or below it
     const uint32_t mid = (a + b) / 2;
-    if (count_entries(M, [&](int i) { return key(i) == c.key && id(i) <= mid; }) >= left)
+    if (count([&](uint32_t k, uint32_t i) { return k == c.key && i <= mid; }) >= left)
       b = mid;
     else
       a = mid + 1;
   }
   c.id = a;
+  __syncthreads();   // the last count has been read
   return c;
 }
 
-__device__ __forceinline__ uint32_t key_of(uint64_t e) { return (uint32_t)(e >> 32); }
-__device__ __forceinline__ uint32_t id_of(uint64_t e) { return ~(uint32_t)e; }
-
-// This CTA's n best elements of row[beg, end), best first, to sorted[]: (key, ~id); sorted[0, n) comes in as zeros.
+// The elements of row[beg, end) that reach `least`, in any order, to cand[]; where they
+// are more than kCands, the n best.  hi: the largest key.  Returns how many.
 // Neither NaN nor +inf is among them.
 template <class E>
-__device__ void best_of_slice(const TopShared<E> &sh, const typename E::T *row, int beg, int end, int n,
-                              uint64_t *sorted, int32_t *status) {
-  __shared__ uint32_t s_hi[kWarps], s_lo[kWarps];
-  __shared__ int s_listed, s_held, s_kept;
-  __shared__ uint64_t s_keep[kMaxTop];
+__device__ int gather_best(const typename E::T *seg, const typename E::T *row, int beg, int end, int n, uint32_t least,
+                           uint32_t hi, uint64_t *cand, int32_t *status) {
+  __shared__ int s_listed, s_held;
+  __shared__ uint16_t list[kListed];
   const int tid = threadIdx.x, segs = ceil_div(end - beg, kSegment);
-  const uint32_t none = E::order_key(E::kNegInf);
-  const auto seg_key = [&](int i) { return E::order_key(sh.seg[i]); };
 
-  // a group of segments per thread; lanes start at different places of theirs (banks)
-  const int G = ceil_div(segs, kThreads), g0 = min(tid * G, segs), gn = min(G, segs - g0);
-  uint32_t group = none;
-  for (int j = 0, k = gn > 0 ? tid % gn : 0; j < gn; ++j) {
-    group = max(group, seg_key(g0 + k));
-    k = k + 1 == gn ? 0 : k + 1;
-  }
-  {
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, group), lo = __reduce_min_sync(0xffffffffu, group);
-    if ((tid & 31) == 0) {
-      s_hi[tid >> 5] = hi;
-      s_lo[tid >> 5] = lo;
-    }
-    if (tid == 0) s_listed = s_held = s_kept = 0;
-  }
-  __syncthreads();
-  uint32_t hi = s_hi[0], lo = s_lo[0];
+  using T = typename E::T;
+  const float least_x = E::to_float(E::from_key(least));   // a bound in passing: x >= it as its key >= least
+  // the segments that `in` takes, to list[]; returns how many
+  const auto list_segments = [&](auto in) {
+    if (tid == 0) s_listed = 0;
+    __syncthreads();
+    for (int i = tid * E::VEC; i < segs; i += kThreads * E::VEC) {
+      const uint4 u = *reinterpret_cast<const uint4 *>(seg + i);
+      const uint32_t top = E::max_words(E::max_words(u.x, u.y), E::max_words(u.z, u.w));
+      if (E::to_float(E::word_max_bits(top)) >= least_x)
 #pragma unroll
-  for (int i = 1; i < kWarps; ++i) {
-    hi = max(hi, s_hi[i]);
-    lo = min(lo, s_lo[i]);
-  }
-  if (hi == none) return;   // nothing above -inf (the same in every thread)
-  lo = max(lo, none + 1);
-  const uint32_t least =
-      largest_reached(lo, hi, n, [&](uint32_t k) { return __syncthreads_count(group >= k); });
-
-  if (group >= least)
-    for (int j = 0; j < gn; ++j)
-      if (seg_key(g0 + j) >= least) sh.list[atomicAdd(&s_listed, 1)] = (uint16_t)(g0 + j);
-  __syncthreads();
-  const int listed = s_listed;
-
-  // the elements at or above `from` of the listed segments that `in` takes
-  constexpr int kVecs = kSegment / E::VEC;
-  const auto gather = [&](uint32_t from, auto in) {
-    for (int i = tid; i < listed * kVecs; i += kThreads) {
-      const int seg = sh.list[i / kVecs];
-      if (!in_bounds(seg, segs, status, kSiteLogprobSegment) || !in(seg)) continue;
-      const int e = beg + seg * kSegment + (i % kVecs) * E::VEC;
-      if (e >= end) continue;
-      const uint4 u = load_raw<E>(row, e, end);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int j = 0; j < E::VEC; ++j) {
-        typename E::T x;
-        if constexpr (E::VEC == 8)
-          x = (typename E::T)(w[j / 2] >> (16 * (j & 1)));
-        else
-          x = __uint_as_float(w[j]);
-        const uint32_t k = E::order_key(x);
-        if (k >= from && e + j < end) {
-          const int at = atomicAdd(&s_held, 1);
-          if (at < kSegment * n) sh.cand[at] = ((uint64_t)k << 32) | (uint32_t)~(uint32_t)(e + j);
-        }
-      }
+        for (int j = 0; j < E::VEC; ++j)
+          if (in(element<E>(u, j), (uint32_t)(i + j))) {
+            const int at = atomicAdd(&s_listed, 1);
+            if (at < kListed) list[at] = (uint16_t)(i + j);
+          }
     }
     __syncthreads();
+    return s_listed;
   };
-  gather(least, [](int) { return true; });
-  if (s_held > kSegment * n) {   // many equal ones: n segments exactly
-    const Cut cut = cut_at(listed, n, least, hi, (uint32_t)segs, [&](int i) { return seg_key(sh.list[i]); },
-                           [&](int i) { return (uint32_t)sh.list[i]; });
+
+  // the i-th vector of the listed segments, the first element's id to e
+  constexpr int kVecs = kSegment / E::VEC;
+  const auto load_listed = [&](int i, int &e) {
+    int s = list[i / kVecs];
+    if (!in_bounds(s, segs, status, kSiteLogprobSegment)) s = 0;
+    e = beg + s * kSegment + (i % kVecs) * E::VEC;
+    return load_raw<E>(row, e, end);
+  };
+  // The elements of listed segments that `in` takes, to cand[]; returns how many.  Two vectors a
+  // thread on their way at once.
+  const auto gather = [&](int listed, auto in) {
     if (tid == 0) s_held = 0;
     __syncthreads();
-    gather(cut.key, [&](int seg) { return cut.in(seg_key(seg), (uint32_t)seg); });
-  }
-  const uint64_t *best = sh.cand;
-  int M = min(s_held, kSegment * n);
-  if (M > kThreads) {            // more than a thread each: n elements exactly
-    const Cut cut = cut_at(M, n, least, hi, (uint32_t)end, [&](int i) { return key_of(sh.cand[i]); },
-                           [&](int i) { return id_of(sh.cand[i]); });
-    for (int i = tid; i < M; i += kThreads)
-      if (cut.in(key_of(sh.cand[i]), id_of(sh.cand[i]))) {
-        const int at = atomicAdd(&s_kept, 1);
-        if (in_bounds(at, kMaxTop, status, kSiteLogprobRank)) s_keep[at] = sh.cand[i];
-      }
+    const auto take = [&](const uint4 &u, int e) {
+      const uint32_t top = E::max_words(E::max_words(u.x, u.y), E::max_words(u.z, u.w));
+      if (E::to_float(E::word_max_bits(top)) >= least_x)
+#pragma unroll
+        for (int j = 0; j < E::VEC; ++j) {
+          const T x = element<E>(u, j);
+          if (in(x, (uint32_t)(e + j))) {
+            const int at = atomicAdd(&s_held, 1);
+            if (at < kCands) cand[at] = entry(E::order_key(x), (uint32_t)(e + j));
+          }
+        }
+    };
+    for (int i = tid; i < listed * kVecs; i += 2 * kThreads) {
+      int e, e2 = 0;
+      const bool two = i + kThreads < listed * kVecs;
+      const uint4 u = load_listed(i, e);
+      uint4 u2;
+      if (two) u2 = load_listed(i + kThreads, e2);
+      take(u, e);
+      if (two) take(u2, e2);
+    }
     __syncthreads();
-    best = s_keep;
-    M = s_kept;
+    return s_held;
+  };
+  const auto reaches = [&](T x, uint32_t) { return E::to_float(x) >= least_x; };
+  const int listed = list_segments(reaches);
+  if (listed <= kListed) {
+    const int held = gather(listed, reaches);
+    if (held <= kCands) return held;
   }
-  if (tid < M) {
-    const uint64_t mine = best[tid];
-    int rank = 0;
-    for (int i = 0; i < M; ++i) rank += best[i] > mine;
-    if (rank < n) sorted[rank] = mine;
-  }
+  // Many equal ones: n segments exactly, then n elements.  More than n segments are above
+  // `least`, unless all of it lies in fewer.
+  Cut cut{least, (uint32_t)segs};
+  if (listed > n)
+    cut = cut_at(n, least, hi, (uint32_t)segs, [&](auto pred) {
+      int c = 0;
+      for (int i = tid; i < segs; i += kThreads) {
+        const uint32_t k = E::order_key(seg[i]);
+        c += k >= least && pred(k, (uint32_t)i);
+      }
+      return c;
+    });
+  const int kept = list_segments([&](T x, uint32_t i) { return cut.in(E::order_key(x), i); });
+  const Cut best = cut_at(n, cut.key, hi, (uint32_t)end, [&](auto pred) {
+    int c = 0;
+    for (int i = tid; i < kept * kVecs; i += kThreads) {
+      int e;
+      const uint4 u = load_listed(i, e);
+#pragma unroll
+      for (int j = 0; j < E::VEC; ++j) {
+        const uint32_t k = E::order_key(element<E>(u, j));
+        c += k >= cut.key && pred(k, (uint32_t)(e + j));
+      }
+    }
+    return c;
+  });
+  return gather(kept, [&](T x, uint32_t i) { return best.in(E::order_key(x), i); });
 }
+
+// The n first of the M > n entries of from[], in any order, to cand[] (which may be from).
+__device__ void keep_best(const uint64_t *from, int M, int n, uint32_t lo, uint32_t hi, int V, uint64_t *cand) {
+  __shared__ int s_kept;
+  if (threadIdx.x == 0) s_kept = 0;
+  const Cut cut = cut_at(n, lo, hi, (uint32_t)V, [&](auto pred) {
+    int c = 0;
+    for (int i = threadIdx.x; i < M; i += kThreads) c += pred(key_of(from[i]), id_of(from[i]));
+    return c;
+  });
+  constexpr int kHold = kMaxCluster * kMaxTop / kThreads;   // entries of a thread, at most
+  uint64_t held[kHold];
+  int count = 0;
+#pragma unroll
+  for (int k = 0; k < kHold; ++k) {
+    const int i = threadIdx.x + k * kThreads;
+    held[k] = i < M && cut.in(key_of(from[i]), id_of(from[i])) ? from[i] : 0;
+    count += held[k] != 0;
+  }
+  __syncthreads();   // all of from has been read
+  int at = take_places(count, &s_kept);
+#pragma unroll
+  for (int k = 0; k < kHold; ++k)
+    if (held[k] != 0) cand[at++] = held[k];
+  __syncthreads();
+}
+
+// What the warps of a cluster tell each other: their sums, and the least of their groups' maxima.
+struct __align__(16) WarpPart {
+  float m, s, w, least;
+};
 
 template <class E, bool TOP>
 __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs a) {
-  extern __shared__ __align__(16) uint8_t dyn[];
-  __shared__ Stats s_warp[kWarps], s_cta[kMaxCluster];
-  __shared__ uint64_t s_sorted[kMaxTop];
+  extern __shared__ __align__(128) uint8_t dyn[];
+  __shared__ WarpPart s_parts[kMaxCluster * kWarps];
+  __shared__ uint32_t s_group[kThreads];
+  __shared__ __align__(16) uint64_t s_cand[kCands];
+  __shared__ int s_count[kMaxCluster];
   griddep_wait();
   griddep_launch();
   const int C = (int)cluster_size(), rank = C > 1 ? (int)cluster_ctarank() : 0;
@@ -384,14 +490,14 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
   const typename E::T *row = static_cast<const typename E::T *>(a.logits) + (int64_t)r * a.ld;
   const int beg = min(rank * a.slice, V), end = min(beg + a.slice, V);
   const TopShared<E> sh(dyn, a.slice, n, C);
+  if (C > 1) cluster_arrive();   // what is pushed to a CTA waits until it runs
   float x_t = 0.f;
   if (rank == 0 && tid == 0) x_t = E::to_float(row[token]);
 
   // ---- one pass over this CTA's part ----
-  constexpr int kChunk = kUnroll * 32 * E::VEC;   // elements of a warp's chunk
+  constexpr int kChunk = chunk_elems<E>();
   const float c = a.c;
   Running<E> run;
-  uint4 u[kUnroll], next[kUnroll];
   const auto load = [&](uint4 (&v)[kUnroll], int e0) {   // chunk at element e0
     if (e0 + kChunk <= end) {
 #pragma unroll
@@ -402,12 +508,10 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
       for (int k = 0; k < kUnroll; ++k) v[k] = load_raw<E>(row, e0 + (k * 32 + lane) * E::VEC, end);
     }
   };
-  int e0 = beg + warp * kChunk;
-  load(next, e0);
-  for (; e0 < end; e0 += kWarps * kChunk) {
-#pragma unroll
-    for (int k = 0; k < kUnroll; ++k) u[k] = next[k];
-    load(next, e0 + kWarps * kChunk);
+  // where this lane's segment of the warp's chunks goes: the one of the four vectors from
+  // vector (lane % 4) * 32 + lane / 4 * 4 of a chunk on
+  typename E::T *seg_at = sh.seg + (warp * kChunk + ((lane & 3) * 32 + (lane & ~3)) * E::VEC) / kSegment;
+  const auto take = [&](const uint4 (&u)[kUnroll], int e0) {
     uint32_t top[kUnroll];
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k)
@@ -417,82 +521,172 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
       // that of its four for vector lane % 4.
       static_assert(kUnroll == 4, "four vectors among four lanes");
       const bool odd = lane & 1, high = lane & 2;
-      uint32_t p = E::max_words(odd ? top[1] : top[0], __shfl_xor_sync(0xffffffffu, odd ? top[0] : top[1], 1));
-      uint32_t q = E::max_words(odd ? top[3] : top[2], __shfl_xor_sync(0xffffffffu, odd ? top[2] : top[3], 1));
-      uint32_t v = E::max_words(high ? q : p, __shfl_xor_sync(0xffffffffu, high ? p : q, 2));
-      const int vec = (lane & 3) * 32 + (lane & ~3);   // the first of the four in the chunk
-      int at = (e0 - beg + vec * E::VEC) / kSegment;
-      if (E::VEC == 4) v = E::max_words(v, __shfl_xor_sync(0xffffffffu, v, 4));   // eight lanes make a segment
-      if ((E::VEC == 8 || !(lane & 4)) && at < ceil_div(end - beg, kSegment)) sh.seg[at] = E::word_max_bits(v);
+      const uint32_t p = E::max_words(odd ? top[1] : top[0], __shfl_xor_sync(0xffffffffu, odd ? top[0] : top[1], 1));
+      const uint32_t q = E::max_words(odd ? top[3] : top[2], __shfl_xor_sync(0xffffffffu, odd ? top[2] : top[3], 1));
+      uint32_t m = E::max_words(high ? q : p, __shfl_xor_sync(0xffffffffu, high ? p : q, 2));
+      if (E::VEC == 4) m = E::max_words(m, __shfl_xor_sync(0xffffffffu, m, 4));   // eight lanes make a segment
+      if (E::VEC == 8 || !(lane & 4)) *seg_at = E::word_max_bits(m);
+      seg_at += kWarps * kChunk / kSegment;
     }
     run.add(u, E::max_words(E::max_words(top[0], top[1]), E::max_words(top[2], top[3])), c,
             [&](int k) { return load_raw<E>(row, e0 + (k * 32 + lane) * E::VEC, end); });
+  };
+  {   // two chunks in turn, each loaded while the other is worked on
+    constexpr int kStride = kWarps * kChunk;
+    uint4 u[kUnroll], v[kUnroll];
+    int e0 = beg + warp * kChunk;
+    load(u, e0);
+    for (; e0 < end; e0 += 2 * kStride) {
+      load(v, e0 + kStride);
+      take(u, e0);
+      if (e0 + kStride >= end) break;
+      load(u, e0 + 2 * kStride);
+      take(v, e0 + kStride);
+    }
   }
 
-  // ---- the CTA's sums and alternatives ----
-  const Stats ws = warp_stats(run.st, c);
-  if (lane == 0) s_warp[warp] = ws;
-  __syncthreads();
-  Stats cta = lane < kWarps ? s_warp[lane] : no_stats();
-  cta = warp_stats(cta, c);
-  if constexpr (TOP) {
-    for (int i = tid; i < n; i += kThreads) s_sorted[i] = 0;
-    // NaN and +inf have no place in the order, and a row that holds one has no alternatives
-    if (cta.s < INFINITY) best_of_slice<E>(sh, row, beg, end, n, s_sorted, a.status);
-    __syncthreads();
-  }
-  if (C > 1) {   // to rank 0
-    cluster_sync_all();   // every CTA of the cluster runs
-    if (tid == 0) {
-      const uint32_t to = peer_addr(&s_cta[rank], 0);
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(cta.m) : "memory");
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4), "f"(cta.s) : "memory");
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 8), "f"(cta.w) : "memory");
-    }
-    for (int i = tid; i < n; i += kThreads)
-      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer_addr(&sh.merge[rank * n + i], 0)), "l"(s_sorted[i])
-                   : "memory");
-    cluster_sync_all();
-    if (rank != 0) return;
-    cta = lane < C ? s_cta[lane] : no_stats();
-    cta = warp_stats(cta, c);
-    if constexpr (TOP) {   // every entry's place among the C lists
-      for (int i = tid; i < n; i += kThreads) s_sorted[i] = 0;
+  // ---- the row's sums, and a threshold for its alternatives ----
+  {
+    float group = run.top;   // the maximum of this thread's group: C threads that lie side by side
+    for (int o = 1; o < C; o <<= 1) group = fmaxf(group, __shfl_xor_sync(0xffffffffu, group, o));
+    const Stats ws = warp_stats(run.st, run.top, c);
+    const WarpPart p{ws.m, ws.s, ws.w, -warp_max(-group)};
+    const int place = rank * kWarps + warp;
+    const uint32_t key = E::order_key(E::from_float(group));
+    const int at = (rank * kThreads + tid) / C;   // the group's, among the row's 256
+    if (C == 1) {
+      if (lane == 0) s_parts[place] = p;
+      if (TOP) s_group[at] = key;
       __syncthreads();
-      for (int i = tid; i < C * n; i += kThreads) {
-        const uint64_t mine = sh.merge[i];
-        int place = i % n;
-        for (int l = 0; l < C && mine; ++l) {
-          if (l == i / n) continue;
-          int lo = 0, hi = n;   // entries of list l before mine
-          while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (sh.merge[l * n + mid] > mine)
-              lo = mid + 1;
-            else
-              hi = mid;
-          }
-          place += lo;
-        }
-        if (mine && place < n) s_sorted[place] = mine;
+    } else {
+      cluster_wait();
+      if (lane < C) {
+        const uint32_t to = peer_addr(&s_parts[place], (uint32_t)lane);
+        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(p.m), "f"(p.s), "f"(p.w),
+                     "f"(p.least)
+                     : "memory");
       }
-      __syncthreads();
+      // thread j of a group tells CTA j
+      if (TOP)
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(&s_group[at], (uint32_t)(tid % C))), "r"(key)
+                     : "memory");
+      cluster_sync_all();
     }
   }
+  Stats all = no_stats();
+  float least_group = INFINITY;
+  for (int i = lane; i < C * kWarps; i += 32) {
+    const WarpPart p = s_parts[i];
+    Stats q{p.m, p.s, p.w};
+    least_group = fminf(least_group, p.least);
+    const float to = fmaxf(all.m, q.m);
+    rebase(all, to, c);
+    rebase(q, to, c);
+    all.s += q.s;
+    all.w += q.w;
+  }
+  all = warp_stats(all, all.m, c);
+  // NaN and +inf have no place in the order, and a row that holds one has no alternatives
+  const bool bad = !(all.s < INFINITY), empty = all.m == -INFINITY && !bad;
+
+  int M = 0;   // the candidates, in s_cand of rank 0
+  if constexpr (TOP) {
+    if (!bad && !empty) {
+      const uint32_t hi = E::order_key(E::from_float(all.m)), none = E::order_key(E::kNegInf);
+      const float lg = -warp_max(-least_group);
+      uint32_t least = max(E::order_key(E::from_float(lg)), none + 1);
+      {   // largest_reached, until not many more than n reach it
+        const uint32_t group = s_group[tid];
+        const int most = min(n + n / 8 + 4, kThreads / 2 + 8);   // about 194 candidates, 256 being the limit
+        uint32_t top = hi;
+        while (least < top) {
+          const uint32_t mid = least + (top - least + 1) / 2;
+          const int reach = __syncthreads_count(group >= mid);
+          if (reach >= n)
+            least = mid;
+          else
+            top = mid - 1;
+          if (reach >= n && reach <= most) break;
+        }
+      }
+      M = gather_best<E>(sh.seg, row, beg, end, n, least, hi, s_cand, a.status);
+      if (C > 1) {   // to rank 0
+        const int cap = sh.merge_cap(n);
+        if (M > cap) {
+          keep_best(s_cand, M, n, least, hi, V, s_cand);
+          M = n;
+        }
+        if (tid == 0)
+          asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(peer_addr(&s_count[rank], 0)), "r"(M) : "memory");
+        if (tid < M)
+          asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer_addr(&sh.merge[rank * cap + tid], 0)),
+                       "l"(s_cand[tid])
+                       : "memory");
+        cluster_sync_all();
+        if (rank != 0) return;
+        // side by side: list k moves down to the end of list k - 1
+        M = s_count[0];
+        for (int k = 1; k < C; ++k) {
+          const int count = s_count[k];
+          const uint64_t e = tid < count ? sh.merge[k * cap + tid] : 0;
+          __syncthreads();
+          if (tid < count) sh.merge[M + tid] = e;
+          M += count;
+        }
+        __syncthreads();
+        if (M > kCands) {
+          keep_best(sh.merge, M, n, least, hi, V, s_cand);
+          M = n;
+        } else {
+          if (tid < M) s_cand[tid] = sh.merge[tid];
+          __syncthreads();
+        }
+      }
+    }
+  }
+  if (rank != 0) return;
 
   // ---- outputs ----
-  const bool bad = !(cta.s < INFINITY), empty = cta.m == -INFINITY && !bad;
-  const float m0 = empty ? 0.f : cta.m, l = bad ? NAN : empty ? 0.f : logf(cta.s);
+  const float m0 = empty ? 0.f : all.m, l = bad ? NAN : empty ? 0.f : logf(all.s);
   if (tid == 0) {
     if (a.logprobs) a.logprobs[r] = bad ? NAN : (x_t - m0) * a.inv_t - l;
-    if (a.entropy) a.entropy[r] = bad ? NAN : empty ? 0.f : l - kLn2 * (cta.w / cta.s);
-    if (a.stats) a.stats[r] = bad ? make_float2(NAN, NAN) : make_float2(cta.m, l);
+    if (a.entropy) a.entropy[r] = bad ? NAN : empty ? 0.f : l - kLn2 * (all.w / all.s);
+    if (a.stats) a.stats[r] = bad ? make_float2(NAN, NAN) : make_float2(all.m, l);
   }
-  for (int i = tid; i < n; i += kThreads) {
-    const uint64_t e = bad ? 0 : s_sorted[i];
-    a.top_ids[(int64_t)r * n + i] = e ? (int)id_of(e) : -1;
-    a.top_logprobs[(int64_t)r * n + i] =
-        bad ? NAN : e ? (E::to_float(E::from_key(key_of(e))) - m0) * a.inv_t - l : -INFINITY;
+  if constexpr (TOP) {
+    uint64_t mine;
+    int place = 0;
+    if (M <= kCands / 2) {   // an entry's place is how many come before it: P threads side by side count for it
+      int P = 1;
+      while (2 * P * M <= kThreads && P < 32) P *= 2;
+      const int i = tid / P;
+      mine = i < M ? s_cand[i] : 0;
+#pragma unroll 8
+      for (int k = tid % P; k < M; k += P) place += s_cand[k] > mine;
+      for (int o = 1; o < P; o <<= 1) place += __shfl_xor_sync(0xffffffffu, place, o);
+      if (tid % P != 0) mine = 0;
+    } else {                 // every warp sorts its 32, then looks for its own in the other warps' lists
+      mine = warp_sorted(tid < M ? s_cand[tid] : 0);
+      __syncthreads();
+      s_cand[tid] = mine;
+      __syncthreads();
+      int before[kWarps] = {};
+#pragma unroll
+      for (int step = 16; step > 0; step >>= 1)
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w)
+          if (s_cand[w * 32 + before[w] + step - 1] > mine) before[w] += step;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) place += before[w] + (before[w] == 31 && s_cand[w * 32 + 31] > mine);
+    }
+    if (mine != 0 && place < n && in_bounds(place, n, a.status, kSiteLogprobRank)) {
+      a.top_ids[(int64_t)r * n + place] = (int)id_of(mine);
+      a.top_logprobs[(int64_t)r * n + place] = (E::to_float(E::from_key(key_of(mine))) - m0) * a.inv_t - l;
+    }
+    if (tid >= M && tid < n) {
+      a.top_ids[(int64_t)r * n + tid] = -1;
+      a.top_logprobs[(int64_t)r * n + tid] = bad ? NAN : -INFINITY;
+    }
   }
 }
 
@@ -550,7 +744,7 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_grad_kernel(GradAr
 #pragma unroll
       for (int i = 0; i < E::VEC / 2; ++i) {
         float2 t = __ffma2_rn(__fadd2_rn(pair_of<E>(u[k], i), nm2), c2, nl2);
-        t = make_float2(fmaxf(t.x, -1000.f), fmaxf(t.y, -1000.f));   // of -inf: 0 times it would be no number
+        t = make_float2(fmaxf(t.x, kLeastT), fmaxf(t.y, kLeastT));
         const float2 v = __fmul2_rn(make_float2(ex2(t.x), ex2(t.y)), __ffma2_rn(t, B2, A2));
         d[2 * i] = v.x;
         d[2 * i + 1] = v.y;
@@ -561,7 +755,7 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_grad_kernel(GradAr
 #pragma unroll
         for (int j = 0; j < E::VEC; ++j)
           if (e + j == token) {
-            const float z = (x[j] - st.x) * a.inv_t - st.y, t = fmaxf(z * kLog2e, -1000.f);
+            const float z = (x[j] - st.x) * a.inv_t - st.y, t = fmaxf(z * kLog2e, kLeastT);
             d[j] = -g * expm1f(z) + ex2(t) * fmaf(t, B, A + g);
           }
       }
@@ -589,10 +783,10 @@ umim_status launch_logprobs(LogprobArgs a, int C, cudaStream_t stream) {
   return e == cudaSuccess ? UMIM_OK : UMIM_ERR_CUDA;
 }
 
-// CTAs per row: enough that the SMs hold four each, where a part is still worth a CTA (2048 elements).
+// CTAs per row: as many as the SMs hold at once, where a part is still worth a CTA (2048 elements).
 int cluster_for(int R, int V, int num_sms) {
   int C = 1;
-  while (C < kMaxCluster && (int64_t)R * C < 4 * num_sms && V / (2 * C) >= 2048) C *= 2;
+  while (C < kMaxCluster && (int64_t)R * 2 * C <= 4 * num_sms && V / (2 * C) >= 2048) C *= 2;
   return C;
 }
 
