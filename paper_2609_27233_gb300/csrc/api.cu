@@ -414,7 +414,7 @@ const char *umim_debug_site_name(int32_t status) {
       "distill.pair",
       "rules.span_slot",
       "rules.span_token",
-      "distill_topk.teacher_row",
+      "distill_topk.student_row",
       "distill_topk.pair",
       "distill_topk.entry",
       "logprobs.segment",

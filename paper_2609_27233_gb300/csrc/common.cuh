@@ -73,7 +73,7 @@ enum DebugSite : int32_t {
   kSiteDistillPair = 21,
   kSiteRulesSpanSlot = 22,
   kSiteRulesSpanToken = 23,
-  kSiteTopkTeacherRow = 24,
+  kSiteTopkStudentRow = 24,
   kSiteTopkPair = 25,
   kSiteTopkEntry = 26,
   kSiteLogprobSegment = 27,

@@ -28,6 +28,13 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
       : "memory");
 }
 
+// An asynchronous store of 16 bytes into a CTA of the cluster; they count on its mbarrier.
+__device__ __forceinline__ void st_async16(uint32_t to, float4 v, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
+               "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(bar)
+               : "memory");
+}
+
 // the maximum over the warp; NaN only where every lane holds one
 __device__ __forceinline__ float warp_max(float x) {
   float r;
