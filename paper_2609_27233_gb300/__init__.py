@@ -577,6 +577,17 @@ def _logit_rows(logits, vocab, what="logits"):
     return logits.data_ptr(), _DTYPE[logits.dtype], shape[0], vocab, ld
 
 
+def _grad_rows(grad, logits, dtype, R, V, ld):
+    """(grad, its address): a gradient like logits, checked or made."""
+    if grad is None:
+        grad = torch.empty_strided((R, logits.shape[1]), (ld, 1), dtype=logits.dtype, device=logits.device)
+        return grad, grad.data_ptr()
+    ptr, g_dtype, g_R, _, g_ld = _logit_rows(grad, V, "grad")
+    if g_dtype != dtype or g_R != R or g_ld != ld:
+        raise ValueError("grad must have the logits' type, rows and row stride")
+    return grad, ptr
+
+
 def _vector(t, n, dtype, what):
     """The address of a contiguous device tensor of n elements, or None."""
     if t is None:
@@ -597,18 +608,27 @@ def umim_token_logprobs(logits, token_ids=None, n_top=0, vocab=None, temperature
     temperature)), top_ids int32 and top_logprobs fp32 [R][n_top]; logprobs is
     None without tokens, the last two are None where n_top is 0."""
     x, dtype, R, V, ld = _logit_rows(logits, vocab)
+    if n_top < 0:
+        raise ValueError("n_top must not be negative")
     if out is None:
-        f32 = lambda *n: torch.empty(n, dtype=torch.float32, device=logits.device)
-        out = dict(logprobs=None if token_ids is None else f32(R), entropy=f32(R), stats=f32(R, 2),
-                   top_ids=torch.empty((R, n_top), dtype=torch.int32, device=logits.device) if n_top else None,
-                   top_logprobs=f32(R, n_top) if n_top else None)
+        # (separate allocations: views into one took 3 us longer)
+        dev, f32 = logits.device, torch.float32
+        logprobs = None if token_ids is None else torch.empty(R, dtype=f32, device=dev)
+        entropy = torch.empty(R, dtype=f32, device=dev)
+        stats = torch.empty((R, 2), dtype=f32, device=dev)
+        top_ids = torch.empty((R, n_top), dtype=torch.int32, device=dev) if n_top else None
+        top_logprobs = torch.empty((R, n_top), dtype=f32, device=dev) if n_top else None
+        out = dict(logprobs=logprobs, entropy=entropy, stats=stats, top_ids=top_ids, top_logprobs=top_logprobs)
+        ptrs = (_p(logprobs), entropy.data_ptr(), stats.data_ptr(), _p(top_ids), _p(top_logprobs))
+    else:
+        ptrs = (_vector(out.get("logprobs"), R, torch.float32, "logprobs"),
+                _vector(out.get("entropy"), R, torch.float32, "entropy"),
+                _vector(out.get("stats"), 2 * R, torch.float32, "stats"),
+                _vector(out.get("top_ids"), R * n_top, torch.int32, "top_ids"),
+                _vector(out.get("top_logprobs"), R * n_top, torch.float32, "top_logprobs"))
     code = lib().umim_token_logprobs(
         x, dtype, R, V, ld, _vector(n_rows, 1, torch.int32, "n_rows"), _vector(token_ids, R, torch.int32, "token_ids"),
-        float(temperature), n_top, _vector(out.get("logprobs"), R, torch.float32, "logprobs"),
-        _vector(out.get("entropy"), R, torch.float32, "entropy"),
-        _vector(out.get("stats"), 2 * R, torch.float32, "stats"),
-        _vector(out.get("top_ids"), R * n_top, torch.int32, "top_ids"),
-        _vector(out.get("top_logprobs"), R * n_top, torch.float32, "top_logprobs"), _p(dev_status), _stream(stream))
+        float(temperature), n_top, *ptrs, _p(dev_status), _stream(stream))
     _check(code, "umim_token_logprobs")
     return out
 
@@ -621,16 +641,11 @@ def umim_token_logprobs_grad(logits, stats, token_ids=None, grad_logprobs=None, 
     stride; logits itself for a gradient in place) is returned; columns past
     vocab are not written."""
     x, dtype, R, V, ld = _logit_rows(logits, vocab)
-    if grad is None:
-        grad = torch.empty_strided((R, logits.shape[1]), (ld, 1), dtype=logits.dtype, device=logits.device)
-    g_ptr, g_dtype, g_R, _, g_ld = _logit_rows(grad, V, "grad")
-    if g_dtype != dtype or g_R != R or g_ld != ld:
-        raise ValueError("grad must have the logits' type, rows and row stride")
+    grad, g_ptr = _grad_rows(grad, logits, dtype, R, V, ld)
     code = lib().umim_token_logprobs_grad(
         x, dtype, R, V, ld, _vector(n_rows, 1, torch.int32, "n_rows"), _vector(token_ids, R, torch.int32, "token_ids"),
         float(temperature), _vector(stats, 2 * R, torch.float32, "stats"),
-        _vector(entropy, R, torch.float32, "entropy"),
-        _vector(grad_logprobs, R, torch.float32, "grad_logprobs"),
+        _vector(entropy, R, torch.float32, "entropy"), _vector(grad_logprobs, R, torch.float32, "grad_logprobs"),
         _vector(grad_entropy, R, torch.float32, "grad_entropy"), g_ptr, _p(dev_status), _stream(stream))
     _check(code, "umim_token_logprobs_grad")
     return grad
@@ -663,11 +678,7 @@ def umim_distill_topk_ce(top_ids, top_logprobs, student_logits, teacher_rows, st
         pair_loss = torch.empty(max(1, P), dtype=torch.float32, device=dev)
     g_ptr = None
     if with_grad:
-        if grad is None:
-            grad = torch.empty_strided((R_S, student_logits.shape[1]), (ld, 1), dtype=student_logits.dtype, device=dev)
-        g_ptr, g_dtype, g_R, _, g_ld = _logit_rows(grad, V, "grad")
-        if g_dtype != dtype or g_R != R_S or g_ld != ld:
-            raise ValueError("grad must have the student logits' type, rows and row stride")
+        grad, g_ptr = _grad_rows(grad, student_logits, dtype, R_S, V, ld)
     if workspace_buf is None:
         workspace_buf = workspace(umim_distill_topk_ce_workspace_size(R_S, P), dev)
     code = lib().umim_distill_topk_ce(
@@ -676,7 +687,8 @@ def umim_distill_topk_ce(top_ids, top_logprobs, student_logits, teacher_rows, st
         R_T, K, x, dtype, R_S, V, ld, _vector(teacher_rows, P, torch.int32, "teacher_rows"),
         _vector(student_rows, P, torch.int32, "student_rows"), P, _vector(n_pairs, 1, torch.int32, "n_pairs"),
         float(temperature), 1 if tail else 0, float(grad_scale), _vector(loss, 1, torch.float32, "loss"),
-        _p(pair_loss), g_ptr, workspace_buf.data_ptr(), workspace_buf.numel(), _p(dev_status), _stream(stream))
+        _vector(pair_loss, max(1, P), torch.float32, "pair_loss"), g_ptr, workspace_buf.data_ptr(),
+        workspace_buf.numel(), _p(dev_status), _stream(stream))
     _check(code, "umim_distill_topk_ce")
     return loss, pair_loss, (grad if with_grad else None)
 
