@@ -80,6 +80,10 @@ struct ElemBf16 {
     return d;
   }
   static __device__ __forceinline__ T word_max_bits(uint32_t w) { return (T)max_words(w, w >> 16); }
+  // all ones in the place of each element of x that is >= y's, else zeros
+  static __device__ __forceinline__ uint32_t reach_words(uint32_t x, uint32_t y) {
+    return __hge2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
+  }
   // -1e30: beside a maximum of any size that fp32 exponents of differences are taken of
   static constexpr bool kHasFinite = true;
   static __device__ __forceinline__ uint32_t finite_words(uint32_t x) {
@@ -114,6 +118,9 @@ struct ElemFp16 {
     return d;
   }
   static __device__ __forceinline__ T word_max_bits(uint32_t w) { return (T)max_words(w, w >> 16); }
+  static __device__ __forceinline__ uint32_t reach_words(uint32_t x, uint32_t y) {
+    return __hge2_mask(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&y));
+  }
   // no finite half is far enough below the others
   static constexpr bool kHasFinite = false;
   static __device__ __forceinline__ uint32_t order_key(T b) { return order_key16(b); }

@@ -252,6 +252,34 @@ __device__ __forceinline__ typename E::T element(const uint4 &u, int j) {
     return __uint_as_float(w[j]);
 }
 
+// the same where j is not known to the compiler
+template <class E>
+__device__ __forceinline__ typename E::T element_at(const uint4 &u, int j) {
+  const int i = E::VEC == 8 ? j / 2 : j;
+  const uint32_t w = i & 2 ? (i & 1 ? u.w : u.z) : (i & 1 ? u.y : u.x);
+  if constexpr (E::VEC == 8)
+    return (typename E::T)(w >> (16 * (j & 1)));
+  else
+    return __uint_as_float(w);
+}
+
+// bit j: element j is no smaller than the one of key `least` (none is NaN)
+template <class E>
+__device__ __forceinline__ uint32_t reach_mask(const uint4 &u, uint32_t least) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  uint32_t mask = 0;
+  if constexpr (E::VEC == 8) {
+    const uint32_t bits = E::from_key(least), both = bits | bits << 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mask |= (E::reach_words(w[i], both) & 0x00020001u) << (2 * i);
+    return (mask | mask >> 16) & 0xffu;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mask |= (__uint_as_float(w[i]) >= E::from_key(least) ? 1u : 0u) << i;
+    return mask;
+  }
+}
+
 // the warp's values in descending order (a bitonic sort)
 __device__ __forceinline__ uint64_t warp_sorted(uint64_t v) {
   const int lane = threadIdx.x & 31;
@@ -338,7 +366,7 @@ __device__ int gather_best(const typename E::T *seg, const typename E::T *row, i
 
   using T = typename E::T;
   const float least_x = E::to_float(E::from_key(least));   // a bound in passing: x >= it as its key >= least
-  // the segments that `in` takes, to list[]; returns how many
+  // the segments that reach `least` and that `in` takes, to list[]; returns how many
   const auto list_segments = [&](auto in) {
     if (tid == 0) s_listed = 0;
     __syncthreads();
@@ -346,12 +374,13 @@ __device__ int gather_best(const typename E::T *seg, const typename E::T *row, i
       const uint4 u = *reinterpret_cast<const uint4 *>(seg + i);
       const uint32_t top = E::max_words(E::max_words(u.x, u.y), E::max_words(u.z, u.w));
       if (E::to_float(E::word_max_bits(top)) >= least_x)
-#pragma unroll
-        for (int j = 0; j < E::VEC; ++j)
-          if (in(element<E>(u, j), (uint32_t)(i + j))) {
+        for (uint32_t hits = reach_mask<E>(u, least); hits; hits &= hits - 1) {
+          const int j = __ffs(hits) - 1;
+          if (in(element_at<E>(u, j), (uint32_t)(i + j))) {
             const int at = atomicAdd(&s_listed, 1);
             if (at < kListed) list[at] = (uint16_t)(i + j);
           }
+        }
     }
     __syncthreads();
     return s_listed;
@@ -365,17 +394,17 @@ __device__ int gather_best(const typename E::T *seg, const typename E::T *row, i
     e = beg + s * kSegment + (i % kVecs) * E::VEC;
     return load_raw<E>(row, e, end);
   };
-  // The elements of listed segments that `in` takes, to cand[]; returns how many.  Two vectors a
-  // thread on their way at once.
+  // The elements of listed segments that reach `least` and that `in` takes, to cand[]; returns how
+  // many.  Two vectors a thread on their way at once.
   const auto gather = [&](int listed, auto in) {
     if (tid == 0) s_held = 0;
     __syncthreads();
     const auto take = [&](const uint4 &u, int e) {
       const uint32_t top = E::max_words(E::max_words(u.x, u.y), E::max_words(u.z, u.w));
       if (E::to_float(E::word_max_bits(top)) >= least_x)
-#pragma unroll
-        for (int j = 0; j < E::VEC; ++j) {
-          const T x = element<E>(u, j);
+        for (uint32_t hits = reach_mask<E>(u, least); hits; hits &= hits - 1) {
+          const int j = __ffs(hits) - 1;
+          const T x = element_at<E>(u, j);
           if (in(x, (uint32_t)(e + j))) {
             const int at = atomicAdd(&s_held, 1);
             if (at < kCands) cand[at] = entry(E::order_key(x), (uint32_t)(e + j));
@@ -394,7 +423,7 @@ __device__ int gather_best(const typename E::T *seg, const typename E::T *row, i
     __syncthreads();
     return s_held;
   };
-  const auto reaches = [&](T x, uint32_t) { return E::to_float(x) >= least_x; };
+  const auto reaches = [](T, uint32_t) { return true; };
   const int listed = list_segments(reaches);
   if (listed <= kListed) {
     const int held = gather(listed, reaches);
