@@ -72,7 +72,7 @@ umim_status token_logprobs(const void *, int, int, int, int64_t, const int32_t *
                            float *, float *, int32_t *, float *, int32_t *, cudaStream_t, int);
 umim_status token_logprobs_grad(const void *, int, int, int, int64_t, const int32_t *, const int32_t *, float,
                                 const float *, const float *, const float *, const float *, void *, int32_t *,
-                                cudaStream_t);
+                                cudaStream_t, int);
 size_t distill_topk_ce_workspace_bytes(int R_S, int max_pairs);
 umim_status distill_topk_ce(const int32_t *, const float *, int, int, const void *, int, int, int, int64_t,
                             const int32_t *, const int32_t *, int, const int32_t *, float, int, float, float *, float *,
@@ -462,7 +462,7 @@ umim_status umim_token_logprobs_grad(const void *logits, int32_t dtype, int32_t 
   if (!stats || !aligned(stats, 8) || !grad || !aligned(grad, 16)) return UMIM_ERR_INVALID_ARG;
   const DeviceScope scope(stream);
   return token_logprobs_grad(logits, dtype, n_rows, vocab, ld, n_dev, token_ids, temperature, stats, entropy,
-                             grad_logprobs, grad_entropy, grad, dev_status, stream);
+                             grad_logprobs, grad_entropy, grad, dev_status, stream, scope.sms());
 }
 
 size_t umim_distill_topk_ce_workspace_size(int32_t n_student_rows, int32_t max_pairs) {

@@ -43,7 +43,7 @@ struct GradArgs {
   const int32_t *n_dev;
   const int32_t *tokens;
   float inv_t, c;            // 1 / T, log2(e) / T
-  int32_t parts;             // CTAs per row
+  int32_t parts, chunks;     // CTAs per row, chunks of a CTA
   const float2 *stats;
   const float *entropy, *g, *h;
   void *grad;
@@ -723,12 +723,10 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
 // gradient
 // ---------------------------------------------------------------------------
 // Elementwise, bound by its one read and one write of every element.  A CTA takes
-// kGradChunks chunks of a row: 4 vectors a thread, loaded together and ahead of the
+// some chunks of a row: 4 vectors a thread each, loaded together and ahead of the
 // row's numbers.  With t = log2 p the element is p (A + B t), A = -(g + h H) / T and
 // B = -h ln 2 / T; the token's own is -g expm1(ln p) / T + p (A + g / T + B t), exact
 // where p is so near 1 that 1 - p would be nothing.
-constexpr int kGradChunks = 2;
-
 template <class E>
 __global__ void __launch_bounds__(kThreads, 4) token_logprobs_grad_kernel(GradArgs a) {
   griddep_wait();
@@ -738,8 +736,8 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_grad_kernel(GradAr
   const typename E::T *row = static_cast<const typename E::T *>(a.logits) + (int64_t)r * a.ld;
   typename E::T *out = static_cast<typename E::T *>(a.grad) + (int64_t)r * a.ld;
   constexpr int kStep = kThreads * E::VEC, kChunk = kUnroll * kStep;
-  int e0 = (blockIdx.x % a.parts) * (kGradChunks * kChunk) + threadIdx.x * E::VEC;
-  const int last = min(V, (int)(blockIdx.x % a.parts + 1) * (kGradChunks * kChunk));
+  const int part = blockIdx.x % a.parts * a.chunks * kChunk, last = min(V, part + a.chunks * kChunk);
+  int e0 = part + threadIdx.x * E::VEC;
 
   const int token = a.tokens ? row_token(a.tokens, r, V, a.status, threadIdx.x == 0) : 0;
   const float2 st = a.stats[r];
@@ -838,12 +836,17 @@ umim_status token_logprobs(const void *logits, int dtype, int R, int V, int64_t 
                                     : launch_logprobs<ElemFp32, false>(a, C, stream);
 }
 
+constexpr int kGradChunks = 4, kGradCtas = 16;
+
 umim_status token_logprobs_grad(const void *logits, int dtype, int R, int V, int64_t ld, const int32_t *n_dev,
                                 const int32_t *tokens, float temperature, const float *stats, const float *entropy,
-                                const float *g, const float *h, void *grad, int32_t *dev_status, cudaStream_t stream) {
+                                const float *g, const float *h, void *grad, int32_t *dev_status, cudaStream_t stream,
+                                int num_sms) {
   const int vec = 16 / (int)dtype_bytes(dtype);
-  const int parts = ceil_div(V, kGradChunks * kUnroll * kThreads * vec);
-  const GradArgs a{logits, R, V, ld, n_dev, tokens, 1.f / temperature, kLog2e / temperature, parts,
+  const int row_chunks = ceil_div(V, kUnroll * kThreads * vec);
+  const int chunks = (int)std::clamp<int64_t>((int64_t)R * row_chunks / (kGradCtas * num_sms), 1, kGradChunks);
+  const int parts = ceil_div(row_chunks, chunks);
+  const GradArgs a{logits, R, V, ld, n_dev, tokens, 1.f / temperature, kLog2e / temperature, parts, chunks,
                    reinterpret_cast<const float2 *>(stats), entropy, g, h, grad, dev_status};
   auto *k = dtype == UMIM_DTYPE_BF16   ? token_logprobs_grad_kernel<ElemBf16>
             : dtype == UMIM_DTYPE_FP16 ? token_logprobs_grad_kernel<ElemFp16>
