@@ -520,7 +520,10 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
   // ---- the loss: the last cluster sums the per-pair losses in pair order ----
   if (rank != 0) return;
   __syncthreads();
-  if (tid == 0) s_last = arrive_is_last(&a.hdr->clusters_done, clusters);
+  if (tid == 0) {
+    s_last = 0;
+    if (arrive_is_last(&a.hdr->clusters_done, clusters)) s_last = 1;
+  }
   __syncthreads();
   if (!s_last) return;
   __shared__ double dsum[kWarps];

@@ -201,9 +201,11 @@ struct Running {
 // holds an element each have an element before it.  So bisections, by value and
 // then by place, pick exactly n segments, and of their elements exactly n.
 //
-// The search keeps its shared memory small (13 KB at 128256 bf16): what it takes
-// the L1 cache lacks, through which the loads in flight pass.  With 25 and 48
-// KB a CTA the pass alone took 175 and 189 us for 4096 such rows, against 156.
+// What bounds it: without alternatives the one read of the logits (4096 rows of 128256
+// bf16: 153 us, 6.9 TB/s, as the measured copy's rate or above); with them
+// the instructions as well, 6.6 a logit for the pass and 1.6 (one alternative) to 3 (128)
+// for segments and search: 167 / 171 / 185 / 199 us with 1 / 20 / 64 / 128 of them.
+// Occupancy is not it: three CTAs of 72 registers an SM took as long as four of 64.
 //
 // All of it happens in shared memory and registers of the cluster: no
 // workspace, no atomics on global memory, the same bits in every call.
@@ -292,21 +294,6 @@ __device__ __forceinline__ uint64_t warp_sorted(uint64_t v) {
       v = (v > o) == larger ? v : o;
     }
   return v;
-}
-
-// The place, among all that the CTA's threads take, of the first of the `count` that this
-// thread takes; *total (shared, 0 before) counts them.  One atomic per warp.
-__device__ __forceinline__ int take_places(int count, int *total) {
-  const int lane = threadIdx.x & 31;
-  int sum = count;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int below = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += below;
-  }
-  int base = 0;
-  if (lane == 31 && sum > 0) base = atomicAdd(total, sum);
-  return __shfl_sync(0xffffffffu, base, 31) + sum - count;
 }
 
 // The n first of the CTA's entries by (key descending, id ascending), of which there are
@@ -469,18 +456,18 @@ __device__ void keep_best(const uint64_t *from, int M, int n, uint32_t lo, uint3
   });
   constexpr int kHold = kMaxCluster * kMaxTop / kThreads;   // entries of a thread, at most
   uint64_t held[kHold];
-  int count = 0;
 #pragma unroll
   for (int k = 0; k < kHold; ++k) {
     const int i = threadIdx.x + k * kThreads;
     held[k] = i < M && cut.in(key_of(from[i]), id_of(from[i])) ? from[i] : 0;
-    count += held[k] != 0;
   }
   __syncthreads();   // all of from has been read
-  int at = take_places(count, &s_kept);
 #pragma unroll
   for (int k = 0; k < kHold; ++k)
-    if (held[k] != 0) cand[at++] = held[k];
+    if (held[k] != 0) {
+      const int at = atomicAdd(&s_kept, 1);
+      cand[at] = held[k];
+    }
   __syncthreads();
 }
 
@@ -653,22 +640,21 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
                        : "memory");
         cluster_sync_all();
         if (rank != 0) return;
-        // side by side: list k moves down to the end of list k - 1
-        M = s_count[0];
-        for (int k = 1; k < C; ++k) {
+        M = 0;
+        for (int k = 0; k < C; ++k) M += s_count[k];
+        const bool fit = M <= kCands;
+        uint64_t *side_by_side = fit ? s_cand : sh.merge;   // in merge list k moves down to the end of list k - 1
+        for (int k = 0, at = 0; k < C; ++k) {
           const int count = s_count[k];
           const uint64_t e = tid < count ? sh.merge[k * cap + tid] : 0;
-          __syncthreads();
-          if (tid < count) sh.merge[M + tid] = e;
-          M += count;
+          if (!fit) __syncthreads();
+          if (tid < count) side_by_side[at + tid] = e;
+          at += count;
         }
         __syncthreads();
-        if (M > kCands) {
+        if (!fit) {
           keep_best(sh.merge, M, n, least, hi, V, s_cand);
           M = n;
-        } else {
-          if (tid < M) s_cand[tid] = sh.merge[tid];
-          __syncthreads();
         }
       }
     }

@@ -95,6 +95,8 @@ def check(out, ids, lp, x, V, tr, sr, T, tail, dtype, scale=1.0):
     if grad is not None:
         wgrad = wgrad * scale
         tiny = 2.0 ** -25 if dtype == "fp16" else 1e-37
+        # an exponential below 2^-126 comes out as 0; what it is multiplied by is at most P + p_rest <= 2 over N T
+        tiny += 2.0 ** -126 * 2 * abs(scale) / (max(N, 1) * T)
         within(f64(grad)[:, :V], wgrad, gtol + (eps + 4 * U) * np.abs(np.nan_to_num(wgrad)) + tiny, "gradient")
 
 
@@ -417,3 +419,51 @@ def test_binding_refusals():
         with pytest.raises(m.UmimError) as e:
             f()
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("tail", [True, False])
+@pytest.mark.parametrize("T", [1.0, 0.01, 0.001])
+@pytest.mark.parametrize("offset", [3e4, -1e5])
+def test_logits_far_from_zero(offset, T, tail):
+    """x c and m c are large beside their difference: its exactness is x - m's."""
+    m, dv = umim(), dev()
+    V, K, R = 3001, 20, 5
+    ids, lp = lists(15, R, K, V)
+    tr = sr = np.arange(R)
+    x = logits(15, R, V, "fp32")
+    x[:, :V] += offset
+    check(run(m, dv, ids, lp, x, V, tr, sr, T, tail), ids, lp, x, V, tr, sr, T, tail, "fp32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V,R,N", [(12000, 600, 513), (70000, 400, 399), (300, 2000, 1999)])
+def test_more_pairs_than_clusters(dtype, V, R, N):
+    """Clusters take pair after pair: every row of the gradient against plain torch in float64."""
+    m, dv = umim(), dev()
+    K, T = 30, 1.2
+    r = np.random.default_rng(V)
+    ids, lp = lists(16, 50, K, V, holes=False)
+    tr, sr = r.integers(0, 50, N), r.permutation(R)[:N]
+    x = logits(16, R, V, dtype)
+    loss, pairs, grad = run(m, dv, ids, lp, x, V, tr, sr, T, True)
+    s, t = torch.from_numpy(sr).to(dv), torch.from_numpy(tr).to(dv)
+    logq = torch.log_softmax(x.to(dv)[s, :V].double() / T, 1)
+    at = torch.from_numpy(ids).to(dv).long()[t]
+    p = torch.from_numpy(lp).to(dv).double()[t].exp()
+    rest = 1 - p.sum(1)
+    q_rest = logq.exp().scatter(1, at, 0.0).sum(1)
+    want = -(p * logq.gather(1, at)).sum(1) - rest * q_rest.log()
+    # every |ln q| here is below 40, p sums to 1
+    tol = 2 * tol_l(V) + U * (8 + K + 8) * 40
+    within(f64(pairs), want.cpu().numpy(), tol, "pair losses")
+    within(f64(loss), [want.mean().item()], tol, "loss")
+    d = logq.exp() * (1 - rest / q_rest)[:, None]
+    d.scatter_(1, at, logq.exp().gather(1, at) * 1.0 - p)
+    wgrad = torch.zeros((R, V), dtype=torch.float64, device=dv)
+    wgrad[s] = d / (N * T)
+    size = torch.zeros((R, V), dtype=torch.float64, device=dv)
+    size[s] = logq.exp() * (1 + rest / q_rest)[:, None] + torch.zeros_like(logq).scatter(1, at, p)
+    eps = torch.finfo(TYPES[dtype]).eps / 2
+    factor = 4 * (tol_l(V) + 8 * U * 64 + U * (K + 8)) / (N * T)
+    off = (grad[:, :V].double() - wgrad).abs() - (eps + 4 * U) * wgrad.abs() - factor * size
+    assert bool((off <= 1e-37).all())

@@ -97,6 +97,9 @@ def check_grad(got, x, V, tokens, g, h, T, dtype):
         size = size + np.abs(hd)[:, None] * p * (np.abs(z) + H + 2)
     eps = torch.finfo(TYPES[dtype]).eps / 2
     tiny = 2.0 ** -25 if dtype == "fp16" else 1e-37
+    # a p below 2^-126 comes out as 0, where |ln p| is below 90 if it counts at all in fp32
+    tiny = tiny + 2.0 ** -126 * (np.zeros((len(xd), 1)) + (0 if g is None else np.abs(gd)[:, None])
+                                 + (0 if h is None else np.abs(hd)[:, None] * (90 + H))) / T
     tol = 2 * dp * size / T + (eps + 4 * U) * np.abs(np.nan_to_num(want)) + tiny
     if h is not None:   # the entropy's own error
         tol = tol + np.abs(hd)[:, None] * p * U * (V / 256 + 300) * (1 + H) / T
@@ -448,3 +451,56 @@ def test_binding_refusals():
         assert e.value.code == code
     out = m.umim_token_logprobs(x[:0], tok[:0], n_top=3)     # no rows: nothing to do
     assert out["top_ids"].shape == (0, 3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("n_top", [3, 20, 128])
+def test_ties_in_many_rows(dtype, n_top):
+    """A CTA to each row: equal values by the hundred, and rows masked with the lowest value."""
+    m, dv = umim(), dev()
+    V, R = 5003, 700
+    x = logits(21, R, V, dtype, std=1.5, levels=1)
+    r = np.random.default_rng(5)
+    low = torch.finfo(TYPES[dtype]).min
+    for row in range(0, R, 7):
+        keep = torch.from_numpy(r.choice(V, 9, replace=False))
+        held = x[row, keep].clone()
+        x[row, :V] = low if row % 2 else -math.inf
+        x[row, keep] = held
+    out = forward(m, x, dv, V, None, 1.0, n_top)
+    ids = x[:, :V].float().sort(dim=1, descending=True, stable=True)[1][:, :n_top]
+    gone = torch.gather(x[:, :V].float(), 1, ids) == -math.inf
+    assert torch.equal(out["top_ids"].cpu().long(), ids.masked_fill(gone, -1))
+    pick = [0, 7, 8, 350, R - 1]
+    check_forward({k: (v[pick] if v is not None else None) for k, v in out.items()}, x[pick], V, None, 1.0, n_top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_one_value_everywhere_in_the_largest_vocabulary(dtype):
+    m, dv = umim(), dev()
+    V, R, n = 262144, 320, 128
+    x = torch.full((R, V), -1.25, dtype=TYPES[dtype], device=dv)
+    x[1::2] = torch.finfo(TYPES[dtype]).min
+    out = m.umim_token_logprobs(x, n_top=n)
+    torch.cuda.synchronize()
+    assert torch.equal(out["top_ids"].cpu(), torch.arange(n, dtype=torch.int32).expand(R, n))
+    # V equal terms: the sums of 256 threads are powers of two, so only ln rounds
+    within(f64(out["entropy"]), np.full(R, math.log(V)), 16 * U * math.log(V), "entropy")
+
+
+@pytest.mark.parametrize("T", [1.0, 0.01, 0.001])
+@pytest.mark.parametrize("offset", [3e4, -1e5])
+def test_logits_far_from_zero(T, offset):
+    """x c and m c are large beside their difference: its exactness is x - m's."""
+    m, dv = umim(), dev()
+    V, R = 3001, 4
+    x = logits(22, R, V, "fp32")
+    x[:, :V] += offset
+    tokens = np.array([0, 5, 2000, 3000])
+    out = forward(m, x, dv, V, tokens, T, 8)
+    check_forward(out, x, V, tokens, T, 8)
+    g, h = torch.linspace(-1, 1, R), torch.linspace(1, 2, R)
+    tok = torch.from_numpy(tokens.astype(np.int32)).to(dv)
+    grad = m.umim_token_logprobs_grad(x.to(dv), out["stats"], tok, g.to(dv), out["entropy"], h.to(dv), vocab=V,
+                                      temperature=T)
+    check_grad(grad, x, V, tokens, g, h, T, "fp32")
