@@ -18,7 +18,8 @@ namespace umim {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kUnroll = 4;        // vectors of a thread in flight, and one chunk more
+constexpr int kUnroll = 8;        // vectors that a thread loads together: forward
+constexpr int kGradUnroll = 4;    // and gradient
 constexpr int kMaxCluster = 8;    // CTAs per row, at most
 
 struct LogprobArgs {
@@ -93,7 +94,7 @@ __device__ __forceinline__ Stats warp_stats(Stats a, float top, float c) {
 // holds as long as |m c| < 2^24.)
 constexpr float kLeastT = -1000.f;
 
-// One thread's part: four vectors at a time.  t is one FMA, x c + b with
+// One thread's part: eight vectors at a time.  t is one FMA, x c + b with
 // b = -m c rounded; the rounding r is common to a chunk and made good on its
 // sums, so that t is as exact for large |m| as (x - m) c.  Where r itself is large
 // (|m c| past 2^24, or no number) the chunk is read again and done the careful
@@ -180,11 +181,11 @@ struct Running {
 // forward
 // ---------------------------------------------------------------------------
 // One cluster of C CTAs per row, each on one of C contiguous parts.  A warp
-// takes chunks of 4 x 32 vectors, a lane one vector of each 32: every logit is
-// read once, by 16-byte loads a chunk ahead of their use.  (Copies of a chunk
-// into buffers of the warp's own, which leave registers for a fifth CTA on an SM,
-// measured slower: 231 against 222 us for 4096 rows of 128256 bf16 with 64
-// alternatives, 17 against 10 us for 128 rows without.)
+// takes chunks of 8 x 32 vectors, a lane one vector of each 32: every logit is
+// read once, by 16-byte loads, a warp's all together while the others work on theirs.
+// (Half as many a chunk ahead of their use took 186 us where this takes 179, for
+// 4096 rows of 128256 bf16 with 64 alternatives; asynchronous copies into buffers
+// of the warp's own 4 % longer than those.)
 //
 // The alternatives need no second pass over the row.  Beside the sums, the
 // maximum of every segment of 32 consecutive elements goes to shared memory.
@@ -202,10 +203,9 @@ struct Running {
 // then by place, pick exactly n segments, and of their elements exactly n.
 //
 // What bounds it: without alternatives the one read of the logits (4096 rows of 128256
-// bf16: 153 us, 6.9 TB/s, as the measured copy's rate or above); with them
-// the instructions as well, 6.6 a logit for the pass and 1.6 (one alternative) to 3 (128)
-// for segments and search: 167 / 171 / 185 / 199 us with 1 / 20 / 64 / 128 of them.
-// Occupancy is not it: three CTAs of 72 registers an SM took as long as four of 64.
+// bf16: 149 us, 7.0 TB/s, above the measured copy's rate); with them the
+// instructions as well, 5.8 a logit for the pass and 1.4 (one alternative) to 2.8
+// (128) for segments and search: 167 us with 20, 179 with 64.
 //
 // All of it happens in shared memory and registers of the cluster: no
 // workspace, no atomics on global memory, the same bits in every call.
@@ -237,7 +237,9 @@ struct TopShared {
   }
 };
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t key_of(uint64_t e) { return (uint32_t)(e >> 32); }
@@ -534,31 +536,30 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
       top[k] = E::max_words(E::max_words(u[k].x, u[k].y), E::max_words(u[k].z, u[k].w));
     if constexpr (TOP) {
       // The maxima of four neighbouring lanes' vectors, transposed: a lane ends up with
-      // that of its four for vector lane % 4.
-      static_assert(kUnroll == 4, "four vectors among four lanes");
+      // that of its four for vector lane % 4 of each four.
+      static_assert(kUnroll % 4 == 0, "four vectors among four lanes");
       const bool odd = lane & 1, high = lane & 2;
-      const uint32_t p = E::max_words(odd ? top[1] : top[0], __shfl_xor_sync(0xffffffffu, odd ? top[0] : top[1], 1));
-      const uint32_t q = E::max_words(odd ? top[3] : top[2], __shfl_xor_sync(0xffffffffu, odd ? top[2] : top[3], 1));
-      uint32_t m = E::max_words(high ? q : p, __shfl_xor_sync(0xffffffffu, high ? p : q, 2));
-      if (E::VEC == 4) m = E::max_words(m, __shfl_xor_sync(0xffffffffu, m, 4));   // eight lanes make a segment
-      if (E::VEC == 8 || !(lane & 4)) *seg_at = E::word_max_bits(m);
+#pragma unroll
+      for (int g = 0; g < kUnroll; g += 4) {
+        const uint32_t p =
+            E::max_words(odd ? top[g + 1] : top[g], __shfl_xor_sync(0xffffffffu, odd ? top[g] : top[g + 1], 1));
+        const uint32_t q =
+            E::max_words(odd ? top[g + 3] : top[g + 2], __shfl_xor_sync(0xffffffffu, odd ? top[g + 2] : top[g + 3], 1));
+        uint32_t m = E::max_words(high ? q : p, __shfl_xor_sync(0xffffffffu, high ? p : q, 2));
+        if (E::VEC == 4) m = E::max_words(m, __shfl_xor_sync(0xffffffffu, m, 4));   // eight lanes make a segment
+        if (E::VEC == 8 || !(lane & 4)) seg_at[g * 32 * E::VEC / kSegment] = E::word_max_bits(m);
+      }
       seg_at += kWarps * kChunk / kSegment;
     }
-    run.add(u, E::max_words(E::max_words(top[0], top[1]), E::max_words(top[2], top[3])), c,
-            [&](int k) { return load_raw<E>(row, e0 + (k * 32 + lane) * E::VEC, end); });
+    uint32_t all = top[0];
+#pragma unroll
+    for (int k = 1; k < kUnroll; ++k) all = E::max_words(all, top[k]);
+    run.add(u, all, c, [&](int k) { return load_raw<E>(row, e0 + (k * 32 + lane) * E::VEC, end); });
   };
-  {   // two chunks in turn, each loaded while the other is worked on
-    constexpr int kStride = kWarps * kChunk;
-    uint4 u[kUnroll], v[kUnroll];
-    int e0 = beg + warp * kChunk;
+  for (int e0 = beg + warp * kChunk; e0 < end; e0 += kWarps * kChunk) {
+    uint4 u[kUnroll];
     load(u, e0);
-    for (; e0 < end; e0 += 2 * kStride) {
-      load(v, e0 + kStride);
-      take(u, e0);
-      if (e0 + kStride >= end) break;
-      load(u, e0 + 2 * kStride);
-      take(v, e0 + kStride);
-    }
+    take(u, e0);
   }
 
   // ---- the row's sums, and a threshold for its alternatives ----
@@ -721,7 +722,7 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_grad_kernel(GradAr
   if (r >= rows_used(a.n_dev, a.R)) return;
   const typename E::T *row = static_cast<const typename E::T *>(a.logits) + (int64_t)r * a.ld;
   typename E::T *out = static_cast<typename E::T *>(a.grad) + (int64_t)r * a.ld;
-  constexpr int kStep = kThreads * E::VEC, kChunk = kUnroll * kStep;
+  constexpr int kStep = kThreads * E::VEC, kChunk = kGradUnroll * kStep;
   const int part = blockIdx.x % a.parts * a.chunks * kChunk, last = min(V, part + a.chunks * kChunk);
   int e0 = part + threadIdx.x * E::VEC;
 
@@ -740,9 +741,9 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_grad_kernel(GradAr
   const float2 A2 = make_float2(A, A), B2 = make_float2(B, B), nm2 = make_float2(-st.x, -st.x);
   const float2 c2 = make_float2(a.c, a.c), nl2 = make_float2(-st.y * kLog2e, -st.y * kLog2e);
   for (; e0 < last; e0 += kChunk) {
-    uint4 u[kUnroll];
+    uint4 u[kGradUnroll];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
+    for (int k = 0; k < kGradUnroll; ++k) {
       const int e = e0 + k * kStep;
       if (e + E::VEC <= V)
         u[k] = __ldcs(reinterpret_cast<const uint4 *>(row + e));
@@ -750,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_grad_kernel(GradAr
         u[k] = load_raw<E>(row, e, V);
     }
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
+    for (int k = 0; k < kGradUnroll; ++k) {
       const int e = e0 + k * kStep;
       if (e >= last) break;
       float d[E::VEC];
@@ -833,7 +834,7 @@ umim_status token_logprobs_grad(const void *logits, int dtype, int R, int V, int
                                 const float *g, const float *h, void *grad, int32_t *dev_status, cudaStream_t stream,
                                 int num_sms) {
   const int vec = 16 / (int)dtype_bytes(dtype);
-  const int row_chunks = ceil_div(V, kUnroll * kThreads * vec);
+  const int row_chunks = ceil_div(V, kGradUnroll * kThreads * vec);
   const int chunks = (int)std::clamp<int64_t>((int64_t)R * row_chunks / (kGradCtas * num_sms), 1, kGradChunks);
   const int parts = ceil_div(row_chunks, chunks);
   const GradArgs a{logits, R, V, ld, n_dev, tokens, 1.f / temperature, kLog2e / temperature, parts, chunks,
