@@ -581,6 +581,10 @@ int resident_clusters(int C, size_t bytes, int num_sms) {
   std::lock_guard<std::mutex> lock(mu);
   for (int i = 0; i < n_known; ++i)
     if (known[i].dev == dev && known[i].C == C && known[i].bytes == bytes) return known[i].n;
+  // before the first launch of any configuration here; the largest size, so that none finds a smaller limit
+  if (!allow_smem(topk_ce_kernel<E>, std::max(part_bytes(kMaxLogitVocab, kMaxCluster, (int)sizeof(typename E::T)),
+                                              (size_t)kPartBytes)))
+    return 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(C * std::max(1, num_sms / C)));
   cfg.blockDim = dim3(kThreads);
@@ -597,7 +601,7 @@ int resident_clusters(int C, size_t bytes, int num_sms) {
     cudaGetLastError();
     n = 0;
   }
-  if (n_known < 64) known[n_known++] = Known{dev, C, n, bytes};
+  if (n > 0 && n_known < 64) known[n_known++] = Known{dev, C, n, bytes};
   return n;
 }
 
@@ -607,10 +611,8 @@ umim_status launch_topk_ce(TopkArgs a, cudaStream_t stream, int num_sms) {
   const int C = cluster_for(std::max(a.R_S, 1), a.V, esize, num_sms);
   const size_t bytes = part_bytes(a.V, C, esize);
   a.slice = slice_of(a.V, C);
-  if (!allow_smem(topk_ce_kernel<E>, std::max(part_bytes(kMaxLogitVocab, kMaxCluster, esize), (size_t)kPartBytes)))
-    return UMIM_ERR_CUDA;
   const int resident = resident_clusters<E>(C, bytes, num_sms);
-  if (resident < 1) return UMIM_ERR_UNSUPPORTED;
+  if (resident < 1) return UMIM_ERR_CUDA;
   const int clusters = std::min(std::max(a.R_S, 1), resident);
   trace_mark(stream, "distill.topk_ce");
   cudaLaunchConfig_t cfg = {};

@@ -797,9 +797,9 @@ namespace {
 
 template <class E, bool TOP>
 umim_status launch_logprobs(LogprobArgs a, int C, cudaStream_t stream) {
+  // a whole row's segments and the largest merge: with the kernel's own 6 KB below the 48 KB that need no leave
+  static_assert(sizeof(float) * (kMaxLogitVocab / kSegment) + 8 * kMaxCluster * kMaxTop <= 42 * 1024, "shared memory");
   const size_t smem = TOP ? TopShared<E>::bytes(a.slice, a.n_top, C) : 0;
-  if (TOP && !allow_smem(token_logprobs_kernel<E, TOP>, TopShared<E>::bytes(kMaxLogitVocab, kMaxTop, kMaxCluster)))
-    return UMIM_ERR_CUDA;
   trace_mark(stream, "logprobs.rows");
   const cudaError_t e = launch_pdl_cluster(token_logprobs_kernel<E, TOP>, dim3((unsigned)a.R * (unsigned)C),
                                            dim3(kThreads), (unsigned)C, smem, stream, a);
