@@ -709,7 +709,8 @@ umim_status umim_token_logprobs_grad(const void *logits, int32_t dtype, int32_t 
  *               only); elements [0, vocab) of every row written; must not
  *               overlap the logits
  * workspace     device, umim_distill_topk_ce_workspace_size() bytes, 256-B
- *               aligned (no initial contents required)
+ *               aligned (no initial contents required); calls sharing one must
+ *               not overlap on the GPU
  * A student row of -inf only has a pair loss of +inf (0 where nothing is
  * asked of it) and a zero gradient; NaN or +inf in it make both NaN.
  * Device-side errors: UMIM_ERR_INVALID_ARG, and nothing written, for N outside

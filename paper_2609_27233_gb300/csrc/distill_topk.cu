@@ -232,7 +232,7 @@ struct __align__(16) Part {
 // their place), so that it sums the rest alone, and their gradients are written
 // after the second pass, over the zeros that it left there.
 //
-// Rows in no pair get their zeros at the end.
+// Rows in no pair get their zeros in between.
 template <class E>
 __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
   extern __shared__ __align__(128) uint8_t dyn[];   // the part
@@ -302,7 +302,16 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
     }
   };
 
+  // Student rows in no pair: a look at one of this cluster's after each pair, the others at the end.
+  int other = a.grad ? cid : a.R_S;
+  const auto is_other = [&](uint32_t word) { return other < a.R_S && !(word >> (other & 31) & 1); };
+  const auto write_zeros = [&]() {
+    const float z[E::VEC] = {};
+    T *out = static_cast<T *>(a.grad) + (int64_t)other * a.ld;
+    for (int i = lane; i < vecs; i += 32) store_vec<E>(out, beg + i * E::VEC, V, z);
+  };
   for (int count = 0; pr < N; pr += clusters, ++count) {
+    const uint32_t word = other < a.R_S ? a.paired[other >> 5] : 0;
     const int next = pr + clusters;
     const int next_row = next < N ? a.student_rows[next] : 0;
     const float whole = head.x, rest = head.y;   // P, p_rest
@@ -509,16 +518,12 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
       copy(s_row);
       load_list(next);
     }
+    if (is_other(word)) write_zeros();
+    if (other < a.R_S) other += clusters;
   }
+  for (; other < a.R_S; other += clusters)
+    if (is_other(a.paired[other >> 5])) write_zeros();
 
-  if (a.grad) {   // student rows in no pair
-    const float z[E::VEC] = {};
-    for (int r = cid; r < a.R_S; r += clusters)
-      if (!(a.paired[r >> 5] >> (r & 31) & 1)) {
-        T *out = static_cast<T *>(a.grad) + (int64_t)r * a.ld;
-        for (int i = lane; i < vecs; i += 32) store_vec<E>(out, beg + i * E::VEC, V, z);
-      }
-  }
   if (C > 1) cluster_sync_all();   // no CTA leaves while one may still tell it anything
   // ---- the loss: the last cluster sums the per-pair losses in pair order ----
   if (rank != 0) return;
