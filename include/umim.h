@@ -630,7 +630,8 @@ umim_status umim_distill_soft_ce(const void *teacher_logits, int32_t n_teacher_r
  * entropy and stats are 0, its alternatives -1 and -inf.  A row of -inf only
  * has logprob -inf, entropy 0 and stats (-inf, 0); a row that holds NaN or
  * +inf has NaN everywhere and no alternatives (ids -1, log probabilities NaN).
- * logits        device [n_rows][ld] of `dtype` (umim_dtype), 16-B aligned
+ * logits        device [n_rows][ld] of `dtype` (umim_dtype), 16-B aligned; at
+ *               most 2^30 rows (as pairs below)
  * vocab, ld     vocabulary size (1 .. 262144) and row stride in elements: a
  *               multiple of 8 (fp32: 4), at least vocab; the elements from
  *               vocab up to ld are neither read nor written

@@ -121,7 +121,7 @@ umim_status logits_ok(const void *logits, int32_t dtype, int32_t n_rows, int32_t
   if (dtype != UMIM_DTYPE_BF16 && dtype != UMIM_DTYPE_FP16 && dtype != UMIM_DTYPE_FP32) return UMIM_ERR_INVALID_ARG;
   const int64_t vec = 16 / (int64_t)dtype_bytes(dtype);
   if (ld % vec != 0 || ld < vocab) return UMIM_ERR_INVALID_ARG;
-  if (vocab > kMaxLogitVocab) return UMIM_ERR_UNSUPPORTED;
+  if (vocab > kMaxLogitVocab || n_rows > kMaxLogitRows) return UMIM_ERR_UNSUPPORTED;
   if (n_rows > 0 && (!logits || !aligned(logits, 16))) return UMIM_ERR_INVALID_ARG;
   return UMIM_OK;
 }
@@ -479,6 +479,7 @@ umim_status umim_distill_topk_ce(const int32_t *top_ids, const float *top_logpro
   const umim_status st = logits_ok(student_logits, dtype, n_student_rows, vocab, ld);
   if (st != UMIM_OK) return st;
   if (n_teacher_rows < 0 || max_pairs < 0 || n_top < 1 || n_top > kMaxTop || !loss) return UMIM_ERR_INVALID_ARG;
+  if (max_pairs > kMaxLogitRows) return UMIM_ERR_UNSUPPORTED;
   if (!temperature_ok(temperature) || !std::isfinite(grad_scale)) return UMIM_ERR_INVALID_ARG;
   if (n_teacher_rows > 0 && (!top_ids || !top_logprobs)) return UMIM_ERR_INVALID_ARG;
   if (grad && !aligned(grad, 16)) return UMIM_ERR_INVALID_ARG;

@@ -9,6 +9,7 @@
 namespace umim {
 
 constexpr int kMaxLogitVocab = 262144;   // vocabulary size of the calls below, at most
+constexpr int kMaxLogitRows = 1 << 30;   // rows and pairs, at most: a row's number and a stride more fit 32 bits
 constexpr int kMaxTop = 128;             // alternatives per row, at most
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;

@@ -34,6 +34,7 @@ def test_token_logprobs(lib):
     assert call(dtype=2, V=1002, ld=1002) == 1
     assert call(V=1000, ld=992) == 1              # rows overlap
     assert call(V=262145, ld=262152) == 2         # vocabulary above the largest
+    assert call(R=2 ** 30 + 1) == 2               # and rows
     for T in (0.0, -1.0, nan, math.inf, 1e-5, 1e5):
         assert call(T=T) == 1, T
     assert call(n=-1) == 1 and call(n=129) == 1
@@ -70,6 +71,7 @@ def test_distill_topk_ce(lib):
     assert call(ids=null) == 1 and call(lp=null) == 1
     assert call(x=odd) == 1 and call(dtype=3) == 1 and call(V=0) == 1 and call(ld=996) == 1
     assert call(V=300000, ld=300000) == 2
+    assert call(R_S=2 ** 30 + 1) == 2 and call(P=2 ** 30 + 1) == 2
     assert call(tr=null) == 1 and call(sr=null) == 1
     assert call(T=nan) == 1 and call(scale=nan) == 1 and call(scale=math.inf) == 1
     assert call(loss=null) == 1
