@@ -467,3 +467,22 @@ def test_more_pairs_than_clusters(dtype, V, R, N):
     factor = 4 * (tol_l(V) + 8 * U * 64 + U * (K + 8)) / (N * T)
     off = (grad[:, :V].double() - wgrad).abs() - (eps + 4 * U) * wgrad.abs() - factor * size
     assert bool((off <= 1e-37).all())
+
+
+def test_rows_beyond_32_bits_of_elements():
+    m, dv = umim(), dev()
+    V, R, K = 128256, 17000, 10                           # 2.18e9 elements; only the first and last rows are paired
+    x = torch.empty((R, V), dtype=torch.bfloat16, device=dv)
+    ids, lp = lists(33, 3, K, V)
+    part = near(logits(33, 3, V, "bf16"), ids, lp, range(3), range(3), 1.0)
+    sr = np.array([R - 1, 0, R - 2])
+    x[torch.from_numpy(sr).to(dv)] = part.to(dv)
+    i32 = lambda a: torch.from_numpy(np.asarray(a, np.int32)).to(dv)
+    st = m.new_status(dv)
+    loss, pairs, grad = m.umim_distill_topk_ce(i32(ids), torch.from_numpy(lp).to(dv), x, i32(np.arange(3)), i32(sr),
+                                               dev_status=st)
+    torch.cuda.synchronize()
+    m.check_status(st)
+    same = np.arange(3)
+    check((loss, pairs, grad[torch.from_numpy(sr).to(dv)]), ids, lp, part, V, same, same, 1.0, True, "bf16")
+    assert not bool(grad[1:R - 2].any())

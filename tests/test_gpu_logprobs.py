@@ -504,3 +504,23 @@ def test_logits_far_from_zero(T, offset):
     grad = m.umim_token_logprobs_grad(x.to(dv), out["stats"], tok, g.to(dv), out["entropy"], h.to(dv), vocab=V,
                                       temperature=T)
     check_grad(grad, x, V, tokens, g, h, T, "fp32")
+
+
+def test_rows_beyond_32_bits_of_elements():
+    m, dv = umim(), dev()
+    V, R = 128256, 17000                                  # 2.18e9 elements; only the first and last rows count
+    x = torch.empty((R, V), dtype=torch.bfloat16, device=dv)
+    some = [0, R - 2, R - 1]
+    part = logits(31, 3, V, "bf16")
+    x[some] = part.to(dv)
+    tokens = np.full(R, -1, np.int32)
+    tokens[some] = [5, 128255, 77]
+    tok = torch.from_numpy(tokens).to(dv)
+    out = m.umim_token_logprobs(x, tok, n_top=9)
+    sub = {k: v[some] for k, v in out.items()}
+    check_forward(sub, part, V, tokens[some], 1.0, 9)
+    g = torch.ones(R, device=dv)
+    grad = m.umim_token_logprobs_grad(x, out["stats"], tok, g, grad=x)
+    torch.cuda.synchronize()
+    check_grad(grad[some], part, V, tokens[some], g[some], None, 1.0, "bf16")
+    assert not bool(grad[1].any()) and not bool(grad[R - 3].any())
