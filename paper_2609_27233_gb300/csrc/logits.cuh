@@ -29,7 +29,7 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
       : "memory");
 }
 
-// Brings whole vectors into L2 (16-byte aligned).
+// Brings whole vectors, one at least, into L2 (16-byte aligned).
 __device__ __forceinline__ void bulk_prefetch(const void *src, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }

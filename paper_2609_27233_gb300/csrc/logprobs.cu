@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
     take(u, e0);
   }
 
-  if (TOP && a.ahead > 0 && tid == 0 && r + a.ahead < rows_used(a.n_dev, a.R) &&
+  if (TOP && a.ahead > 0 && tid == 0 && end >= E::VEC && r + a.ahead < rows_used(a.n_dev, a.R) &&
       (!a.tokens || a.tokens[r + a.ahead] >= 0))
     bulk_prefetch(row + (int64_t)a.ahead * a.ld, (uint32_t)min(end / E::VEC * 16, kAheadBytes));
 

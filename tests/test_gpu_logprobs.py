@@ -475,6 +475,20 @@ def test_ties_in_many_rows(dtype, n_top):
     check_forward({k: (v[pick] if v is not None else None) for k, v in out.items()}, x[pick], V, None, 1.0, n_top)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("V,n_top", [(3, 3), (7, 5), (130, 128), (1999, 64), (4001, 128), (8192, 127), (16383, 128), (16385, 100)])
+def test_many_alternatives_of_many_rows(dtype, V, n_top):
+    """A CTA to each row, on both sides of what it reads in one go."""
+    m, dv = umim(), dev()
+    R = 620   # more than run at once
+    x = logits(V, R, V, dtype)
+    out = forward(m, x, dv, V, None, 1.0, n_top)
+    ids = x[:, :V].float().sort(dim=1, descending=True, stable=True)[1][:, :n_top]
+    assert torch.equal(out["top_ids"].cpu().long(), ids)
+    pick = [0, 151, 152, 304, R - 1]
+    check_forward({k: (v[pick] if v is not None else None) for k, v in out.items()}, x[pick], V, None, 1.0, n_top)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_one_value_everywhere_in_the_largest_vocabulary(dtype):
     m, dv = umim(), dev()
