@@ -634,12 +634,14 @@ umim_status launch_topk_ce(TopkArgs a, cudaStream_t stream, int num_sms) {
   attr[0].val.clusterDim.x = (unsigned)C;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
-  // Few CTAs start while the plan is being made.  Many must not: those that find an SM taken by it
-  // would wait for others to end, 402 against 286 us for 2870 pairs of 128256 bf16.
+  // Where a cluster has few pairs it starts while the plan is being made: 18.7 us instead of 21.7 for 108
+  // pairs of 128256 bf16, 31.5 instead of 34.5 for 220, 27.5 instead of 30.0 for 456 of 50257.  Where it
+  // has many it must not: some clusters find their SMs taken by the plan, come late and end last, 56.2
+  // instead of 54.5 for 448 pairs of 128256, 301 instead of 245 for 2870.
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = clusters * C <= 2 * num_sms ? 2 : 1;
+  cfg.numAttrs = (int64_t)a.R_S <= 2 * (int64_t)resident ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, topk_ce_kernel<E>, a);
   trace_mark(stream, nullptr);
   return e == cudaSuccess ? UMIM_OK : UMIM_ERR_CUDA;
