@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 #include "logits.cuh"
 
@@ -194,11 +195,11 @@ __global__ void __launch_bounds__(kPlanThreads) topk_plan_kernel(TopkArgs a) {
   if (lane == 0) a.heads[pr] = make_float2(whole, rest);
 }
 
-// A warp's stretch of a part of `vecs` vectors, and the shared memory for it: whole rounds of the
-// first pass, in vectors.
+// A warp's stretch of a part of `vecs` vectors, and the shared memory for it: a vector for each
+// lane, in vectors.
 __host__ __device__ __forceinline__ int stretch_vecs(int vecs) { return ceil_div(vecs, kWarps); }
 __host__ __device__ __forceinline__ int room_vecs(int vecs) {
-  return ceil_div(stretch_vecs(vecs), kUnroll * 32) * (kUnroll * 32);
+  return ceil_div(stretch_vecs(vecs), 32) * 32;
 }
 
 // What a warp's stretch of the row adds: outside the list the maximum mr and the sum of
@@ -342,13 +343,14 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
     // t = log2 e^((x - m) / T) is one FMA, x c + b with b = -m c rounded; the rounding r is made
     // good on a round's sum.  m follows the maximum when that has come 2^16 past it.
     float m = -INFINITY, top = -INFINITY, s = 0.f, b = 0.f, rf = 1.f;
-    for (int i0 = lane; i0 - lane < vecs; i0 += kUnroll * 32) {
-      uint4 u[kUnroll];
+    const auto sum_vecs = [&](auto many, int i0) {   // vectors i0, i0 + 32, ...
+      constexpr int U = decltype(many)::value;
+      uint4 u[U];
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) u[k] = pvec[i0 + k * 32];
+      for (int k = 0; k < U; ++k) u[k] = pvec[i0 + k * 32];
       uint32_t w = E::max_words(E::max_words(u[0].x, u[0].y), E::max_words(u[0].z, u[0].w));
 #pragma unroll
-      for (int k = 1; k < kUnroll; ++k)
+      for (int k = 1; k < U; ++k)
         w = E::max_words(w, E::max_words(E::max_words(u[k].x, u[k].y), E::max_words(u[k].z, u[k].w)));
       const float cm = E::to_float(E::word_max_bits(w));
       top = fmaxf(top, cm);
@@ -364,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
       float2 s0 = make_float2(0.f, 0.f), s1 = s0;
       if (!isnan(b)) {
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k)
+        for (int k = 0; k < U; ++k)
 #pragma unroll
           for (int i = 0; i < E::VEC / 2; ++i) {
             const float2 t = __ffma2_rn(pair_of<E>(u[k], i), c2, b2);
@@ -378,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
         s = fmaf(rf, s0.x + s0.y, s);
       } else {
 #pragma unroll 1
-        for (int k = 0; k < kUnroll; ++k) {
+        for (int k = 0; k < U; ++k) {
           const uint4 v = pvec[i0 + k * 32];
 #pragma unroll
           for (int i = 0; i < E::VEC / 2; ++i) {
@@ -387,7 +389,11 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
           }
         }
       }
-    }
+    };
+    int i0 = lane;
+    for (; i0 - lane + (kUnroll - 1) * 32 < vecs; i0 += kUnroll * 32)
+      sum_vecs(std::integral_constant<int, kUnroll>(), i0);
+    for (; i0 - lane < vecs; i0 += 32) sum_vecs(std::integral_constant<int, 1>(), i0);
     Part mine;
     mine.mr = warp_max(top);
     mine.m = fmaxf(mine.mr, warp_max(mx));
