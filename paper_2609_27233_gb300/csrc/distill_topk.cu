@@ -27,6 +27,7 @@ constexpr int kUnroll = 4;
 constexpr float kSlack = 16.f;
 constexpr int kMaxCluster = 8;    // CTAs per row, at most
 constexpr int kPartBytes = 65536; // three parts of this size fit an SM's shared memory
+constexpr int kHalfBytes = 106496; // two
 constexpr int kPlanThreads = 512, kPlanPairs = kPlanThreads / 32;
 constexpr int kTable = 2 * kMaxTop;   // slots for the ids of a list
 constexpr int kEntries = kMaxTop / 32;   // entries of a list per lane
@@ -568,14 +569,20 @@ size_t part_bytes(int V, int C, int esize) {
   return (size_t)room_vecs(slice_of(V, C) / (16 / esize)) * kWarps * 16;
 }
 
-// CTAs per row: as many as it takes for three parts to fit an SM, and for few rows more, while
-// that leaves an SM to each and a part is still worth a CTA (2048 elements).  Measured
-// for 57 rows of 32000 bf16: 11.5 us by two CTAs a row, 14.2 by four and eight.
+// CTAs per row: as many as it takes for three parts to fit an SM, or two where no cluster is large enough
+// for that; and for few rows more, while that leaves an SM to each and a part is still worth a CTA
+// (2048 elements).  Measured for 57 rows of 32000 bf16: 11.5 us by two CTAs a row, 14.2 by four
+// and eight; for 1500 of 151936 bf16: 160 by five, 166 by six, 201 by eight, three parts fitting
+// in each case; for 700 of 151936 fp32: 155 by six, two parts fitting as by seven, 172, and eight, 164.
 int cluster_for(int R, int V, int esize, int num_sms) {
-  int C = 1;
-  while (C < kMaxCluster && (part_bytes(V, C, esize) > (size_t)kPartBytes ||
-                             ((int64_t)R * 2 * C <= num_sms && V / (2 * C) >= 2048)))
-    C *= 2;
+  const auto fitting = [&](int bytes) {
+    int C = 1;
+    while (C < kMaxCluster && part_bytes(V, C, esize) > (size_t)bytes) ++C;
+    return C;
+  };
+  int C = fitting(kPartBytes);
+  if (part_bytes(V, C, esize) > (size_t)kPartBytes) C = fitting(kHalfBytes);
+  while (C < kMaxCluster && (int64_t)R * 2 * C <= num_sms && V / (2 * C) >= 2048) C = std::min(2 * C, kMaxCluster);
   return C;
 }
 

@@ -436,7 +436,9 @@ def test_logits_far_from_zero(offset, T, tail):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("V,R,N", [(12000, 600, 513), (70000, 400, 399), (300, 2000, 1999)])
+@pytest.mark.parametrize("V,R,N", [(12000, 600, 513), (70000, 400, 399), (300, 2000, 1999),
+                                   # clusters of 3, 5, 6 and 7 for bf16, of 6 and 7 for fp32
+                                   (96001, 330, 310), (151936, 200, 190), (185003, 170, 160), (215001, 130, 121)])
 def test_more_pairs_than_clusters(dtype, V, R, N):
     """Clusters take pair after pair: every row of the gradient against plain torch in float64."""
     m, dv = umim(), dev()
