@@ -519,8 +519,9 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
   const int beg = min(rank * a.slice, V), end = min(beg + a.slice, V);
   const TopShared<E> sh(dyn, a.slice, n, C);
   if (C > 1) cluster_arrive();   // what is pushed to a CTA waits until it runs
+  const bool writes = rank == 0 && tid == kThreads - 32;   // the row's numbers: a warp with little to search
   float x_t = 0.f;
-  if (rank == 0 && tid == 0) x_t = E::to_float(row[token]);
+  if (writes) x_t = E::to_float(row[token]);
 
   // ---- one pass over this CTA's part ----
   const float c = a.c;
@@ -621,6 +622,13 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
   // NaN and +inf have no place in the order, and a row that holds one has no alternatives
   const bool bad = !(all.s < INFINITY), empty = all.m == -INFINITY && !bad;
 
+  const float m0 = empty ? 0.f : all.m, l = bad ? NAN : empty ? 0.f : logf(all.s);
+  if (writes) {
+    if (a.logprobs) a.logprobs[r] = bad ? NAN : (x_t - m0) * a.inv_t - l;
+    if (a.entropy) a.entropy[r] = bad ? NAN : empty ? 0.f : l - kLn2 * (all.w / all.s);
+    if (a.stats) a.stats[r] = bad ? make_float2(NAN, NAN) : make_float2(all.m, l);
+  }
+
   int M = 0;   // the candidates, in s_cand of rank 0
   if constexpr (TOP) {
     if (!bad && !empty) {
@@ -677,13 +685,7 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
   }
   if (rank != 0) return;
 
-  // ---- outputs ----
-  const float m0 = empty ? 0.f : all.m, l = bad ? NAN : empty ? 0.f : logf(all.s);
-  if (tid == 0) {
-    if (a.logprobs) a.logprobs[r] = bad ? NAN : (x_t - m0) * a.inv_t - l;
-    if (a.entropy) a.entropy[r] = bad ? NAN : empty ? 0.f : l - kLn2 * (all.w / all.s);
-    if (a.stats) a.stats[r] = bad ? make_float2(NAN, NAN) : make_float2(all.m, l);
-  }
+  // ---- the alternatives in order ----
   if constexpr (TOP) {
     uint64_t mine;
     int place = 0;
