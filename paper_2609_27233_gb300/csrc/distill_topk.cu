@@ -215,7 +215,7 @@ struct __align__(16) Part {
 // student's row, and each warp on one of eight contiguous stretches of that,
 // which stays in shared memory between the two passes over it: every logit is
 // read once and every gradient element written once, and what bounds the kernel is
-// that traffic (8700 pairs of 128256 bf16 with 9600 rows: 740 us, 6.3 TB/s).  A warp
+// that traffic (8700 pairs of 128256 bf16 with 9600 rows: 746 us, 6.3 TB/s).  A warp
 // loads its stretch of the next pair's row, by an asynchronous copy, as soon as it has
 // written this one's gradient.  Once a pair every warp tells all CTAs of the
 // cluster its sums, by asynchronous stores that count on a barrier in each of

@@ -210,7 +210,7 @@ struct Running {
 // What bounds it: without alternatives the one read of the logits (4096 rows of 128256
 // bf16: 149 us, 7.0 TB/s, above the measured copy's rate); with them the
 // instructions as well, 5.8 a logit for the pass and 1.4 (one alternative) to 2.8
-// (128) for segments and search: 167 us with 20, 179 with 64.
+// (128) for segments and search: 165 us with 20, 174 with 64, 187 with 128.
 //
 // All of it happens in shared memory and registers of the cluster: no
 // workspace, no atomics on global memory, the same bits in every call.
