@@ -520,6 +520,52 @@ def test_logits_far_from_zero(T, offset):
     check_grad(grad, x, V, tokens, g, h, T, "fp32")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("V,R,n_top", [(1, 3, 1), (2, 9, 2), (700, 40, 5), (8191, 700, 0), (32000, 7, 20), (50257, 200, 0),
+                                       (128256, 6, 0), (128256, 40, 3), (151936, 90, 64), (262143, 3, 10)])
+def test_rows_of_one_outcome(dtype, V, R, n_top):
+    """One element has nearly all of the probability: the others' share, ln s and the entropy to their own size."""
+    m, dv = umim(), dev()
+    T = 0.7
+    r = np.random.default_rng(V + R)
+    x = logits(V + R, R, V, dtype, std=1.5)
+    at = np.concatenate([[0, V - 1, V // 2], r.integers(0, V, R)])[:R]
+    gap = np.resize([4.0, 6.0, 10.0, 20.0, 40.0, 80.0], R)
+    lse = torch.logsumexp(x[:, :V].double() / T, 1).numpy()
+    x[np.arange(R), at] = torch.from_numpy(T * (lse + gap)).to(x.dtype)
+    if R > 8:
+        x[8, :V] = -math.inf                             # and one with nothing else
+        x[8, at[8]] = 1.5
+    out = forward(m, x, dv, V, at, T, n_top)
+    y = f64(x)[:, :V]
+    y = (y - y[np.arange(R), at][:, None]) / T
+    y[np.arange(R), at] = -np.inf
+    assert (y < 0).all()
+    e, ay = np.exp(y), np.where(np.isinf(y), 0.0, -y)
+    rest = e.sum(1)
+    assert (rest < 1 / 32).all()
+    H = np.log1p(rest) + (e * ay).sum(1) / (1 + rest)
+    # An exponential: 3 U |y| from the exponent, 4 U its own, and from up to four changes of reference by
+    # d nats 2 U |d| + 4 U each, the |d| adding up to |y| + 12; sums of V / 256 terms and less.
+    # Weighed with y, a change by up to 12 loses 3 x 12 U beside terms of 3 and more.
+    # Exponentials below 2^-126, where |y| is above 87.3, come out as 0: V of them at most, and as y e^-y falls
+    # there, each with less than 88.4 2^-126 of entropy.
+    k = U * (V / 256 + 300 + 8 * ay)
+    tol_rest, tol_H = (k * e).sum(1) + V * 2.0 ** -126, (k * e * (1 + ay)).sum(1) + V * 88.4 * 2.0 ** -126
+    within(f64(out["stats"])[:, 1], np.log1p(rest), tol_rest, "log of the sum")
+    within(f64(out["logprobs"]), -np.log1p(rest), tol_rest, "logprobs")
+    within(f64(out["entropy"]), H, tol_H, "entropy")
+    if n_top:
+        assert np.array_equal(out["top_ids"][:, 0].cpu().numpy(), at)
+        within(f64(out["top_logprobs"])[:, 0], -np.log1p(rest), tol_rest, "best alternative")
+    # two of them share it: neither is certain
+    other = (at + 1) % V
+    x[np.arange(R), other] = x[np.arange(R), at]
+    out = forward(m, x, dv, V, at, T, n_top)
+    few = slice(0, 10)
+    check_forward({k: (v[few] if v is not None else None) for k, v in out.items()}, x[few], V, at[few], T, n_top)
+
+
 def test_rows_beyond_32_bits_of_elements():
     m, dv = umim(), dev()
     V, R = 128256, 17000                                  # 2.18e9 elements; only the first and last rows count
