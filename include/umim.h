@@ -686,9 +686,12 @@ umim_status umim_token_logprobs_grad(const void *logits, int32_t dtype, int32_t 
  * row s_k; umim_distill_align), with the teacher's entries (a_i, lambda_i)
  * and q = softmax(x / T) of the student's row x:
  *   tail == 0   p = softmax(lambda) over the entries, p_rest = 0
- *   tail != 0   p_i = exp(lambda_i), p_rest = 1 - sum_i p_i: the rest of the
- *               vocabulary counts as one outcome (below 2^-20, which is the
- *               rounding of a list that holds everything, it counts as 0)
+ *   tail != 0   p_i = exp(lambda_i), p_rest = 1 - sum_i p_i, at least 0: the
+ *               rest of the vocabulary counts as one outcome.  p_rest is as
+ *               exact as the largest entry's 1 - p (its error is 2^-20 of
+ *               that at most); where q_rest is none either (below 2^-100), a
+ *               p_rest below 2^-20, which is the rounding of a list that
+ *               holds everything, counts as 0
  *   pair loss = -sum_i p_i ln q(a_i) - p_rest ln q_rest,
  *     q_rest = the sum of q outside the list;  loss = the pair losses' mean
  * and grad_scale times the loss's gradient with respect to the student logits,

@@ -19,8 +19,10 @@ teacher's entries make a distribution over the listed ids and, with a tail, one
 more outcome that stands for everything else; the student's q is summed
 over everything else for that outcome.  The gradient is that of the loss written
 as cross-entropy with a full target: the tail's mass spread over the
-unlisted ids in the student's own proportions.  A rest below 2^-20 is what rounding left of a list
-that holds everything, and counts as none.
+unlisted ids in the student's own proportions.  The rest is 1 - sum p, taken as the largest entry's
+1 - p less the others, so that it keeps its digits where one entry has nearly everything.  Only where the
+student has no rest either (q_rest below 2^-100) a rest below 2^-20 is what rounding left
+of a list that holds everything, and counts as none.
 """
 import numpy as np
 
@@ -104,13 +106,16 @@ def topk_ce(top_ids, top_logprobs, student, teacher_rows, student_rows, T=1.0, t
         p = np.exp(np.array([lam for _, lam in entries], np.float64))
         if not tail and p.sum() > 0:
             p = p / p.sum()
-        rest = 1.0 - p.sum() if tail else 0.0
-        if rest < 2.0 ** -20:
-            rest = 0.0
+        rest = 0.0
+        if tail:
+            lam = np.sort(np.array([lam for _, lam in entries], np.float64))
+            rest = max(0.0, -np.expm1(lam[-1]) - np.exp(lam[:-1]).sum()) if len(lam) else 1.0
         inside = np.zeros(V, bool)
         inside[ids] = True
         logq = _log_softmax(x[s] / T)
         q = np.exp(logq)
+        if rest < 2.0 ** -20 and q[~inside].sum() < 2.0 ** -100:
+            rest = 0.0
         if np.any(p > 0):
             i = np.array(ids)[p > 0]
             losses[k] -= (p[p > 0] * logq[i]).sum()

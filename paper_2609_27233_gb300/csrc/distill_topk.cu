@@ -31,10 +31,12 @@ constexpr int kHalfBytes = 106496; // two
 constexpr int kPlanThreads = 512, kPlanPairs = kPlanThreads / 32;
 constexpr int kTable = 2 * kMaxTop;   // slots for the ids of a list
 constexpr int kEntries = kMaxTop / 32;   // entries of a list per lane
-// The listed log probabilities are fp32: their exponentials are off by up to
-// about 16 2^-24 each, relatively, so 1 - sum p below 2^-20 is rounding, and
-// its logarithm's partner q_rest may be 0 where the list holds all there is.
+// A list that holds all there is leaves a p_rest of rounding: the listed log probabilities are fp32, each
+// off by up to about 16 2^-24.  Where the student's rest is nothing too (its mask is
+// the teacher's, or no id is left), ln q_rest is no measure of anything, so
+// there, and only there, a p_rest below 2^-20 counts as 0.
 constexpr float kLeastRest = 9.5367431640625e-7f;
+constexpr float kNoRest = 7.8886090522101181e-31f;   // q_rest below 2^-100 is none: far above where it underflows
 
 struct TopkHeader {
   int32_t status;         // status word when the caller passes none
@@ -170,22 +172,37 @@ __global__ void __launch_bounds__(kPlanThreads) topk_plan_kernel(TopkArgs a) {
       id[j] = -1;
     }
   if (wrong) set_error(a.status, UMIM_ERR_INVALID_ARG);
-  float top = -INFINITY, sum = 0.f;
+  float top = -INFINITY;
 #pragma unroll
   for (int j = 0; j < kEntries; ++j)
     if (id[j] >= 0) top = fmaxf(top, lam[j]);
-  top = a.tail ? 0.f : warp_max(top);
+  top = warp_max(top);
+  // The largest entry is kept apart from the sum of the others.  1 - sum p is taken as (1 - p_max) - others,
+  // 1 - p_max as -expm1(lambda_max): off by 16 2^-24 of 1 - p_max at most, about what the rounding of the other
+  // entries' lambda means.  (1 minus the sum of all is off by 2^-24 of 1: a teacher
+  // that is sure of one token lost up to 7 % of a p_rest of 3e-6.)
+  bool mine = false;   // this lane has the largest entry, or one as large
+#pragma unroll
+  for (int j = 0; j < kEntries; ++j) mine |= id[j] >= 0 && lam[j] == top;
+  const unsigned holders = __ballot_sync(0xffffffffu, mine && top != -INFINITY);
+  mine = holders != 0 && lane == __ffs(holders) - 1;
+  const float base = a.tail || top == -INFINITY ? 0.f : top;
+  float others = 0.f;
 #pragma unroll
   for (int j = 0; j < kEntries; ++j) {
-    p[j] = id[j] >= 0 && !(lam[j] == -INFINITY) ? expf(lam[j] - top) : 0.f;
-    sum += p[j];
+    p[j] = id[j] >= 0 && !(lam[j] == -INFINITY) ? expf(lam[j] - base) : 0.f;
+    if (mine && id[j] >= 0 && lam[j] == top)
+      mine = false;   // the largest, once
+    else
+      others += p[j];
   }
-  sum = warp_sum(sum);
+  others = warp_sum(others);
+  const float sum = (holders ? expf(top - base) : 0.f) + others;
   float whole = sum, rest = 0.f, scale = 1.f;
   if (a.tail) {
-    rest = 1.f - sum;
-    if (rest < kLeastRest) rest = 0.f;
-    whole += rest;
+    rest = -expm1f(top) - others;
+    if (rest < 0.f) rest = 0.f;
+    if (rest > 0.f) whole = 1.f;
   } else if (sum != 0.f) {   // a row without entries adds nothing
     scale = 1.f / sum;
     whole = 1.f;
@@ -320,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
     const uint32_t word = other < a.R_S ? a.paired[other >> 5] : 0;
     const int next = pr + clusters;
     const int next_row = next < N ? a.student_rows[next] : 0;
-    const float whole = head.x, rest = head.y;   // P, p_rest
+    float whole = head.x, rest = head.y;   // P, p_rest
     wait(landed, (uint32_t)count & 1u);
     if (lane == 0 && whole_vecs < vecs) pvec[whole_vecs] = cut;
     __syncwarp();
@@ -457,6 +474,10 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
     const float down = rescale(all_mr, all_m);   // from the rest's maximum to the row's
     const float Z = all_rest * down + all_top;
     const bool empty = all_m == -INFINITY && Z == 0.f;
+    if (rest < kLeastRest && all_rest * down / Z < kNoRest) {
+      whole -= rest;
+      rest = 0.f;
+    }
     if (rank == 0 && tid == 0 && in_bounds(pr, a.max_pairs, a.status, kSiteTopkPair)) {
       // sum p (ln Z - y) + p_rest (ln Z - ln of the rest's sum)
       const float lz = logf(Z), listed = whole - rest;
