@@ -698,7 +698,9 @@ umim_status umim_token_logprobs_grad(const void *logits, int32_t dtype, int32_t 
  * with P = sum_i p_i + p_rest:
  *   grad_scale / (N T) q_v (P - p_rest / q_rest)     outside the list
  *   grad_scale / (N T) (P q_v - p_i)                 at v = a_i;
- * student rows in no pair have a zero gradient.  Computed in fp32.
+ * student rows in no pair have a zero gradient.  Computed in fp32; where one
+ * token, or the rest, has nearly all of the student's probability (or of the
+ * teacher's), losses and gradients are exact to the size of what is left.
  * top_ids, top_logprobs  device int32 / fp32 [n_teacher_rows][n_top]; id -1:
  *               no entry (a teacher row without entries has a pair loss of 0,
  *               and its pair's gradient is 0)

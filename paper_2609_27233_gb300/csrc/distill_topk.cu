@@ -12,6 +12,8 @@
 //                   (1/T) (P q_v - p_i)               at v = a_i,   P = sum p + p_rest
 // q_rest is summed over the elements outside the list: one minus the listed
 // ones would lose it where the student puts nearly everything on them.
+// For the same reason every 1 - q and 1 - p below is a sum of what is left, and every ln of
+// a q near 1 a log1p.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -51,6 +53,13 @@ struct Entry {
   float p;
 };
 
+// A pair's teacher row beside its entries.
+struct __align__(16) Head {
+  float listed, rest;   // sum p, p_rest
+  float others;         // sum p without the largest entry
+  float pad;
+};
+
 struct TopkArgs {
   const int32_t *top_ids;      // [R_T][K]
   const float *top_logprobs;   // [R_T][K]
@@ -67,7 +76,7 @@ struct TopkArgs {
   void *grad;                  // or nullptr
   uint32_t *paired;            // [R_S] bits: the student rows in a pair
   Entry *lists;                // [max_pairs][K] the pairs' entries as the main kernel takes them
-  float2 *heads;               // [max_pairs] (P, p_rest)
+  Head *heads;                 // [max_pairs]
   TopkHeader *hdr;
   int32_t *status;
 };
@@ -198,19 +207,18 @@ __global__ void __launch_bounds__(kPlanThreads) topk_plan_kernel(TopkArgs a) {
   }
   others = warp_sum(others);
   const float sum = (holders ? expf(top - base) : 0.f) + others;
-  float whole = sum, rest = 0.f, scale = 1.f;
+  float listed = sum, rest = 0.f, scale = 1.f;
   if (a.tail) {
     rest = -expm1f(top) - others;
     if (rest < 0.f) rest = 0.f;
-    if (rest > 0.f) whole = 1.f;
   } else if (sum != 0.f) {   // a row without entries adds nothing
     scale = 1.f / sum;
-    whole = 1.f;
+    listed = 1.f;
   }
 #pragma unroll
   for (int j = 0; j < kEntries; ++j)
     if (j * 32 + lane < K) a.lists[(int64_t)pr * K + j * 32 + lane] = Entry{id[j], p[j] * scale};
-  if (lane == 0) a.heads[pr] = make_float2(whole, rest);
+  if (lane == 0) a.heads[pr] = Head{listed, rest, others * scale, 0.f};
 }
 
 // A warp's stretch of a part of `vecs` vectors, and the shared memory for it: a vector for each
@@ -221,9 +229,10 @@ __host__ __device__ __forceinline__ int room_vecs(int vecs) {
 }
 
 // What a warp's stretch of the row adds: outside the list the maximum mr and the sum of
-// 2^((x - mr) c); the maximum m of the whole stretch, and over the listed
-// elements the sums of 2^((x - m) c), p and p (x - m) / T.  The rest keeps a maximum
+// 2^((x - mr) c); over the listed elements the maximum m, and the sums of 2^((x - m) c), without one
+// element at m itself, of p and of p (x - m) / T.  The rest keeps a maximum
 // of its own: where the listed ones are far above it, its sum would be nothing beside m.
+// The element at m, a 1, is left out because beside it the others would lose their digits.
 struct __align__(16) Part {
   float m, mr, rest, top, p, py, pad[2];
 };
@@ -281,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
   if (s_row >= a.R_S) s_row = -1;
   uint4 cut = make_uint4(0, 0, 0, 0);
   Entry e[kEntries];
-  float2 head = make_float2(0.f, 0.f);
+  Head head{0.f, 0.f, 0.f, 0.f};
   const auto load_list = [&](int q) {
 #pragma unroll
     for (int j = 0; j < kEntries; ++j)
@@ -337,7 +346,8 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
     const uint32_t word = other < a.R_S ? a.paired[other >> 5] : 0;
     const int next = pr + clusters;
     const int next_row = next < N ? a.student_rows[next] : 0;
-    float whole = head.x, rest = head.y;   // P, p_rest
+    const float listed = head.listed, others = head.others;
+    float rest = head.rest;
     wait(landed, (uint32_t)count & 1u);
     if (lane == 0 && whole_vecs < vecs) pvec[whole_vecs] = cut;
     __syncwarp();
@@ -414,21 +424,28 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
     for (; i0 - lane < vecs; i0 += 32) sum_vecs(std::integral_constant<int, 1>(), i0);
     Part mine;
     mine.mr = warp_max(top);
-    mine.m = fmaxf(mine.mr, warp_max(mx));
+    mine.m = warp_max(mx);
     {
       const float m0 = mine.m == -INFINITY ? 0.f : mine.m;
       float top = 0.f, p = 0.f, py = 0.f;
+      int at_m = 0;
 #pragma unroll
       for (int j = 0; j < kEntries; ++j)
         if (j * 32 < K && e[j].id >= 0) {
           const float y = x[j] - m0;
-          top += ex2(y * c);
+          if (x[j] == mine.m && mine.m != -INFINITY) {
+            ++at_m;
+            top += y;   // nothing, or NaN for +inf
+          } else {
+            top += ex2(y * c);
+          }
           p += e[j].p;
           if (e[j].p != 0.f) py = fmaf(e[j].p, y * a.inv_t, py);
         }
       const float2 u = warp_sum2(make_float2(s * rescale(m, mine.mr), top)), v = warp_sum2(make_float2(p, py));
       mine.rest = u.x;
-      mine.top = u.y;
+      at_m = __reduce_add_sync(0xffffffffu, at_m);
+      mine.top = u.y + (float)max(at_m - 1, 0);
       mine.p = v.x;
       mine.py = v.y;
     }
@@ -450,40 +467,52 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
       if (lane == 0) s_parts[turn][warp] = mine;
       __syncthreads();
     }
-    float all_m = -INFINITY, all_mr = -INFINITY;
+    float all_ml = -INFINITY, all_mr = -INFINITY;
     for (int i = lane; i < C * kWarps; i += 32) {
-      all_m = fmaxf(all_m, parts[i].m);
+      all_ml = fmaxf(all_ml, parts[i].m);
       all_mr = fmaxf(all_mr, parts[i].mr);
     }
-    all_m = warp_max(all_m);
+    all_ml = warp_max(all_ml);
     all_mr = warp_max(all_mr);
-    float all_rest = 0.f, all_top = 0.f, all_py = 0.f;
+    const float all_m = fmaxf(all_ml, all_mr);
+    float all_rest = 0.f, all_top = 0.f, all_py = 0.f, at_ml = 0.f;
     for (int i = lane; i < C * kWarps; i += 32) {
       const Part q = parts[i];
       all_rest += q.rest * rescale(q.mr, all_mr);
-      all_top += q.top * rescale(q.m, all_m);
+      if (q.m == all_ml) {
+        all_top += q.top;
+        at_ml += 1.f;
+      } else {
+        all_top += (q.top + 1.f) * rescale(q.m, all_ml);
+      }
       all_py += q.py + (q.p != 0.f && q.m != all_m && q.m != -INFINITY ? q.p * ((q.m - all_m) * a.inv_t) : 0.f);
     }
     {
-      const float2 u = warp_sum2(make_float2(all_rest, all_top));
+      const float2 u = warp_sum2(make_float2(all_rest, all_top)), v = warp_sum2(make_float2(all_py, at_ml));
       all_rest = u.x;
-      all_top = u.y;
-      all_py = warp_sum(all_py);
+      all_top = all_ml == -INFINITY ? u.y : u.y + (v.y - 1.f);
+      all_py = v.x;
     }
+    // The row's sum at its maximum: what is listed and the rest.  Where the maximum is a listed element, Z is
+    // 1 + beside; with q = 1 / Z of that element, 1 - q is beside / Z and -ln q is log1p(beside), to
+    // their own digits however near 1 q is.
     const float m0 = all_m == -INFINITY ? 0.f : all_m;
     const float down = rescale(all_mr, all_m);   // from the rest's maximum to the row's
-    const float Z = all_rest * down + all_top;
-    const bool empty = all_m == -INFINITY && Z == 0.f;
-    if (rest < kLeastRest && all_rest * down / Z < kNoRest) {
-      whole -= rest;
-      rest = 0.f;
-    }
+    const float sum_rest = all_rest * down;
+    const float sum_listed = all_ml == -INFINITY ? all_top : (1.f + all_top) * rescale(all_ml, all_m);
+    const bool best_listed = all_ml == all_m && all_ml != -INFINITY;
+    const float beside = all_top + sum_rest, Z = best_listed ? 1.f + beside : sum_listed + sum_rest;
+    const bool empty = all_m == -INFINITY && Z == 0.f, no_rest = sum_rest / Z < kNoRest;
+    if (rest < kLeastRest && no_rest) rest = 0.f;
+    const float whole = rest > 0.f ? 1.f : listed;   // P
     if (rank == 0 && tid == 0 && in_bounds(pr, a.max_pairs, a.status, kSiteTopkPair)) {
       // sum p (ln Z - y) + p_rest (ln Z - ln of the rest's sum)
-      const float lz = logf(Z), listed = whole - rest;
+      const float lz = best_listed ? log1pf(beside) : logf(Z);
       float loss = (listed != 0.f ? listed * lz : 0.f) - all_py;
       if (rest > 0.f)
-        loss += all_rest == 0.f ? INFINITY : rest * (lz - logf(all_rest) + (all_m - all_mr) * a.inv_t);
+        loss += all_rest == 0.f ? INFINITY
+                                : rest * (no_rest ? lz - logf(all_rest) + (all_m - all_mr) * a.inv_t
+                                                  : log1pf(sum_listed / sum_rest));
       if (empty) loss = whole != 0.f ? INFINITY : 0.f;
       a.pair_loss[pr] = isnan(Z) ? NAN : loss;
     }
@@ -491,9 +520,10 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
     // ---- the gradient ----
     if (a.grad && in_bounds(s_row, a.R_S, a.status, kSiteTopkStudentRow)) {
       const float g = a.grad_scale * a.inv_t / (float)N;
-      // outside: 2^((x - mr) c) times this
-      const float q = whole * (down / Z);
-      const float coef = empty ? 0.f : g * (rest > 0.f && all_rest > 0.f ? q - rest / all_rest : q);
+      // Outside: 2^((x - mr) c), over the rest's sum, times P q_rest - p_rest; where the rest has most of the row,
+      // that is sum p - P q_listed, both of them small.
+      const float pull = sum_rest > sum_listed ? listed - whole * (sum_listed / Z) : whole * (sum_rest / Z) - rest;
+      const float coef = empty ? 0.f : all_rest > 0.f ? g * pull / all_rest : 0.f * Z;   // NaN stays one
       const float mr = all_mr == -INFINITY ? 0.f : all_mr, bias = -mr * c, r = fmaf(-mr, c, -bias);
       const bool exact = fabsf(r) <= 1.f;   // as above
       const float fcoef = coef * ex2(r);
@@ -539,8 +569,14 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < kEntries; ++j)
-        if (j * 32 < K && e[j].id >= 0)
-          out[e[j].id] = E::from_float(empty ? 0.f : g * (whole * (ex2((x[j] - m0) * c) / Z) - e[j].p));
+        if (j * 32 < K && e[j].id >= 0) {
+          // P q - p; where q is above one half, (P - p) - P (1 - q) instead, and where p is too (it is the
+          // largest then), P - p is what the others and the rest add up to
+          const float d = x[j] == all_m && beside < 1.f
+                              ? (e[j].p > 0.5f * whole ? others + rest : whole - e[j].p) - whole * (beside / Z)
+                              : whole * (ex2((x[j] - m0) * c) / Z) - e[j].p;
+          out[e[j].id] = E::from_float(empty ? 0.f : g * d);
+        }
     }
     // ---- the next pair's ----
     s_row = next_row;
@@ -686,7 +722,7 @@ umim_status launch_topk_ce(TopkArgs a, cudaStream_t stream, int num_sms) {
 size_t distill_topk_ce_workspace_bytes(int R_S, int max_pairs) {
   const size_t P = (size_t)std::max(max_pairs, 1);
   return sizeof(TopkHeader) + a256(sizeof(uint32_t) * ((size_t)R_S / 32 + 1)) + a256(sizeof(float) * P) +
-         a256(sizeof(float2) * P) + a256(sizeof(Entry) * kMaxTop * P);
+         a256(sizeof(Head) * P) + a256(sizeof(Entry) * kMaxTop * P);
 }
 
 umim_status distill_topk_ce(const int32_t *top_ids, const float *top_logprobs, int R_T, int K, const void *student,
@@ -725,7 +761,7 @@ umim_status distill_topk_ce(const int32_t *top_ids, const float *top_logprobs, i
   a.paired = reinterpret_cast<uint32_t *>(take(sizeof(uint32_t) * ((size_t)R_S / 32 + 1)));
   float *ws_pair_loss = reinterpret_cast<float *>(take(sizeof(float) * P));
   a.pair_loss = pair_loss ? pair_loss : ws_pair_loss;
-  a.heads = reinterpret_cast<float2 *>(take(sizeof(float2) * P));
+  a.heads = reinterpret_cast<Head *>(take(sizeof(Head) * P));
   a.lists = reinterpret_cast<Entry *>(take(sizeof(Entry) * kMaxTop * P));
   a.hdr = hdr;
   a.status = dev_status ? dev_status : &hdr->status;
