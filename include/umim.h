@@ -703,7 +703,10 @@ umim_status umim_token_logprobs_grad(const void *logits, int32_t dtype, int32_t 
  * teacher's), losses and gradients are exact to the size of what is left.
  * top_ids, top_logprobs  device int32 / fp32 [n_teacher_rows][n_top]; id -1:
  *               no entry (a teacher row without entries has a pair loss of 0,
- *               and its pair's gradient is 0)
+ *               and its pair's gradient is 0).  A row of ids -1 with log
+ *               probabilities NaN only, as umim_token_logprobs writes it for
+ *               logits with NaN or +inf, and a row with NaN at an id, make
+ *               the pair's loss and gradient NaN
  * n_top         1 .. 128
  * student_logits, dtype, vocab, ld, temperature  as umim_token_logprobs
  * teacher_rows, student_rows  device int32 [max_pairs] (e.g. from

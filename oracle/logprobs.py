@@ -22,7 +22,8 @@ as cross-entropy with a full target: the tail's mass spread over the
 unlisted ids in the student's own proportions.  The rest is 1 - sum p, taken as the largest entry's
 1 - p less the others, so that it keeps its digits where one entry has nearly everything.  Only where the
 student has no rest either (q_rest below 2^-100) a rest below 2^-20 is what rounding left
-of a list that holds everything, and counts as none.
+of a list that holds everything, and counts as none.  A teacher row that held NaN or +inf (ids -1, all log
+probabilities NaN), or has NaN at an id, makes the pair's loss and gradient NaN.
 """
 import numpy as np
 
@@ -103,6 +104,10 @@ def topk_ce(top_ids, top_logprobs, student, teacher_rows, student_rows, T=1.0, t
         entries = [(int(i), float(lam)) for i, lam in zip(top_ids[t], top_logprobs[t]) if i >= 0]
         ids = [i for i, _ in entries]
         assert len(set(ids)) == len(ids)
+        lam_t = np.asarray(top_logprobs[t], np.float64)
+        if np.isnan([lam for _, lam in entries]).any() or (not entries and np.isnan(lam_t).all()):
+            losses[k] = grad[s] = np.nan
+            continue
         p = np.exp(np.array([lam for _, lam in entries], np.float64))
         if not tail and p.sum() > 0:
             p = p / p.sum()

@@ -148,6 +148,11 @@ __global__ void __launch_bounds__(kPlanThreads) topk_plan_kernel(TopkArgs a) {
     id[j] = i < K ? a.top_ids[(int64_t)t * K + i] : -1;
     lam[j] = i < K ? a.top_logprobs[(int64_t)t * K + i] : -INFINITY;
   }
+  // what umim_token_logprobs leaves of a row of logits with NaN or +inf in it
+  bool spoilt = true;
+#pragma unroll
+  for (int j = 0; j < kEntries; ++j) spoilt &= j * 32 + lane >= K || (id[j] == -1 && isnan(lam[j]));
+  spoilt = __all_sync(0xffffffffu, spoilt);
   bool wrong = false;
 #pragma unroll
   for (int j = 0; j < kEntries; ++j)
@@ -208,12 +213,14 @@ __global__ void __launch_bounds__(kPlanThreads) topk_plan_kernel(TopkArgs a) {
   others = warp_sum(others);
   const float sum = (holders ? expf(top - base) : 0.f) + others;
   float listed = sum, rest = 0.f, scale = 1.f;
-  if (a.tail) {
+  if (spoilt) {
+    listed = NAN;
+  } else if (a.tail) {
     rest = -expm1f(top) - others;
     if (rest < 0.f) rest = 0.f;
   } else if (sum != 0.f) {   // a row without entries adds nothing
     scale = 1.f / sum;
-    listed = 1.f;
+    if (!isnan(sum)) listed = 1.f;
   }
 #pragma unroll
   for (int j = 0; j < kEntries; ++j)
@@ -514,16 +521,16 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
                                 : rest * (no_rest ? lz - logf(all_rest) + (all_m - all_mr) * a.inv_t
                                                   : log1pf(sum_listed / sum_rest));
       if (empty) loss = whole != 0.f ? INFINITY : 0.f;
-      a.pair_loss[pr] = isnan(Z) ? NAN : loss;
+      a.pair_loss[pr] = isnan(Z) || isnan(whole) ? NAN : loss;
     }
 
     // ---- the gradient ----
     if (a.grad && in_bounds(s_row, a.R_S, a.status, kSiteTopkStudentRow)) {
-      const float g = a.grad_scale * a.inv_t / (float)N;
+      const float per = empty ? 0.f : 1.f / Z, g = empty ? 0.f : a.grad_scale * a.inv_t / (float)N;
       // Outside: 2^((x - mr) c), over the rest's sum, times P q_rest - p_rest; where the rest has most of the row,
       // that is sum p - P q_listed, both of them small.
-      const float pull = sum_rest > sum_listed ? listed - whole * (sum_listed / Z) : whole * (sum_rest / Z) - rest;
-      const float coef = empty ? 0.f : all_rest > 0.f ? g * pull / all_rest : 0.f * Z;   // NaN stays one
+      const float pull = sum_rest > sum_listed ? listed - whole * (sum_listed * per) : whole * (sum_rest * per) - rest;
+      const float coef = all_rest > 0.f ? g * pull / all_rest : 0.f * Z * whole;   // NaN stays one
       const float mr = all_mr == -INFINITY ? 0.f : all_mr, bias = -mr * c, r = fmaf(-mr, c, -bias);
       const bool exact = fabsf(r) <= 1.f;   // as above
       const float fcoef = coef * ex2(r);
@@ -573,9 +580,9 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
           // P q - p; where q is above one half, (P - p) - P (1 - q) instead, and where p is too (it is the
           // largest then), P - p is what the others and the rest add up to
           const float d = x[j] == all_m && beside < 1.f
-                              ? (e[j].p > 0.5f * whole ? others + rest : whole - e[j].p) - whole * (beside / Z)
-                              : whole * (ex2((x[j] - m0) * c) / Z) - e[j].p;
-          out[e[j].id] = E::from_float(empty ? 0.f : g * d);
+                              ? (e[j].p > 0.5f * whole ? others + rest : whole - e[j].p) - whole * (beside * per)
+                              : whole * (ex2((x[j] - m0) * c) * per) - e[j].p;
+          out[e[j].id] = E::from_float(g * d);
         }
     }
     // ---- the next pair's ----

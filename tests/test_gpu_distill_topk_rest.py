@@ -126,3 +126,39 @@ def test_a_rest_of_rounding_counts_only_where_the_student_has_one(dtype, mask):
     eps = torch.finfo(TYPES[dtype]).eps / 2
     within(f64(grad)[:, :V], wgrad, (eps + 4 * U) * np.abs(wgrad) + (4 * tol_l(V) + 800 * U) / R, "gradient")
     assert bool((grad[:6, blocked.to(dv)] == 0).all())
+
+
+@pytest.mark.parametrize("tail", [True, False])
+@pytest.mark.parametrize("K", [1, 20, 33, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_teacher_row_without_a_distribution_is_not_lost(bad, K, tail):
+    """NaN or +inf among the teacher's logits: the cache says so, and the pair's loss and gradient are NaN, as are those
+    of a list with NaN at an id.  A row left out, and one whose ids are -1 whatever stands beside, ask nothing."""
+    m, dv = umim(), dev()
+    V, R = 3000, 6
+    r = np.random.default_rng(K)
+    t, x = padded(2.0 * r.standard_normal((R, V)), "bf16"), padded(2.0 * r.standard_normal((R, V)), "fp32")
+    t[1, V - 1] = bad
+    tok = torch.tensor([0, 0, -1, 0, 0, 0], dtype=torch.int32, device=dv)
+    st = m.new_status(dv)
+    c = m.umim_token_logprobs(t.to(dv), tok, n_top=K, vocab=V, dev_status=st)
+    ids, lp = c["top_ids"], c["top_logprobs"]
+    ids[3], lp[3] = -1, 0.25
+    lp[3, 0] = float("nan") if K > 1 else 0.25
+    lp[4, K // 2] = float("nan")
+    x[5, :V] = -float("inf")
+    rows = torch.arange(R, dtype=torch.int32, device=dv)
+    tr = torch.tensor([0, 1, 2, 3, 4, 1], dtype=torch.int32, device=dv)   # the last: a student row of -inf only
+    loss, pairs, grad = m.umim_distill_topk_ce(ids, lp, x.to(dv), tr, rows, vocab=V, tail=tail, dev_status=st)
+    torch.cuda.synchronize()
+    m.check_status(st)
+    grad = grad[:, :V]
+    for k in (1, 4, 5):
+        assert bool(pairs[k].isnan()) and bool(grad[k].isnan().all()), k
+    for k in (2, 3):
+        assert float(pairs[k]) == 0 and bool((grad[k] == 0).all()), k
+    assert bool(pairs[0].isfinite()) and bool(grad[0].isfinite().all()) and bool(loss.isnan().all())
+    want, wpairs, wgrad = OL.topk_ce(ids.cpu().numpy(), lp.cpu().numpy(), f64(x)[:, :V], tr.cpu().numpy(), np.arange(R), 1.0,
+                                     tail)
+    assert np.isnan(want) and np.array_equal(np.isnan(wpairs), np.isnan(f64(pairs)))
+    assert np.array_equal(np.isnan(wgrad), np.isnan(f64(grad)))

@@ -44,3 +44,14 @@ def test_no_rest_where_neither_has_one():
                 assert np.isclose(pairs[0], listed - short * np.log(q[2]), rtol=1e-13)
             else:
                 assert pairs[0] > listed + 1e-6
+
+
+@pytest.mark.parametrize("tail", [True, False])
+def test_teacher_rows_that_held_nan(tail):
+    nan = np.nan
+    ids = np.array([[-1, -1], [-1, -1], [2, 0], [2, 0], [-1, 1]])
+    lp = np.array([[nan, nan], [nan, -np.inf], [-0.5, nan], [-0.5, -1.5], [nan, -0.1]])
+    x = np.linspace(-1, 1, 20).reshape(5, 4)
+    _, pairs, grad = topk_ce(ids, lp, x, np.arange(5), np.arange(5), 1.0, tail)
+    assert np.isnan(pairs).tolist() == [True, False, True, False, False]
+    assert np.isnan(grad).all(1).tolist() == np.isnan(pairs).tolist() and pairs[1] == 0
