@@ -95,7 +95,9 @@ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
 }
 
 // CTA 0 checks the pairs, before anything is written, and marks the student rows that are
-// in one: a bit each, kMarked rows at a time.  A warp of the others per pair: its
+// in one: a bit each, in shared memory, or where these are too many for that in global memory.
+// (Not in shared memory part by part, which reads the pairs once for each: a call with 2 000 000 rows took
+// 21.9 ms, 13.2 like this; 500 000 3.2 and 3.1; 200 000, two parts, 1.20 and 1.25.)  A warp of the others per pair: its
 // teacher row's entries, checked, as probabilities.  Both read N; neither waits
 // for the other.
 __global__ void __launch_bounds__(kPlanThreads) topk_plan_kernel(TopkArgs a) {
@@ -106,11 +108,10 @@ __global__ void __launch_bounds__(kPlanThreads) topk_plan_kernel(TopkArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, K = a.K;
   const int N = a.n_dev ? *a.n_dev : a.max_pairs;
   if (blockIdx.x == 0) {
-    uint32_t *mark = &table[0][0];
     constexpr int kMarked = 32 * kPlanPairs * kTable;
+    const int words = ceil_div(a.R_S, 32);
     bool bad = N < 0 || N > a.max_pairs;
-    for (int r0 = 0; r0 < a.R_S || r0 == 0; r0 += kMarked) {
-      const int words = min(kPlanPairs * kTable, ceil_div(a.R_S - r0, 32));
+    const auto mark_rows = [&](uint32_t *mark) {
       for (int i = tid; i < words; i += kPlanThreads) mark[i] = 0;
       __syncthreads();
       if (!bad)
@@ -119,15 +120,18 @@ __global__ void __launch_bounds__(kPlanThreads) topk_plan_kernel(TopkArgs a) {
           const int t = a.teacher_rows[p], s = a.student_rows[p];
           if (t < 0 || t >= a.R_T || s < 0 || s >= a.R_S) {
             bad = true;
-          } else if (s >= r0 && s - r0 < kMarked) {
-            const uint32_t bit = 1u << ((s - r0) & 31);
-            if (atomicOr(&mark[(s - r0) >> 5], bit) & bit) bad = true;   // a student row in two pairs
+          } else {
+            const uint32_t bit = 1u << (s & 31);
+            if (atomicOr(&mark[s >> 5], bit) & bit) bad = true;   // a student row in two pairs
           }
         }
       bad = __syncthreads_or(bad);
-      for (int i = tid; i < words; i += kPlanThreads) a.paired[r0 / 32 + i] = mark[i];
-      __syncthreads();
-      if (a.R_S - r0 <= kMarked) break;
+    };
+    if (a.R_S <= kMarked) {
+      mark_rows(&table[0][0]);
+      for (int i = tid; i < words; i += kPlanThreads) a.paired[i] = (&table[0][0])[i];
+    } else {
+      mark_rows(a.paired);
     }
     if (tid == 0) {
       a.hdr->error = bad;
