@@ -2,7 +2,9 @@
 context of UMIM (arXiv 2609.27233).
 
 Thin argument marshalling only: every step runs in the library's CUDA
-kernels.  PyTorch provides device memory and the current stream.  The entry
+kernels.  PyTorch provides device memory and the current stream.  A call given a
+`stream` runs on that one, and makes there what the caller leaves it to make (outputs,
+a workspace); its inputs have to be ready there (stream.wait_stream).  The entry
 points keep the C names:
 
   umim_merge_spans        merge module M_phi (Sec. 3.2 Eq. 1, App. C.1)
@@ -109,9 +111,20 @@ def check_status(dev_status, where="device"):
         raise UmimError(v, where)
 
 
-def workspace(nbytes, device):
-    """A zero-filled, 256-byte aligned device workspace of at least nbytes."""
-    return torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+def _made(stream, make, *args, **kwargs):
+    """make(*args, **kwargs), a new tensor, on the stream of the call that is going to use it (None: the current
+    one): its zeros are written before the call reads them, and its memory, handed on by
+    the allocator in a stream's order, is nobody else's while the call runs."""
+    if stream is None:
+        return make(*args, **kwargs)
+    with torch.cuda.stream(stream):
+        return make(*args, **kwargs)
+
+
+def workspace(nbytes, device, stream=None):
+    """A zero-filled, 256-byte aligned device workspace of at least nbytes, made
+    on `stream` (None: the current one)."""
+    return _made(stream, torch.zeros, max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
 def _pool_fields(pool):
@@ -187,9 +200,9 @@ def umim_merge_spans(embeddings, token_ids, span_offsets, weights, surrogates=No
     S = span_offsets.numel() - 1
     T = token_ids.numel()
     if surrogates is None:
-        surrogates = torch.empty((S, d), dtype=torch.float32, device=embeddings.device)
+        surrogates = _made(stream, torch.empty, (S, d), dtype=torch.float32, device=embeddings.device)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_merge_spans_workspace_size(T, S, d), embeddings.device)
+        workspace_buf = workspace(umim_merge_spans_workspace_size(T, S, d), embeddings.device, stream)
     ptrs, rest = _weight_fields(weights)
     code = lib().umim_merge_spans(embeddings.data_ptr(), vocab, token_ids.data_ptr(), T, span_offsets.data_ptr(), S,
                                   _pack_weights(*ptrs, *rest), surrogates.data_ptr(), workspace_buf.data_ptr(),
@@ -210,13 +223,13 @@ def umim_build_compressed(embeddings, token_ids, span_offsets, span_start, span_
     vocab, d = shape[0], shape[1]
     S = span_start.numel()
     if out_embeds is None:
-        out_embeds = torch.empty((B * L, d), dtype=torch.bfloat16, device=dev)
+        out_embeds = _made(stream, torch.empty, (B * L, d), dtype=torch.bfloat16, device=dev)
     if position_ids is None:
-        position_ids = torch.empty(out_embeds.shape[0], dtype=torch.int32, device=dev)
+        position_ids = _made(stream, torch.empty, out_embeds.shape[0], dtype=torch.int32, device=dev)
     if cu_seqlens is None:
-        cu_seqlens = torch.empty(B + 1, dtype=torch.int32, device=dev)
+        cu_seqlens = _made(stream, torch.empty, B + 1, dtype=torch.int32, device=dev)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_build_compressed_workspace_size(B, S), dev)
+        workspace_buf = workspace(umim_build_compressed_workspace_size(B, S), dev, stream)
     code = lib().umim_build_compressed(_p(embeddings), vocab, d, _p(token_ids), B, L,
                                        _p(span_offsets), _p(span_start), _p(span_len), S, _p(surrogates),
                                        _p(out_embeds), out_embeds.shape[0], _p(position_ids), _p(cu_seqlens),
@@ -237,9 +250,10 @@ def umim_kv_rollback(pool, block_table, seq_lens, span_offsets, span_start, span
     B, max_pages = block_table.shape
     S = span_start.numel()
     if freed_pages is None:
-        freed_pages = torch.empty(max(1, B * max_pages), dtype=torch.int32, device=pool.device)
+        freed_pages = _made(stream, torch.empty, max(1, B * max_pages), dtype=torch.int32, device=pool.device)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_kv_rollback_workspace_size(B, S, max_pages, kv[1], kv[3], kv[5]), pool.device)
+        workspace_buf = workspace(umim_kv_rollback_workspace_size(B, S, max_pages, kv[1], kv[3], kv[5]), pool.device,
+                                  stream)
     if rope_inv_freq is None:
         code = lib().umim_kv_rollback(_pack_kv(*kv), _p(block_table), max_pages, _p(seq_lens), B,
                                       _p(span_offsets), _p(span_start), _p(span_len), S, _p(surrogate_k),
@@ -276,7 +290,7 @@ def umim_decode_append_merge(pool, block_table, seq_lens, new_k, new_v, new_page
     kv = _pack_kv(*_pool_fields(pool))
     B, max_pages = block_table.shape
     if released is None:
-        released = torch.empty(B, dtype=torch.int32, device=pool.device)
+        released = _made(stream, torch.empty, B, dtype=torch.int32, device=pool.device)
     n_rows = 0 if surrogate_k is None else surrogate_k.shape[0]
     code = lib().umim_decode_append_merge(kv, _p(block_table), max_pages, _p(seq_lens), B, _p(new_k),
                                           _p(new_v), _p(new_pages), _p(merge_k), _p(merge_row), n_rows,
@@ -293,9 +307,9 @@ def umim_decode_attention(q, pool, layer, block_table, seq_lens, scale=0.0, out=
     kv = _pool_fields(pool)
     B, Hq, D = q.shape
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(stream, torch.empty_like, q)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_decode_attention_workspace_size(B, Hq, kv[3], D), q.device)
+        workspace_buf = workspace(umim_decode_attention_workspace_size(B, Hq, kv[3], D), q.device, stream)
     code = lib().umim_decode_attention(q.data_ptr(), Hq, _pack_kv(*kv), layer, block_table.data_ptr(),
                                        block_table.shape[1], seq_lens.data_ptr(), B, float(scale), out.data_ptr(),
                                        workspace_buf.data_ptr(), workspace_buf.numel(), _p(dev_status),
@@ -328,9 +342,9 @@ def umim_decode_layer_step(q, pool, layer, block_table, seq_lens, new_k, new_v, 
         if st[0] != stride[0]:
             raise ValueError("new_k and new_v must have the same row stride")
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(stream, torch.empty_like, q)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_decode_layer_step_workspace_size(B, kv[3], D), q.device)
+        workspace_buf = workspace(umim_decode_layer_step_workspace_size(B, kv[3], D), q.device, stream)
     n_rows = 0 if surrogate_k is None else surrogate_k.shape[0]
     code = lib().umim_decode_layer_step(_p(q), Hq, _pack_kv(*kv), layer, _p(block_table), block_table.shape[1],
                                         _p(seq_lens), B, _p(new_k), _p(new_v), stride[0], _p(new_pages),
@@ -350,7 +364,7 @@ def umim_decode_attention_static(q, pool, layer, block_table, seq_lens, scale=0.
     kv = _pack_kv(*_pool_fields(pool))
     B, Hq, D = q.shape
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(stream, torch.empty_like, q)
     code = lib().umim_decode_attention_static(_p(q), Hq, kv, layer, _p(block_table),
                                               block_table.shape[1], _p(seq_lens), B, float(scale), _p(out),
                                               _p(dev_status), _stream(stream))
@@ -370,9 +384,9 @@ def umim_prefill_attention(q, k, v, cu_seqlens, scale=0.0, out=None, workspace_b
     Hkv = k.shape[1]
     B = cu_seqlens.numel() - 1
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(stream, torch.empty_like, q)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_prefill_attention_workspace_size(B, T, Hkv, D), dev)
+        workspace_buf = workspace(umim_prefill_attention_workspace_size(B, T, Hkv, D), dev, stream)
     code = lib().umim_prefill_attention(_p(q), _p(k), _p(v), T, Hq, Hkv, D, _p(cu_seqlens), B, float(scale), _p(out),
                                         _p(workspace_buf), workspace_buf.numel(), _p(dev_status), _stream(stream))
     _check(code, "umim_prefill_attention")
@@ -382,9 +396,9 @@ def umim_prefill_attention(q, k, v, cu_seqlens, scale=0.0, out=None, workspace_b
 def umim_selftest_bounded_wait(which, limit_us, device, dev_status=None, stream=None):
     """Run one of the library's bounded waits on something that never happens
     (0: an mbarrier, 1: a counter); returns (status, elapsed_ns)."""
-    flags = torch.zeros(2, dtype=torch.int32, device=device)
-    elapsed = torch.zeros(1, dtype=torch.int64, device=device)
-    status = new_status(device) if dev_status is None else dev_status
+    flags = _made(stream, torch.zeros, 2, dtype=torch.int32, device=device)
+    elapsed = _made(stream, torch.zeros, 1, dtype=torch.int64, device=device)
+    status = _made(stream, new_status, device) if dev_status is None else dev_status
     code = lib().umim_selftest_bounded_wait(int(which), int(limit_us), _p(flags), _p(elapsed), _p(status),
                                             _stream(stream))
     _check(code, "umim_selftest_bounded_wait")
@@ -404,7 +418,7 @@ def umim_debug_site_name(code):
 def umim_selftest_bounds_check(buf, index, dev_status=None, stream=None):
     """Debug build only: store 1 into buf[index] (buf a device int32 tensor)
     through the kernels' access-site check; returns the status tensor."""
-    status = new_status(buf.device) if dev_status is None else dev_status
+    status = _made(stream, new_status, buf.device) if dev_status is None else dev_status
     code = lib().umim_selftest_bounds_check(_p(buf), int(buf.numel()), int(index), _p(status), _stream(stream))
     _check(code, "umim_selftest_bounds_check")
     return status
@@ -420,7 +434,7 @@ def umim_rules_build(rule_tokens, table=None, dev_status=None, stream=None):
     R = rule_tokens.shape[0]
     nbytes = umim_rule_table_bytes(R)
     if table is None:
-        table = torch.empty(nbytes, dtype=torch.uint8, device=rule_tokens.device)
+        table = _made(stream, torch.empty, nbytes, dtype=torch.uint8, device=rule_tokens.device)
     code = lib().umim_rules_build(_p(table), table.numel(), _p(rule_tokens), R, _p(dev_status), _stream(stream))
     _check(code, "umim_rules_build")
     return table
@@ -440,13 +454,13 @@ def umim_match_prompts(table, token_ids, prompt_lens=None, merge_inputs=False, o
     dev = _dev(token_ids)
     B, L = token_ids.shape
     cap = max(1, B * (L // 2))
-    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=dev)
+    i32 = lambda n: _made(stream, torch.empty, n, dtype=torch.int32, device=dev)
     if out is None:
         out = dict(span_offsets=i32(B + 1), span_start=i32(cap), span_len=i32(cap), span_rule=i32(cap),
                    merge_token_ids=i32(max(1, B * L)) if merge_inputs else None,
                    merge_offsets=i32(cap + 1) if merge_inputs else None)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_match_prompts_workspace_size(B, L), dev)
+        workspace_buf = workspace(umim_match_prompts_workspace_size(B, L), dev, stream)
     code = lib().umim_match_prompts(_p(table), table.numel(), _p(token_ids), B, L, _p(prompt_lens),
                                     _p(out["span_offsets"]), _p(out["span_start"]), _p(out["span_len"]),
                                     _p(out["span_rule"]), _p(out["merge_token_ids"]), _p(out["merge_offsets"]),
@@ -466,12 +480,12 @@ def umim_match_suffix(table, state, new_tokens, merge_k=None, merge_rule=None, m
     Returns (merge_k, merge_rule, merge_row, rows_rule, n_merges)."""
     dev = _dev(new_tokens)
     B = new_tokens.shape[0]
-    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=dev)
+    i32 = lambda n: _made(stream, torch.empty, n, dtype=torch.int32, device=dev)
     merge_k = i32(B) if merge_k is None else merge_k
     merge_rule = i32(B) if merge_rule is None else merge_rule
     merge_row = i32(B) if merge_row is None else merge_row
     if rows_rule is None:   # entries past n_merges are not written
-        rows_rule = torch.full((max(1, B),), -1, dtype=torch.int32, device=dev)
+        rows_rule = _made(stream, torch.full, (max(1, B),), -1, dtype=torch.int32, device=dev)
     n_merges = i32(1) if n_merges is None else n_merges
     code = lib().umim_match_suffix(_p(table), table.numel(), _p(state), _p(new_tokens), B, _p(merge_k),
                                    _p(merge_rule), _p(merge_row), _p(rows_rule), _p(n_merges), _p(dev_status),
@@ -486,7 +500,7 @@ def umim_lookup_surrogates(lut, rule_ids, n_dev=None, out=None, dev_status=None,
     R, d = lut.shape
     n_max = rule_ids.shape[0]
     if out is None:
-        out = torch.zeros((max(1, n_max), d), dtype=torch.float32, device=lut.device)
+        out = _made(stream, torch.zeros, (max(1, n_max), d), dtype=torch.float32, device=lut.device)
     code = lib().umim_lookup_surrogates(_p(lut), R, d, _p(rule_ids), n_max, _p(n_dev), _p(out), _p(dev_status),
                                         _stream(stream))
     _check(code, "umim_lookup_surrogates")
@@ -505,12 +519,12 @@ def umim_distill_align(seq_lens, span_offsets, span_start, span_len, capacity, o
     dev = _dev(seq_lens)
     B = seq_lens.numel()
     S = span_start.numel()
-    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=dev)
+    i32 = lambda n: _made(stream, torch.empty, n, dtype=torch.int32, device=dev)
     if out is None:
         out = dict(pair_offsets=i32(B + 1), teacher_rows=i32(max(1, capacity)),
                    student_rows=i32(max(1, capacity)), student_cu=i32(B + 1))
     if workspace_buf is None:
-        workspace_buf = workspace(umim_distill_align_workspace_size(B, S), dev)
+        workspace_buf = workspace(umim_distill_align_workspace_size(B, S), dev, stream)
     code = lib().umim_distill_align(_p(seq_lens), B, _p(span_offsets), _p(span_start), _p(span_len), S,
                                     _p(out["pair_offsets"]), _p(out["teacher_rows"]), _p(out["student_rows"]),
                                     int(capacity), _p(out.get("student_cu")), _p(workspace_buf),
@@ -540,13 +554,13 @@ def umim_distill_soft_ce(teacher_logits, student_logits, teacher_rows, student_r
     V = ld if vocab is None else int(vocab)
     P = teacher_rows.numel()
     if loss is None:
-        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        loss = _made(stream, torch.empty, 1, dtype=torch.float32, device=dev)
     if pair_loss is None:
-        pair_loss = torch.empty(max(1, P), dtype=torch.float32, device=dev)
+        pair_loss = _made(stream, torch.empty, max(1, P), dtype=torch.float32, device=dev)
     if with_grad and grad is None:
-        grad = torch.empty_like(student_logits)
+        grad = _made(stream, torch.empty_like, student_logits)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_distill_soft_ce_workspace_size(R_S, P), dev)
+        workspace_buf = workspace(umim_distill_soft_ce_workspace_size(R_S, P), dev, stream)
     code = lib().umim_distill_soft_ce(_p(teacher_logits), R_T, _p(student_logits), R_S, V, ld, _p(teacher_rows),
                                       _p(student_rows), P, _p(n_pairs), float(eps), _p(loss), _p(pair_loss),
                                       _p(grad if with_grad else None), _p(workspace_buf), workspace_buf.numel(),
@@ -577,10 +591,11 @@ def _logit_rows(logits, vocab, what="logits"):
     return logits.data_ptr(), _DTYPE[logits.dtype], shape[0], vocab, ld
 
 
-def _grad_rows(grad, logits, dtype, R, V, ld):
+def _grad_rows(grad, logits, dtype, R, V, ld, stream):
     """(grad, its address): a gradient like logits, checked or made."""
     if grad is None:
-        grad = torch.empty_strided((R, logits.shape[1]), (ld, 1), dtype=logits.dtype, device=logits.device)
+        grad = _made(stream, torch.empty_strided, (R, logits.shape[1]), (ld, 1), dtype=logits.dtype,
+                     device=logits.device)
         return grad, grad.data_ptr()
     ptr, g_dtype, g_R, _, g_ld = _logit_rows(grad, V, "grad")
     if g_dtype != dtype or g_R != R or g_ld != ld:
@@ -607,6 +622,9 @@ def umim_token_logprobs(logits, token_ids=None, n_top=0, vocab=None, temperature
     [R], stats fp32 [R][2] (the row's maximum m, and ln sum exp((x - m) /
     temperature)), top_ids int32 and top_logprobs fp32 [R][n_top]; logprobs is
     None without tokens, the last two are None where n_top is 0."""
+    if stream is not None and out is None:
+        with torch.cuda.stream(stream):   # as _made does it, once for all outputs
+            return umim_token_logprobs(logits, token_ids, n_top, vocab, temperature, n_rows, None, dev_status)
     x, dtype, R, V, ld = _logit_rows(logits, vocab)
     if n_top < 0:
         raise ValueError("n_top must not be negative")
@@ -641,7 +659,7 @@ def umim_token_logprobs_grad(logits, stats, token_ids=None, grad_logprobs=None, 
     stride; logits itself for a gradient in place) is returned; columns past
     vocab are not written."""
     x, dtype, R, V, ld = _logit_rows(logits, vocab)
-    grad, g_ptr = _grad_rows(grad, logits, dtype, R, V, ld)
+    grad, g_ptr = _grad_rows(grad, logits, dtype, R, V, ld, stream)
     code = lib().umim_token_logprobs_grad(
         x, dtype, R, V, ld, _vector(n_rows, 1, torch.int32, "n_rows"), _vector(token_ids, R, torch.int32, "token_ids"),
         float(temperature), _vector(stats, 2 * R, torch.float32, "stats"),
@@ -673,14 +691,14 @@ def umim_distill_topk_ce(top_ids, top_logprobs, student_logits, teacher_rows, st
     R_T, K = top_ids.shape
     P = teacher_rows.numel()
     if loss is None:
-        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        loss = _made(stream, torch.empty, 1, dtype=torch.float32, device=dev)
     if pair_loss is None:
-        pair_loss = torch.empty(max(1, P), dtype=torch.float32, device=dev)
+        pair_loss = _made(stream, torch.empty, max(1, P), dtype=torch.float32, device=dev)
     g_ptr = None
     if with_grad:
-        grad, g_ptr = _grad_rows(grad, student_logits, dtype, R_S, V, ld)
+        grad, g_ptr = _grad_rows(grad, student_logits, dtype, R_S, V, ld, stream)
     if workspace_buf is None:
-        workspace_buf = workspace(umim_distill_topk_ce_workspace_size(R_S, P), dev)
+        workspace_buf = workspace(umim_distill_topk_ce_workspace_size(R_S, P), dev, stream)
     code = lib().umim_distill_topk_ce(
         _vector(top_ids, R_T * K, torch.int32, "top_ids"),
         _vector(top_logprobs, R_T * K, torch.float32, "top_logprobs"),
