@@ -185,9 +185,7 @@ struct Running {
 // 32 vectors after the other.  A warp takes eight strips of it side by side, a lane one vector
 // of each: every logit is read once, by 16-byte loads, a warp's eight together while
 // the others work on theirs.  (SPREAD: every eighth strip, so that all threads
-// have some of a part that is no whole chunk; the search below wants them.  For 16384 rows of
-// 8000 bf16 with 128 alternatives 269 us instead of 1608, but 178 instead of
-// 176 for 4096 rows of 128256 with 64.)
+// have some of a part that is no whole chunk; spread_pays has when.)
 // (Half as many a chunk ahead of their use took 186 us where this takes 179, for
 // 4096 rows of 128256 bf16 with 64 alternatives; asynchronous copies into buffers
 // of the warp's own 4 % longer than those.)
@@ -879,11 +877,23 @@ umim_status launch_logprobs(LogprobArgs a, int C, cudaStream_t stream) {
   return e == cudaSuccess ? UMIM_OK : UMIM_ERR_CUDA;
 }
 
+// Whether to spread a part over all warps.  Side by side, its first warps have eight strips each and the
+// others nothing: that is less to do where few warps are busy, but only the busy ones' threads make groups, and the search
+// needs half as many groups again as alternatives, or its threshold is the part's lowest element.  Past
+// half a chunk the warps' unequal shares cost more.  Measured spread / side by side, us, bf16: 32768 rows of 2000 with 5, 20
+// and 64 alternatives 421 / 337, 443 / 372 and 506 / 1698; 8192 of 8000 with 20, 64 and 128: 99.7 / 95.0, 118 / 119 and 137 / 698;
+// 5461 of 12000 with 5 and 20: 64.0 / 66.1 and 66.9 / 69.7; 4096 of 16000, nearly a chunk, with 64: 61.1 / 60.7.
+template <class E>
+bool spread_pays(int slice, int n_top) {
+  const int busy = ceil_div(slice, chunk_elems<E>() / kWarps);
+  return slice < chunk_elems<E>() && (2 * slice > chunk_elems<E>() || 3 * n_top > 2 * 32 * busy);
+}
+
 template <class E>
 umim_status launch_type(const LogprobArgs &a, int C, cudaStream_t stream) {
   if (a.n_top == 0) return launch_logprobs<E, false, false>(a, C, stream);
-  return a.slice < chunk_elems<E>() ? launch_logprobs<E, true, true>(a, C, stream)
-                                    : launch_logprobs<E, true, false>(a, C, stream);
+  return spread_pays<E>(a.slice, a.n_top) ? launch_logprobs<E, true, true>(a, C, stream)
+                                          : launch_logprobs<E, true, false>(a, C, stream);
 }
 
 // CTAs per row: rows are divided while that leaves at most three CTAs to an SM, or two with
