@@ -222,17 +222,6 @@ __device__ __forceinline__ uint4 pack(const float (&f)[E::VEC]) {
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
 }
 
-// The elements of the vector at element e of a row; none at or past V is read, they come out as `fill`.
-template <class E>
-__device__ __forceinline__ void load_vec(const typename E::T *row, int e, int V, float fill, float (&f)[E::VEC]) {
-  if (e + E::VEC <= V) {
-    unpack<E>(*reinterpret_cast<const uint4 *>(row + e), f);
-  } else {
-#pragma unroll
-    for (int j = 0; j < E::VEC; ++j) f[j] = e + j < V ? E::to_float(row[e + j]) : fill;
-  }
-}
-
 // Store the elements of a vector at element e of a row that are below V.
 template <class E>
 __device__ __forceinline__ void store_vec(typename E::T *row, int e, int V, const float (&f)[E::VEC]) {
