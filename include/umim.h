@@ -625,9 +625,11 @@ umim_status umim_distill_soft_ce(const void *teacher_logits, int32_t n_teacher_r
  *     order, equal ones in ascending order of their id, and their log
  *     probabilities.  A logit of -inf is no alternative: entries past a row's
  *     last one hold -1 and -inf.
- * Computed in fp32 whatever the logits' type; each logit is read once.  Where one
- * token has nearly all of the probability, its log probability and the entropy are
- * exact to their own, small size.
+ * Computed in fp32 whatever the logits' type, in one pass over each row; what is
+ * read a second time are the segments of 32 logits that hold the alternatives,
+ * 1/256 of a row that has one certain token, and rows whose logits times
+ * log2(e) / T pass 2^24.  Where one token has nearly all of the probability, its
+ * log probability and the entropy are exact to their own, small size.
  * A row whose token is -1 is left out: its logits are not read, logprobs,
  * entropy and stats are 0, its alternatives -1 and -inf.  A row of -inf only
  * has logprob -inf, entropy 0 and stats (-inf, 0); a row that holds NaN or

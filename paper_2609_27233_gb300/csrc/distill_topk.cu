@@ -254,7 +254,8 @@ struct __align__(16) Part {
 // student's row, and each warp on one of eight contiguous stretches of that,
 // which stays in shared memory between the two passes over it: every logit is
 // read once and every gradient element written once, and what bounds the kernel is
-// that traffic (8700 pairs of 128256 bf16 with 9600 rows: 746 us, 6.3 TB/s).  A warp
+// that traffic (8700 pairs of 128256 bf16 with 9600 rows: 739 us, 6.35 TB/s; without the
+// gradient 2870 pairs take 144 us, 5.1 TB/s, with it 262 of 3260 rows).  A warp
 // loads its stretch of the next pair's row, by an asynchronous copy, as soon as it has
 // written this one's gradient.  Once a pair every warp tells all CTAs of the
 // cluster its sums, by asynchronous stores that count on a barrier in each of
@@ -262,7 +263,7 @@ struct __align__(16) Part {
 // before everybody has read what it held.  Three CTAs of up to 64 KB to an SM load,
 // sum and write in turn.
 //
-// Measured for 2870 pairs, against the 261 us of this: a CTA for every row, with the
+// Measured for 2870 pairs of 3260 rows, against 261 us like this: a CTA for every row, with the
 // same parts, which starts and loads anew each time, 316; with parts of
 // half the size 358; a cluster barrier a pair, which waits for the
 // gradient's stores too, 467.
@@ -641,7 +642,7 @@ size_t part_bytes(int V, int C, int esize) {
 
 // CTAs per row: as many as it takes for three parts to fit an SM, or two where no cluster is large enough
 // for that; and for few rows more, while that leaves an SM to each and a part is still worth a CTA
-// (2048 elements).  Measured for 57 rows of 32000 bf16: 11.5 us by two CTAs a row, 14.2 by four
+// (2048 elements).  Measured for 57 rows of 32000 bf16: 11.1 us by two CTAs a row, 14.2 by four
 // and eight; for 1500 of 151936 bf16: 160 by five, 166 by six, 201 by eight, three parts fitting
 // in each case; for 700 of 151936 fp32: 155 by six, two parts fitting as by seven, 172, and eight, 164.
 int cluster_for(int R, int V, int esize, int num_sms) {
@@ -720,7 +721,7 @@ umim_status launch_topk_ce(TopkArgs a, cudaStream_t stream, int num_sms) {
   // Where a cluster has few pairs it starts while the plan is being made: 18.7 us instead of 21.7 for 108
   // pairs of 128256 bf16, 31.5 instead of 34.5 for 220, 27.5 instead of 30.0 for 456 of 50257.  Where it
   // has many it must not: some clusters find their SMs taken by the plan, come late and end last, 56.2
-  // instead of 54.5 for 448 pairs of 128256, 301 instead of 245 for 2870.
+  // instead of 54.5 for 448 pairs of 128256, 301 instead of 245 for 2870 of as many rows.
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;

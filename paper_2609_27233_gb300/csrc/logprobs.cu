@@ -186,9 +186,9 @@ struct Running {
 // of each: every logit is read once, by 16-byte loads, a warp's eight together while
 // the others work on theirs.  (SPREAD: every eighth strip, so that all threads
 // have some of a part that is no whole chunk; spread_pays has when.)
-// (Half as many a chunk ahead of their use took 186 us where this takes 179, for
-// 4096 rows of 128256 bf16 with 64 alternatives; asynchronous copies into buffers
-// of the warp's own 4 % longer than those.)
+// (Half as many a chunk ahead of their use took 4 % longer for 4096 rows of 128256
+// bf16 with 64 alternatives, asynchronous copies into buffers of the warp's own another
+// 4 %.)
 //
 // The alternatives need no second pass over the row.  Beside the sums, the
 // maximum of every segment of 32 consecutive elements goes to shared memory.
@@ -208,7 +208,8 @@ struct Running {
 // What bounds it: without alternatives the one read of the logits (4096 rows of 128256
 // bf16: 149 us, 7.0 TB/s, above the measured copy's rate); with them the
 // instructions as well, 5.8 a logit for the pass and 1.4 (one alternative) to 2.8
-// (128) for segments and search: 166 us with 20, 177 with 64, 186 with 128.
+// (128) for segments and search: 166 us with 20, 176 with 64, 186 with 128.  Rows that take the bisections cost four
+// times that: 749 us with 64 alternatives where all but 12 side by side are masked by the type's lowest value.
 //
 // All of it happens in shared memory and registers of the cluster: no
 // workspace, no atomics on global memory, the same bits in every call.
@@ -220,9 +221,9 @@ __host__ __device__ constexpr int chunk_elems() {   // of a CTA's chunk
 }
 
 // While a CTA searches it reads nothing, so before that it has the beginning of the row that a CTA in
-// its place is likely to take next brought into L2 (179.8 -> 176.1 us for 4096 rows of 128256
-// bf16 with 64 alternatives, 48.7 -> 46.8 for 2000 rows of 50257; with 16 KB 177.7 and 46.3, with
-// 64 KB 174.9 and 50.2).
+// its place is likely to take next brought into L2 (2.1 % less time for 4096 rows of 128256 bf16
+// with 64 alternatives, 3.9 % for 2000 rows of 50257; with 16 KB 1.2 and 4.9 %, with 64 KB 2.7 % less
+// and 3.1 % more).
 constexpr int kAheadBytes = 32768;
 constexpr int kCands = kThreads;     // candidates that are ranked, at most
 constexpr int kListed = 2 * kThreads; // segments that reach the threshold, at most (else the exact way)
@@ -628,10 +629,10 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
   // Where one element has nearly all of the probability, ln s and the entropy are as small as what the others
   // add to its 1, and a sum that holds the 1 has rounded that away.  (Equal largest ones make s 2 or more.)
   // So they are summed alone: every warp but that element's has, its other lanes have too, and its
-  // own lane's elements are read again, by the whole warp.  The entropy of such rows was off by up to 7e-7 before,
-  // 5e-8 now, and in proportion where it is smaller.  Rows like these cost 1.5 us each: 177 us instead of
-  // 174 for 4096 random rows of 128256 bf16 with 64 alternatives, 66 instead of 63 for 4104 of 32000 with
-  // 20, 9.6 instead of 8.0 for 32 of 128256.
+  // own lane's elements are read again, by the whole warp.  (Summed with the 1, the entropy of such rows was off by
+  // up to 7e-7, so it is 5e-8, and in proportion where it is smaller.)  A row like this costs its CTA about 1.5 us.  Where
+  // every row is one, for random rows and for those, us: 4096 of 128256 bf16 with 64 alternatives 176 and 193, 8192 without
+  // 288 and 307, 4104 of 32000 with 20 66 and 74, 16384 of 8000 with 128 271 and 296, 128 of 128256 with 5 14.3 and 14.7.
   const bool peaked = !bad && !empty && all.s < kPeaked;   // the same in all of a row's threads
   float rest = 0.f;
   if (peaked) {
@@ -897,9 +898,9 @@ umim_status launch_type(const LogprobArgs &a, int C, cudaStream_t stream) {
 }
 
 // CTAs per row: rows are divided while that leaves at most three CTAs to an SM, or two with
-// alternatives, whose exchange costs each of them more, and a part is still worth one
-// (2048 elements).  Measured for 152 rows of 128256 bf16 with 20 alternatives: 14.2 us by two
-// CTAs a row, 20.1 by four; for 200 rows of 32000: 7.5 by one, 10.0 by two; without
+// alternatives, and a part is still worth one (2048 elements).  Measured for 152 rows of 128256 bf16 with 20
+// alternatives: 14.2 us by two CTAs a row, 20.1 by four, which are all the places that the SMs have, so that some
+// clusters may wait for others; for 200 rows of 32000: 7.5 by one, 10.0 by two; without
 // alternatives, 200 rows of 128256: 14.5 by two, 16.2 by one.
 int cluster_for(int R, int V, int n_top, int num_sms) {
   int C = 1;
