@@ -29,6 +29,7 @@ struct LogprobArgs {
   const int32_t *n_dev;
   const int32_t *tokens;     // nullptr: no token, every row counts
   float inv_t, c;            // 1 / T, log2(e) / T
+  float inv_low, c_low;      // what is left of 1 / T, and of c, relative to it, past their fp32 values
   int32_t n_top, slice;      // slice: elements of a row per CTA
   int32_t ahead;             // rows between one and that whose beginning its CTA brings into L2, or 0
   float *logprobs, *entropy;
@@ -685,10 +686,17 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
     all.s = 1.f + rest;
   }
 
-  const float m0 = empty ? 0.f : all.m, l = bad ? NAN : empty ? 0.f : peaked ? log1pf(rest) : logf(all.s);
+  // The sums were taken with c, off by c_low of itself: ln s by c_low times the mean of (x - m) / T, to first order.  (The
+  // entropy's two parts are off alike.)  And log probabilities are rounded once: x - m, then both parts of 1 / T by FMA.
+  const float mean = kLn2 * (all.w / all.s), l0 = peaked ? log1pf(rest) : logf(all.s);
+  const float m0 = empty ? 0.f : all.m, l = bad ? NAN : empty ? 0.f : fmaf(a.c_low, mean, l0);
+  const auto log_prob = [&](float x) {
+    const float d = x - m0;
+    return d == -INFINITY ? d : fmaf(d, a.inv_t, fmaf(d, a.inv_low, -l));
+  };
   if (writes) {
-    if (a.logprobs) a.logprobs[r] = bad ? NAN : (x_t - m0) * a.inv_t - l;
-    if (a.entropy) a.entropy[r] = bad ? NAN : empty ? 0.f : l - kLn2 * (all.w / all.s);
+    if (a.logprobs) a.logprobs[r] = bad ? NAN : log_prob(x_t);
+    if (a.entropy) a.entropy[r] = bad ? NAN : empty ? 0.f : l0 - mean;
     if (a.stats) a.stats[r] = bad ? make_float2(NAN, NAN) : make_float2(all.m, l);
   }
 
@@ -777,7 +785,7 @@ __global__ void __launch_bounds__(kThreads, 4) token_logprobs_kernel(LogprobArgs
     }
     if (mine != 0 && place < n && in_bounds(place, n, a.status, kSiteLogprobRank)) {
       a.top_ids[(int64_t)r * n + place] = (int)id_of(mine);
-      a.top_logprobs[(int64_t)r * n + place] = (E::to_float(E::from_key(key_of(mine))) - m0) * a.inv_t - l;
+      a.top_logprobs[(int64_t)r * n + place] = log_prob(E::to_float(E::from_key(key_of(mine))));
     }
     if (tid >= M && tid < n) {
       a.top_ids[(int64_t)r * n + tid] = -1;
@@ -917,8 +925,10 @@ umim_status token_logprobs(const void *logits, int dtype, int R, int V, int64_t 
   const int C = cluster_for(R, V, n_top, num_sms);
   const int slice = ceil_div(ceil_div(V, C), kSegment) * kSegment;
   const int ahead = C == 1 ? 4 * num_sms : 0;   // as many CTAs run at once
-  const LogprobArgs a{logits, R, V, ld, n_dev, tokens, 1.f / temperature, kLog2e / temperature, n_top, slice, ahead,
-                      logprobs, entropy, reinterpret_cast<float2 *>(stats), top_ids, top_logprobs, dev_status};
+  const double inv = 1.0 / (double)temperature, c = 1.4426950408889634 * inv;
+  const LogprobArgs a{logits, R, V, ld, n_dev, tokens, (float)inv, (float)c, (float)(inv - (float)inv),
+                      (float)(c / (float)c - 1.0), n_top, slice, ahead, logprobs, entropy,
+                      reinterpret_cast<float2 *>(stats), top_ids, top_logprobs, dev_status};
   return dtype == UMIM_DTYPE_BF16   ? launch_type<ElemBf16>(a, C, stream)
          : dtype == UMIM_DTYPE_FP16 ? launch_type<ElemFp16>(a, C, stream)
                                     : launch_type<ElemFp32>(a, C, stream);
