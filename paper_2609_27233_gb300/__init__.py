@@ -111,13 +111,19 @@ def check_status(dev_status, where="device"):
         raise UmimError(v, where)
 
 
+def _current(stream):
+    """A context in which `stream` is the current one: a torch stream, or any object with its handle as cuda_stream."""
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream)
+                             else torch.cuda.ExternalStream(stream.cuda_stream))
+
+
 def _made(stream, make, *args, **kwargs):
     """make(*args, **kwargs), a new tensor, on the stream of the call that is going to use it (None: the current
     one): its zeros are written before the call reads them, and its memory, handed on by
     the allocator in a stream's order, is nobody else's while the call runs."""
     if stream is None:
         return make(*args, **kwargs)
-    with torch.cuda.stream(stream):
+    with _current(stream):
         return make(*args, **kwargs)
 
 
@@ -623,7 +629,7 @@ def umim_token_logprobs(logits, token_ids=None, n_top=0, vocab=None, temperature
     temperature)), top_ids int32 and top_logprobs fp32 [R][n_top]; logprobs is
     None without tokens, the last two are None where n_top is 0."""
     if stream is not None and out is None:
-        with torch.cuda.stream(stream):   # as _made does it, once for all outputs
+        with _current(stream):   # as _made does it, once for all outputs
             return umim_token_logprobs(logits, token_ids, n_top, vocab, temperature, n_rows, None, dev_status)
     x, dtype, R, V, ld = _logit_rows(logits, vocab)
     if n_top < 0:

@@ -1,6 +1,8 @@
 """A call given a stream makes its outputs and its workspace on that stream: the zeros of a workspace made on another one
 could be written while the call runs, and memory that the allocator hands on in another stream's
 order could still be in use there.  (Which stream each tensor is made on is asked of the binding; no race is run.)"""
+import types
+
 import numpy as np
 import pytest
 import torch
@@ -68,7 +70,8 @@ def test_what_a_call_makes_is_made_on_its_stream(made):
     m, dv = umim(), dev()
     side = torch.cuda.Stream()
     here = torch.cuda.current_stream().cuda_stream
-    for stream, handle in ((side, side.cuda_stream), (None, here)):
+    bare = types.SimpleNamespace(cuda_stream=side.cuda_stream)   # another library's stream: its handle is enough
+    for stream, handle in ((side, side.cuda_stream), (bare, side.cuda_stream), (None, here)):
         todo = calls(m, dv)        # inputs of their own for each, ready before the call
         torch.cuda.synchronize()
         for name, call in todo.items():
