@@ -311,8 +311,9 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
       e[j] = j * 32 + lane < K ? a.lists[(int64_t)q * K + j * 32 + lane] : Entry{-1, 0.f};
     head = a.heads[q];
   };
+  bool failed = false;   // a wait gave up: this thread starts nothing more that would land later, and waits for nothing
   const auto copy = [&](int s) {   // the stretch of student row s
-    if (lane == 0) {
+    if (lane == 0 && !failed) {
       mbar_arrive_expect_tx(landed, (uint32_t)whole_vecs * 16u);
       if (whole_vecs > 0) bulk_load(part, row_of(s) + beg, (uint32_t)whole_vecs * 16u, landed);
       if (whole_vecs < vecs) cut = load_raw<E>(row_of(s), beg + whole_vecs * E::VEC, V);
@@ -331,11 +332,11 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
   fence_mbar_init();
   __syncwarp();
   if (s_row >= 0) copy(s_row);
-  bool failed = false;
   const auto wait = [&](uint64_t *bar, uint32_t parity) {
     if (!failed && !mbar_wait_sleep(bar, parity)) {
       failed = true;
       set_error(a.status, UMIM_ERR_TIMEOUT);
+      mbar_wait_sleep(bar, parity);   // once more, for what may be on its way
     }
   };
   griddep_wait();
@@ -468,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
     const int turn = count & 1;
     const Part *parts = s_parts[turn];
     if (C > 1) {
-      if (lane < C) {
+      if (lane < C && !failed) {
         const uint32_t to = peer_addr(&s_parts[turn][rank * kWarps + warp], (uint32_t)lane);
         const uint32_t bar = peer_addr(&s_told[turn], (uint32_t)lane);
         st_async16(to, make_float4(mine.m, mine.mr, mine.rest, mine.top), bar);
@@ -476,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 3) topk_ce_kernel(TopkArgs a) {
       }
       __syncwarp();
       wait(&s_told[turn], (uint32_t)(count >> 1) & 1u);
-      if (tid == 0) mbar_arrive_expect_tx(&s_told[turn], told_bytes);   // for the pair after the next
+      if (tid == 0 && !failed) mbar_arrive_expect_tx(&s_told[turn], told_bytes);   // for the pair after the next
     } else {
       if (lane == 0) s_parts[turn][warp] = mine;
       __syncthreads();
