@@ -210,7 +210,7 @@ struct Running {
 // bf16: 149 us, 7.0 TB/s, above the measured copy's rate); with them the
 // instructions as well, 5.8 a logit for the pass and 1.4 (one alternative) to 2.8
 // (128) for segments and search: 166 us with 20, 176 with 64, 186 with 128.  Rows that take the bisections cost four
-// times that: 749 us with 64 alternatives where all but 12 side by side are masked by the type's lowest value.
+// times that: 751 us with 64 alternatives where all but 12 are masked by the type's lowest value (327 of it the pass).
 //
 // All of it happens in shared memory and registers of the cluster: no
 // workspace, no atomics on global memory, the same bits in every call.
