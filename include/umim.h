@@ -108,6 +108,26 @@ typedef struct umim_paged_kv {
   int32_t head_dim;   /* 64 or 128                                     */
 } umim_paged_kv;
 
+/* A paged 8-bit KV cache: the pages of umim_paged_kv with e4m3 values, and
+ * one e8m0 scale (the code e + 127 of a power of two 2^e) for each row of
+ * head_dim values: entry = value * 2^e.
+ *     values  [n_layers][n_pages][2 (K, V)][n_kv_heads][16][head_dim]
+ *     scales  [n_layers][n_pages][2 (K, V)][n_kv_heads][16]
+ * A row x is stored as e4m3(x / 2^e), rounded to nearest with ties to even, e
+ * the smallest whole number with max |x| <= 448 * 2^e over the row's finite
+ * values, kept within [-100, 120] (0 for a row without any but zeros).  NaN
+ * and infinities are stored as NaN.  A stored value is off by at most 2^-4 of
+ * itself, or by 2^-10 * 2^e where it is below 2^-6 * 2^e. */
+typedef struct umim_paged_kv8 {
+  void *values;       /* device, 16-B aligned                          */
+  void *scales;       /* device, 16-B aligned                          */
+  int32_t n_layers;
+  int32_t n_pages;    /* physical pages per layer                      */
+  int32_t n_kv_heads;
+  int32_t page_size;  /* must be UMIM_PAGE_SIZE                         */
+  int32_t head_dim;   /* 64 or 128                                     */
+} umim_paged_kv8;
+
 /* ------------------------------------------------------------------------
  * Merge module forward (Sec. 3.2 Eq. 1; App. C.1 full form):
  *   P   = LN_kv(GELU(E_s W_kv^T + b_kv)),  P = [P_1 .. P_h]
@@ -391,6 +411,128 @@ umim_status umim_decode_attention(const void *q, int32_t n_q_heads, const umim_p
                                   const int32_t *block_table, int32_t max_pages, const int32_t *seq_lens,
                                   int32_t batch, float scale, void *out, void *workspace,
                                   size_t workspace_bytes, int32_t *dev_status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The 8-bit cache, written and read back (the paper keeps its cache in 16
+ * bits; this is a capacity and bandwidth option beside it: an entry takes
+ * 2 * n_kv_heads * (head_dim + 1) bytes in place of 4 * n_kv_heads * head_dim).
+ *
+ * umim_kv8_write quantises rows of K and V into one layer's pages: sequence b
+ * owns rows cu_rows[b] .. cu_rows[b+1]-1 and its i-th row becomes entry
+ * start[b] + i; with cu_rows NULL there is one row a sequence (n_rows ==
+ * batch).  umim_kv8_read writes the same rows' values, value * 2^e, as bf16
+ * (exact for every scale that a write makes).  Block tables and lengths are
+ * the caller's: neither is changed.
+ *
+ * kv, layer    cache and the layer
+ * block_table  device int32 [batch][max_pages]
+ * start        device int32 [batch]
+ * cu_rows      device int32 [batch + 1], cu_rows[0] = 0, nondecreasing,
+ *              cu_rows[batch] <= n_rows, or NULL.  Rows behind
+ *              cu_rows[batch] are neither read nor written
+ * k, v         device bf16, 16-B aligned: row r at k + r * row_stride elements,
+ *              n_kv_heads * head_dim values; row_stride 0 means n_kv_heads *
+ *              head_dim, otherwise a multiple of 8 not below it (rows inside
+ *              a fused QKV projection output)
+ * n_rows       rows of k and v, at most 2^24
+ * No workspace.  Device-side errors: UMIM_ERR_INVALID_ARG, and the row is left
+ * out (nothing of it written), for an entry outside [0, 16*max_pages) or in a
+ * block-table entry outside [0, n_pages); UMIM_ERR_INVALID_ARG for offsets
+ * that break the rules above (rows that then lie in no sequence are left out).
+ * Not checked: that two rows have two places.
+ * ------------------------------------------------------------------------ */
+umim_status umim_kv8_write(const umim_paged_kv8 *kv, int32_t layer, const int32_t *block_table, int32_t max_pages,
+                           const int32_t *start, const int32_t *cu_rows, int32_t batch, const void *k, const void *v,
+                           int64_t row_stride, int32_t n_rows, int32_t *dev_status, cudaStream_t stream);
+
+umim_status umim_kv8_read(const umim_paged_kv8 *kv, int32_t layer, const int32_t *block_table, int32_t max_pages,
+                          const int32_t *start, const int32_t *cu_rows, int32_t batch, void *k, void *v,
+                          int64_t row_stride, int32_t n_rows, int32_t *dev_status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * umim_decode_append_merge for the 8-bit cache (App. E "Decoding-Time Merging
+ * and KV-Cache Update"): the same arguments, decisions, released pages and
+ * device-side errors, the new or surrogate rows (bf16, 16-B aligned)
+ * quantised as they are written.  merge_k NULL: append only.
+ * ------------------------------------------------------------------------ */
+umim_status umim_kv8_append_merge(const umim_paged_kv8 *kv, int32_t *block_table, int32_t max_pages,
+                                  int32_t *seq_lens, int32_t batch, const void *new_k, const void *new_v,
+                                  const int32_t *new_pages, const int32_t *merge_k, const int32_t *merge_row,
+                                  int32_t n_merge_rows, const void *surrogate_k, const void *surrogate_v,
+                                  int32_t *released_pages, int32_t *dev_status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * umim_decode_attention over the 8-bit cache: K and V are value * 2^e, the
+ * sums and the softmax fp32.
+ *
+ * q             device bf16 [batch][n_q_heads][head_dim], 8-B aligned
+ * out           device bf16 [batch][n_q_heads][head_dim]
+ * workspace     device, umim_decode_attention_kv8_workspace_size() bytes, 256-B
+ *               aligned; calls sharing one must not overlap on the GPU
+ * batch * max_pages * n_kv_heads may be 2^30 at most (UMIM_ERR_UNSUPPORTED).
+ * Device-side errors are those of umim_decode_attention (a page outside
+ * [0, n_pages) reads as zeros).
+ * ------------------------------------------------------------------------ */
+size_t umim_decode_attention_kv8_workspace_size(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                                int32_t head_dim);
+
+umim_status umim_decode_attention_kv8(const void *q, int32_t n_q_heads, const umim_paged_kv8 *kv, int32_t layer,
+                                      const int32_t *block_table, int32_t max_pages, const int32_t *seq_lens,
+                                      int32_t batch, float scale, void *out, void *workspace,
+                                      size_t workspace_bytes, int32_t *dev_status, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Decode attention of sequences that share prefixes (many continuations of
+ * one compressed prompt; App. I.1's decode attention otherwise): a prefix's
+ * pages are in the cache once and are read once for the sequences that share
+ * it.  Sequences prefix_offsets[i] .. prefix_offsets[i+1]-1 attend to the
+ * prefix_lens[i] entries of prefix i and to their own:
+ *   out[b][h] = sum_j softmax_j(scale <q[b][h], K_j[g]>) V_j[g],
+ *   j over the entries of b's prefix, then the seq_lens[b] entries of b.
+ * Either may be empty; a sequence of no prefix has its own entries only, and
+ * one without any entry a zero output.  The result is umim_decode_attention's
+ * over tables that hold the prefix's pages first, but for rounding, and prefix
+ * lengths need not be multiples of 16.
+ *
+ * q               device bf16 [batch][n_q_heads][head_dim], 8-B aligned
+ * prefix_table    device int32 [n_prefixes][max_prefix_pages]
+ * prefix_lens     device int32 [n_prefixes]
+ * prefix_offsets  device int32 [n_prefixes + 1], nondecreasing in [0, batch],
+ *                 or NULL with n_prefixes == 1: every sequence
+ * block_table     device int32 [batch][max_pages]: own entries (entry t of a
+ *                 sequence, t = 0 behind the prefix, in page t / 16)
+ * seq_lens        device int32 [batch]: own entries
+ * out             device bf16 [batch][n_q_heads][head_dim]
+ * workspace       device, umim_decode_attention_shared_workspace_size() bytes
+ *                 (the same for both caches), 256-B aligned; calls sharing one
+ *                 must not overlap on the GPU
+ * UMIM_ERR_UNSUPPORTED: batch > 4096, n_prefixes > 512, page visits
+ * n_kv_heads * (batch * max_pages + (n_prefixes + batch * n_q_heads /
+ * n_kv_heads / 16) * max_prefix_pages) above 2^30, and the shapes that
+ * umim_decode_attention does not support.  Device-side errors:
+ * UMIM_ERR_INVALID_ARG for a length outside its table (it counts as 0), an
+ * offset that decreases (it counts as the largest before it) or leaves
+ * [0, batch] (as 0), and a used page outside [0, n_pages) (it reads as
+ * zeros); UMIM_ERR_TIMEOUT for a stalled copy.
+ * ------------------------------------------------------------------------ */
+size_t umim_decode_attention_shared_workspace_size(int32_t batch, int32_t n_prefixes, int32_t n_q_heads,
+                                                   int32_t n_kv_heads, int32_t head_dim);
+
+umim_status umim_decode_attention_shared(const void *q, int32_t n_q_heads, const umim_paged_kv *kv, int32_t layer,
+                                         const int32_t *prefix_table, int32_t max_prefix_pages,
+                                         const int32_t *prefix_lens, const int32_t *prefix_offsets,
+                                         int32_t n_prefixes, const int32_t *block_table, int32_t max_pages,
+                                         const int32_t *seq_lens, int32_t batch, float scale, void *out,
+                                         void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                         cudaStream_t stream);
+
+umim_status umim_decode_attention_shared_kv8(const void *q, int32_t n_q_heads, const umim_paged_kv8 *kv,
+                                             int32_t layer, const int32_t *prefix_table, int32_t max_prefix_pages,
+                                             const int32_t *prefix_lens, const int32_t *prefix_offsets,
+                                             int32_t n_prefixes, const int32_t *block_table, int32_t max_pages,
+                                             const int32_t *seq_lens, int32_t batch, float scale, void *out,
+                                             void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                             cudaStream_t stream);
 
 /* ------------------------------------------------------------------------
  * Prefill attention over packed compressed prompts (App. E "Prompt

@@ -43,6 +43,10 @@ for indices and moved KV bytes:
                           log probabilities, entropy and alternatives of rows
                           of logits, their gradient, and App. F's loss from
                           the teacher's top log probabilities
+  kv8.quantise / append_merge / attend
+                          the 8-bit cache (this library's own format): rows
+                          quantised, a decode step's update on it, and
+                          attention over shared prefixes
 
 bf16 values are represented by their raw bit patterns (numpy uint16) and
 upcast exactly to float64.
@@ -69,8 +73,11 @@ Parity status per function (what pins it is in tests/test_oracle_*.py):
   token_logprobs, its gradient, topk_ce
                     pinned (library log-softmax and sort, autograd, the full
                     soft cross-entropy when every id is listed)
+  kv8               pinned (the library's e4m3 cast, closed forms and the
+                    rounding bounds; the 16-bit cache's append and rollback;
+                    decode_attention over joined tables)
 """
-from . import bf16, spans, merge, rollback, append, attention, compaction, rules, prefill, distill, logprobs  # noqa: F401
+from . import bf16, spans, merge, rollback, append, attention, compaction, rules, prefill, distill, logprobs, kv8  # noqa: F401
 from .merge import merge_spans, merge_span_reference_steps  # noqa: F401
 from .rollback import kv_rollback  # noqa: F401
 from .append import kv_append  # noqa: F401

@@ -15,6 +15,11 @@ points keep the C names:
   umim_decode_attention   GQA decode attention over the compacted paged cache (App. I.1)
   umim_decode_layer_step  one layer of a decode step: its new or surrogate entry written and
                           attention over the updated cache in one launch (App. E, App. I.1)
+  umim_kv8_write, umim_kv8_read, umim_kv8_append_merge, umim_decode_attention_kv8
+                          the paged cache in 8 bits (Kv8Pool): rows quantised as they are written,
+                          read back, a decode step's entries with merges, and attention over it
+  umim_decode_attention_shared, umim_decode_attention_shared_kv8
+                          decode attention of sequences that share prefixes, each read once
   umim_prefill_attention  causal GQA attention over the packed compressed prompts (App. E, App. C.5)
   umim_rules_build, umim_match_prompts, umim_match_suffix, umim_lookup_surrogates
                           merge-rule table, longest-first span selection for prompts
@@ -142,13 +147,43 @@ def _pool_fields(pool):
     return pool.data_ptr(), layers, pages, heads, page_size, head_dim
 
 
+class Kv8Pool:
+    """An 8-bit paged cache: values torch.float8_e4m3fn [layers][pages][2][Hkv][16][D] and scales
+    torch.float8_e8m0fnu [layers][pages][2][Hkv][16], an entry's value times its row's scale.  It holds the two
+    tensors and copies nothing."""
+    __slots__ = ("values", "scales", "layers", "pages", "heads", "head_dim", "device", "_c")
+
+    def __init__(self, values, scales):
+        shape = values.shape
+        if values.dtype != torch.float8_e4m3fn or len(shape) != 6 or shape[2] != 2 or not values.is_contiguous():
+            raise ValueError("values must be contiguous float8_e4m3fn [layers][pages][2][Hkv][16][D]")
+        if scales.dtype != torch.float8_e8m0fnu or scales.shape != shape[:5] or not scales.is_contiguous():
+            raise ValueError("scales must be contiguous float8_e8m0fnu [layers][pages][2][Hkv][16]")
+        _on_gpu(values)
+        if scales.device != values.device:
+            raise ValueError("values and scales must be on one device")
+        self.values, self.scales, self.device = values, scales, values.device
+        self.layers, self.pages, _, self.heads, page_size, self.head_dim = shape
+        self._c = _pack_kv8(values.data_ptr(), scales.data_ptr(), self.layers, self.pages, self.heads, page_size,
+                            self.head_dim)
+
+    @classmethod
+    def zeros(cls, layers, pages, heads, head_dim, device, stream=None):
+        """A cache of zeros (scales 1)."""
+        shape = (layers, pages, 2, heads, PAGE_SIZE)
+        values = _made(stream, torch.zeros, shape + (head_dim,), dtype=torch.uint8, device=device)
+        scales = _made(stream, torch.full, shape, 127, dtype=torch.uint8, device=device)
+        return cls(values.view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu))
+
+
 def paged_kv(pool):
     """umim_paged_kv for a bf16 pool shaped [layers][pages][2][Hkv][16][D]."""
     return PagedKVC(*_pool_fields(pool))
 
 
-# the layouts of umim_paged_kv and umim_merge_weights (native alignment)
+# the layouts of umim_paged_kv, umim_paged_kv8 and umim_merge_weights (native alignment)
 _pack_kv = struct.Struct("@P5i4x").pack
+_pack_kv8 = struct.Struct("@2P5i4x").pack
 _pack_weights = struct.Struct("@9P2if4x").pack
 _WEIGHTS = ("w_kv", "b_kv", "ln_kv_gamma", "ln_kv_beta", "query", "w_o", "b_o", "ln_o_gamma", "ln_o_beta")
 
@@ -376,6 +411,176 @@ def umim_decode_attention_static(q, pool, layer, block_table, seq_lens, scale=0.
                                               _p(dev_status), _stream(stream))
     _check(code, "umim_decode_attention_static")
     return out
+
+
+# ---------------------------------------------------------------------------
+# the 8-bit cache, and decode attention over it and over shared prefixes
+# ---------------------------------------------------------------------------
+def _ints(t, shape, what):
+    """The address of a contiguous device int32 tensor of the given shape, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what} must be a contiguous CUDA int32 tensor of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _table(t, what):
+    """(address, rows, columns) of a block table."""
+    if t.dim() != 2:
+        raise ValueError(f"{what} must be [rows][pages]")
+    rows, cols = t.shape
+    return _ints(t, (rows, cols), what), rows, cols
+
+
+def _kv_rows(t, n, heads, head_dim, what):
+    """(address, row stride) of bf16 rows [n][heads][head_dim], which may be strided."""
+    if t.dtype != torch.bfloat16 or t.shape != (n, heads, head_dim) or not t.is_cuda:
+        raise ValueError(f"{what} must be CUDA bf16 [{n}][{heads}][{head_dim}]")
+    st = t.stride()
+    if st[2] != 1 or (st[1] != head_dim and heads > 1):
+        raise ValueError(f"the heads of a row of {what} must be contiguous")
+    if n > 1 and st[0] < heads * head_dim:
+        raise ValueError(f"the rows of {what} overlap")
+    return t.data_ptr(), (st[0] if n > 1 else 0)
+
+
+def _whole(t, shape, what):
+    """The address of a contiguous bf16 device tensor of the given shape, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.bfloat16 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what} must be a contiguous CUDA bf16 tensor of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _query(q, heads, head_dim):
+    """(address, batch, query heads) of q [B][Hq][D]."""
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != head_dim:
+        raise ValueError(f"q must be [batch][query heads][{head_dim}]")
+    return _whole(q, shape, "q"), shape[0], shape[1]
+
+
+def umim_kv8_write(pool, layer, block_table, start, k, v, cu_rows=None, dev_status=None, stream=None):
+    """Quantise rows k / v bf16 [T][Hkv][D] (rows may be strided, both alike) into one layer of a Kv8Pool:
+    rows cu_rows[b] .. cu_rows[b+1]-1 (int32 [B+1]; None: row b) become entries start[b], start[b] + 1, ... of
+    sequence b."""
+    table, B, cols = _table(block_table, "block_table")
+    T = k.shape[0]
+    pk, stride = _kv_rows(k, T, pool.heads, pool.head_dim, "k")
+    pv, stride_v = _kv_rows(v, T, pool.heads, pool.head_dim, "v")
+    if stride != stride_v:
+        raise ValueError("k and v must have the same row stride")
+    code = lib().umim_kv8_write(pool._c, layer, table, cols, _ints(start, (B,), "start"),
+                                _ints(cu_rows, (B + 1,), "cu_rows"), B, pk, pv, stride, T, _p(dev_status),
+                                _stream(stream))
+    _check(code, "umim_kv8_write")
+
+
+def umim_kv8_read(pool, layer, block_table, start, n_rows, cu_rows=None, out=None, dev_status=None, stream=None):
+    """(k, v) bf16 [n_rows][Hkv][D]: the rows that umim_kv8_write would write, value times scale.  out: a pair of
+    such tensors (rows may be strided, both alike); rows of no sequence are left as they are."""
+    table, B, cols = _table(block_table, "block_table")
+    if out is None:
+        make = lambda: _made(stream, torch.empty, (n_rows, pool.heads, pool.head_dim), dtype=torch.bfloat16,
+                             device=pool.device)
+        out = make(), make()
+    k, v = out
+    pk, stride = _kv_rows(k, n_rows, pool.heads, pool.head_dim, "k")
+    pv, stride_v = _kv_rows(v, n_rows, pool.heads, pool.head_dim, "v")
+    if stride != stride_v:
+        raise ValueError("k and v must have the same row stride")
+    code = lib().umim_kv8_read(pool._c, layer, table, cols, _ints(start, (B,), "start"),
+                               _ints(cu_rows, (B + 1,), "cu_rows"), B, pk, pv, stride, n_rows, _p(dev_status),
+                               _stream(stream))
+    _check(code, "umim_kv8_read")
+    return k, v
+
+
+def umim_kv8_append_merge(pool, block_table, seq_lens, new_k, new_v, new_pages=None, merge_k=None, merge_row=None,
+                          surrogate_k=None, surrogate_v=None, released=None, dev_status=None, stream=None):
+    """umim_decode_append_merge for a Kv8Pool: the new (or surrogate) rows, bf16, quantised as they are
+    written.  Returns released [B] int32."""
+    table, B, cols = _table(block_table, "block_table")
+    row = (pool.layers, pool.heads, pool.head_dim)
+    if released is None:
+        released = _made(stream, torch.empty, B, dtype=torch.int32, device=pool.device)
+    n_rows = 0 if surrogate_k is None else surrogate_k.shape[0]
+    code = lib().umim_kv8_append_merge(
+        pool._c, table, cols, _ints(seq_lens, (B,), "seq_lens"), B, _whole(new_k, (B,) + row, "new_k"),
+        _whole(new_v, (B,) + row, "new_v"), _ints(new_pages, (B,), "new_pages"), _ints(merge_k, (B,), "merge_k"),
+        _ints(merge_row, (B,), "merge_row"), n_rows, _whole(surrogate_k, (n_rows,) + row, "surrogate_k"),
+        _whole(surrogate_v, (n_rows,) + row, "surrogate_v"), _ints(released, (B,), "released"), _p(dev_status),
+        _stream(stream))
+    _check(code, "umim_kv8_append_merge")
+    return released
+
+
+def umim_decode_attention_kv8_workspace_size(batch, n_q_heads, n_kv_heads, head_dim):
+    return int(lib().umim_decode_attention_kv8_workspace_size(batch, n_q_heads, n_kv_heads, head_dim))
+
+
+def umim_decode_attention_kv8(q, pool, layer, block_table, seq_lens, scale=0.0, out=None, workspace_buf=None,
+                              dev_status=None, stream=None):
+    """out [B][Hq][D] bf16 = GQA attention of q over a Kv8Pool."""
+    pq, B, Hq = _query(q, pool.heads, pool.head_dim)
+    table, rows, cols = _table(block_table, "block_table")
+    if rows != B:
+        raise ValueError("block_table must have a row for every sequence")
+    if out is None:
+        out = _made(stream, torch.empty_like, q)
+    if workspace_buf is None:
+        workspace_buf = workspace(umim_decode_attention_kv8_workspace_size(B, Hq, pool.heads, pool.head_dim), q.device,
+                                  stream)
+    code = lib().umim_decode_attention_kv8(pq, Hq, pool._c, layer, table, cols, _ints(seq_lens, (B,), "seq_lens"), B,
+                                           float(scale), _whole(out, q.shape, "out"), workspace_buf.data_ptr(),
+                                           workspace_buf.numel(), _p(dev_status), _stream(stream))
+    _check(code, "umim_decode_attention_kv8")
+    return out
+
+
+def umim_decode_attention_shared_workspace_size(batch, n_prefixes, n_q_heads, n_kv_heads, head_dim):
+    return int(lib().umim_decode_attention_shared_workspace_size(batch, n_prefixes, n_q_heads, n_kv_heads, head_dim))
+
+
+def _shared(call, q, cache, heads, head_dim, layer, prefix_table, prefix_lens, block_table, seq_lens, prefix_offsets,
+            scale, out, workspace_buf, dev_status, stream):
+    pq, B, Hq = _query(q, heads, head_dim)
+    prefixes, n, prefix_cols = _table(prefix_table, "prefix_table")
+    table, rows, cols = _table(block_table, "block_table")
+    if rows != B:
+        raise ValueError("block_table must have a row for every sequence")
+    if out is None:
+        out = _made(stream, torch.empty_like, q)
+    if workspace_buf is None:
+        workspace_buf = workspace(umim_decode_attention_shared_workspace_size(B, n, Hq, heads, head_dim), q.device,
+                                  stream)
+    code = getattr(lib(), call)(
+        pq, Hq, cache, layer, prefixes, prefix_cols, _ints(prefix_lens, (n,), "prefix_lens"),
+        _ints(prefix_offsets, (n + 1,), "prefix_offsets"), n, table, cols, _ints(seq_lens, (B,), "seq_lens"), B,
+        float(scale), _whole(out, q.shape, "out"), workspace_buf.data_ptr(), workspace_buf.numel(), _p(dev_status),
+        _stream(stream))
+    _check(code, call)
+    return out
+
+
+def umim_decode_attention_shared(q, pool, layer, prefix_table, prefix_lens, block_table, seq_lens, prefix_offsets=None,
+                                 scale=0.0, out=None, workspace_buf=None, dev_status=None, stream=None):
+    """out [B][Hq][D] bf16 = GQA attention of q over a prefix's entries and the sequence's own: sequences
+    prefix_offsets[i] .. prefix_offsets[i+1]-1 (int32 [n+1]; None: all, of one prefix) share the prefix_lens[i]
+    entries in the pages of prefix_table[i] (int32 [n][pages])."""
+    kv = _pool_fields(pool)
+    return _shared("umim_decode_attention_shared", q, _pack_kv(*kv), kv[3], kv[5], layer, prefix_table, prefix_lens,
+                   block_table, seq_lens, prefix_offsets, scale, out, workspace_buf, dev_status, stream)
+
+
+def umim_decode_attention_shared_kv8(q, pool, layer, prefix_table, prefix_lens, block_table, seq_lens,
+                                     prefix_offsets=None, scale=0.0, out=None, workspace_buf=None, dev_status=None,
+                                     stream=None):
+    """umim_decode_attention_shared over a Kv8Pool."""
+    return _shared("umim_decode_attention_shared_kv8", q, pool._c, pool.heads, pool.head_dim, layer, prefix_table,
+                   prefix_lens, block_table, seq_lens, prefix_offsets, scale, out, workspace_buf, dev_status, stream)
 
 
 # ---------------------------------------------------------------------------

@@ -31,6 +31,13 @@ class PagedKVC(ctypes.Structure):
     ]
 
 
+class PagedKV8C(ctypes.Structure):
+    _fields_ = [
+        ("values", c_ptr), ("scales", c_ptr), ("n_layers", c_i32), ("n_pages", c_i32), ("n_kv_heads", c_i32),
+        ("page_size", c_i32), ("head_dim", c_i32),
+    ]
+
+
 # name -> (restype, argtypes), exactly as declared in include/umim.h; a pointer
 # to a host struct is a c_void_p here, which takes byref(struct) as well as the
 # packed bytes of one (the binding packs them: a fraction of a ctypes struct's cost)
@@ -90,6 +97,22 @@ SIGNATURES = {
                                              c_ptr]),
     "umim_decode_attention_static": (ctypes.c_int, [c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_i32,
                                                     c_ptr, c_i32, ctypes.c_float, c_ptr, c_ptr, c_ptr]),
+    "umim_kv8_write": (ctypes.c_int, [c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_ptr, c_i32, c_ptr, c_ptr, c_i64, c_i32,
+                                      c_ptr, c_ptr]),
+    "umim_kv8_read": (ctypes.c_int, [c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_ptr, c_i32, c_ptr, c_ptr, c_i64, c_i32,
+                                     c_ptr, c_ptr]),
+    "umim_kv8_append_merge": (ctypes.c_int, [c_ptr, c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_ptr,
+                                             c_ptr, c_ptr, c_ptr, c_i32, c_ptr, c_ptr, c_ptr, c_ptr, c_ptr]),
+    "umim_decode_attention_kv8_workspace_size": (c_size, [c_i32, c_i32, c_i32, c_i32]),
+    "umim_decode_attention_kv8": (ctypes.c_int, [c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_i32,
+                                                 ctypes.c_float, c_ptr, c_ptr, c_size, c_ptr, c_ptr]),
+    "umim_decode_attention_shared_workspace_size": (c_size, [c_i32, c_i32, c_i32, c_i32, c_i32]),
+    "umim_decode_attention_shared": (ctypes.c_int, [c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_ptr, c_i32,
+                                                    c_ptr, c_i32, c_ptr, c_i32, ctypes.c_float, c_ptr, c_ptr, c_size,
+                                                    c_ptr, c_ptr]),
+    "umim_decode_attention_shared_kv8": (ctypes.c_int, [c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_i32, c_ptr, c_ptr, c_i32,
+                                                        c_ptr, c_i32, c_ptr, c_i32, ctypes.c_float, c_ptr, c_ptr,
+                                                        c_size, c_ptr, c_ptr]),
     "umim_debug_build": (ctypes.c_int, []),
     "umim_debug_site_name": (ctypes.c_char_p, [c_i32]),
     "umim_selftest_bounds_check": (ctypes.c_int, [c_ptr, c_i64, c_i64, c_ptr, c_ptr]),

@@ -86,6 +86,19 @@ umim_status decode_layer_step(const void *, int, const umim_paged_kv *, int, int
 size_t decode_attention_workspace_bytes(int B, int Hq, int Hkv, int D, int num_sms);
 umim_status decode_attention(const void *, int, const umim_paged_kv *, int, const int32_t *, int, const int32_t *,
                              int, float, void *, void *, int32_t *, cudaStream_t, int);
+umim_status kv8_rows(bool, const umim_paged_kv8 *, int, const int32_t *, int, const int32_t *, const int32_t *, int,
+                     void *, void *, int, int64_t, int32_t *, cudaStream_t, int);
+umim_status kv8_append_merge(const umim_paged_kv8 *, int32_t *, int32_t, int32_t *, int32_t, const void *, const void *,
+                             const int32_t *, const int32_t *, const int32_t *, int32_t, const void *, const void *,
+                             int32_t *, int32_t *, cudaStream_t);
+size_t decode_attention_kv8_workspace_bytes(int B, int Hkv, int D, int num_sms);
+umim_status decode_attention_kv8(const void *, int, const umim_paged_kv8 *, int, const int32_t *, int, const int32_t *,
+                                 int, float, void *, void *, int32_t *, cudaStream_t, int);
+bool decode_attention_shared_supported(int B, int n_prefixes);
+size_t decode_attention_shared_workspace_bytes(int B, int n_prefixes, int Hq, int Hkv, int D, int num_sms);
+umim_status decode_attention_shared(const void *, int, void *, void *, int, int, int, int, int, const int32_t *, int,
+                                    const int32_t *, const int32_t *, int, const int32_t *, int, const int32_t *, int,
+                                    float, void *, void *, int32_t *, cudaStream_t, int);
 
 namespace {
 
@@ -113,6 +126,27 @@ bool kv_ok(const umim_paged_kv *kv) {
 
 bool kv_supported(const umim_paged_kv *kv) {
   return kv->page_size == UMIM_PAGE_SIZE && (kv->head_dim == 64 || kv->head_dim == 128) && kv->n_kv_heads <= 64;
+}
+
+bool kv8_ok(const umim_paged_kv8 *kv) {
+  return kv && kv->values && kv->scales && kv->n_layers > 0 && kv->n_pages > 0 && kv->n_kv_heads > 0 &&
+         aligned(kv->values, 16) && aligned(kv->scales, 16);
+}
+
+bool kv8_supported(const umim_paged_kv8 *kv) {
+  return kv->page_size == UMIM_PAGE_SIZE && (kv->head_dim == 64 || kv->head_dim == 128) && kv->n_kv_heads <= 64;
+}
+
+bool heads_supported(int32_t n_q_heads, int32_t n_kv_heads) {
+  return n_q_heads % n_kv_heads == 0 && n_q_heads / n_kv_heads <= 16;
+}
+
+constexpr int64_t kMaxPageVisits = int64_t(1) << 30;   // (segment, page) pairs are counted in 32 bits
+constexpr int32_t kMaxKv8Rows = 1 << 24;
+
+int sms_or_largest() {
+  const int sms = current_sms();
+  return sms > 0 ? sms : 256;   // no device yet: size for the largest grid this library launches
 }
 
 // rows of logits: each starts on a 16-byte vector
@@ -419,6 +453,10 @@ const char *umim_debug_site_name(int32_t status) {
       "distill_topk.entry",
       "logprobs.segment",
       "logprobs.rank",
+      "kv8.dst",
+      "kv8.src",
+      "attention_pages.block_table",
+      "attention_pages.piece",
   };
   const int site = (status >> 8) & 0xffffff;
   return site < kSiteCount ? names[site] : "";
@@ -599,6 +637,149 @@ umim_status umim_decode_attention(const void *q, int32_t n_q_heads, const umim_p
   int32_t *status = dev_status;
   return decode_attention(q, n_q_heads, kv, layer, block_table, max_pages, seq_lens, batch, scale, out, workspace,
                           status, stream, sms);
+}
+
+namespace {
+umim_status kv8_rows_checked(bool write, const umim_paged_kv8 *kv, int32_t layer, const int32_t *block_table,
+                             int32_t max_pages, const int32_t *start, const int32_t *cu_rows, int32_t batch, void *k,
+                             void *v, int64_t row_stride, int32_t n_rows, int32_t *dev_status, cudaStream_t stream) {
+  if (!kv8_ok(kv) || batch < 0 || max_pages < 0 || n_rows < 0 || row_stride < 0) return UMIM_ERR_INVALID_ARG;
+  if (!kv8_supported(kv)) return UMIM_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= kv->n_layers) return UMIM_ERR_INVALID_ARG;
+  if (!cu_rows && n_rows != batch) return UMIM_ERR_INVALID_ARG;
+  if ((int64_t)batch * max_pages > INT32_MAX / 16 || n_rows > kMaxKv8Rows) return UMIM_ERR_UNSUPPORTED;
+  const int64_t row = (int64_t)kv->n_kv_heads * kv->head_dim;
+  if (row_stride == 0) row_stride = row;
+  if (row_stride < row || row_stride % 8 != 0) return UMIM_ERR_INVALID_ARG;
+  if (batch == 0 || n_rows == 0) return UMIM_OK;
+  if (!block_table || !start || !k || !v || !aligned(k, 16) || !aligned(v, 16)) return UMIM_ERR_INVALID_ARG;
+  const DeviceScope scope(stream);
+  return kv8_rows(write, kv, layer, block_table, max_pages, start, cu_rows, batch, k, v, n_rows, row_stride, dev_status,
+                  stream, scope.sms());
+}
+
+umim_status shared_checked(const void *q, int32_t n_q_heads, void *values, void *scales, int32_t n_layers,
+                           int32_t n_pages, int32_t n_kv_heads, int32_t head_dim, int32_t layer,
+                           const int32_t *prefix_table, int32_t max_prefix_pages, const int32_t *prefix_lens,
+                           const int32_t *prefix_offsets, int32_t n_prefixes, const int32_t *block_table,
+                           int32_t max_pages, const int32_t *seq_lens, int32_t batch, float scale, void *out,
+                           void *workspace, size_t workspace_bytes, int32_t *dev_status, cudaStream_t stream) {
+  if (batch < 0 || max_pages < 0 || max_prefix_pages < 0 || n_prefixes < 1 || n_q_heads <= 0) return UMIM_ERR_INVALID_ARG;
+  if (!heads_supported(n_q_heads, n_kv_heads) || !decode_attention_shared_supported(batch, n_prefixes))
+    return UMIM_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= n_layers || (!prefix_offsets && n_prefixes != 1)) return UMIM_ERR_INVALID_ARG;
+  const int64_t blocks = n_prefixes + (int64_t)batch * (n_q_heads / n_kv_heads) / 16;
+  if ((int64_t)batch * max_pages > kMaxPageVisits / n_kv_heads || blocks * max_prefix_pages > kMaxPageVisits ||
+      n_kv_heads * ((int64_t)batch * max_pages + blocks * max_prefix_pages) > kMaxPageVisits)
+    return UMIM_ERR_UNSUPPORTED;
+  if (batch == 0) return UMIM_OK;
+  if (!q || !prefix_table || !prefix_lens || !block_table || !seq_lens || !out) return UMIM_ERR_INVALID_ARG;
+  if (!aligned(q, 8) || !aligned(out, 2)) return UMIM_ERR_INVALID_ARG;
+  const DeviceScope scope(stream);
+  const int sms = scope.sms();
+  if (!workspace || !aligned(workspace, 256) ||
+      workspace_bytes < decode_attention_shared_workspace_bytes(batch, n_prefixes, n_q_heads, n_kv_heads, head_dim, sms))
+    return UMIM_ERR_WORKSPACE;
+  if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)head_dim);
+  return decode_attention_shared(q, n_q_heads, values, scales, n_layers, n_pages, n_kv_heads, head_dim, layer,
+                                 prefix_table, max_prefix_pages, prefix_lens, prefix_offsets, n_prefixes, block_table,
+                                 max_pages, seq_lens, batch, scale, out, workspace, dev_status, stream, sms);
+}
+}  // namespace
+
+umim_status umim_kv8_write(const umim_paged_kv8 *kv, int32_t layer, const int32_t *block_table, int32_t max_pages,
+                           const int32_t *start, const int32_t *cu_rows, int32_t batch, const void *k, const void *v,
+                           int64_t row_stride, int32_t n_rows, int32_t *dev_status, cudaStream_t stream) {
+  return kv8_rows_checked(true, kv, layer, block_table, max_pages, start, cu_rows, batch, const_cast<void *>(k),
+                          const_cast<void *>(v), row_stride, n_rows, dev_status, stream);
+}
+
+umim_status umim_kv8_read(const umim_paged_kv8 *kv, int32_t layer, const int32_t *block_table, int32_t max_pages,
+                          const int32_t *start, const int32_t *cu_rows, int32_t batch, void *k, void *v,
+                          int64_t row_stride, int32_t n_rows, int32_t *dev_status, cudaStream_t stream) {
+  return kv8_rows_checked(false, kv, layer, block_table, max_pages, start, cu_rows, batch, k, v, row_stride, n_rows,
+                          dev_status, stream);
+}
+
+umim_status umim_kv8_append_merge(const umim_paged_kv8 *kv, int32_t *block_table, int32_t max_pages,
+                                  int32_t *seq_lens, int32_t batch, const void *new_k, const void *new_v,
+                                  const int32_t *new_pages, const int32_t *merge_k, const int32_t *merge_row,
+                                  int32_t n_merge_rows, const void *surrogate_k, const void *surrogate_v,
+                                  int32_t *released_pages, int32_t *dev_status, cudaStream_t stream) {
+  if (!kv8_ok(kv) || batch < 0 || max_pages < 0 || n_merge_rows < 0) return UMIM_ERR_INVALID_ARG;
+  if (!kv8_supported(kv)) return UMIM_ERR_UNSUPPORTED;
+  if ((int64_t)batch * max_pages > INT32_MAX / 16) return UMIM_ERR_UNSUPPORTED;
+  if (batch == 0) return UMIM_OK;
+  if (!block_table || !seq_lens || !new_k || !new_v) return UMIM_ERR_INVALID_ARG;
+  if (!aligned(new_k, 16) || !aligned(new_v, 16)) return UMIM_ERR_INVALID_ARG;
+  if (merge_k && n_merge_rows > 0 && (!merge_row || !surrogate_k || !surrogate_v)) return UMIM_ERR_INVALID_ARG;
+  if (n_merge_rows > 0 && (!aligned(surrogate_k, 16) || !aligned(surrogate_v, 16))) return UMIM_ERR_INVALID_ARG;
+  const DeviceScope scope(stream);
+  return kv8_append_merge(kv, block_table, max_pages, seq_lens, batch, new_k, new_v, new_pages, merge_k, merge_row,
+                          n_merge_rows, surrogate_k, surrogate_v, released_pages, dev_status, stream);
+}
+
+size_t umim_decode_attention_kv8_workspace_size(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                                int32_t head_dim) {
+  if (batch < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || (head_dim != 64 && head_dim != 128)) return 0;
+  return decode_attention_kv8_workspace_bytes(batch, n_kv_heads, head_dim, sms_or_largest());
+}
+
+umim_status umim_decode_attention_kv8(const void *q, int32_t n_q_heads, const umim_paged_kv8 *kv, int32_t layer,
+                                      const int32_t *block_table, int32_t max_pages, const int32_t *seq_lens,
+                                      int32_t batch, float scale, void *out, void *workspace,
+                                      size_t workspace_bytes, int32_t *dev_status, cudaStream_t stream) {
+  if (!kv8_ok(kv) || batch < 0 || max_pages < 0 || n_q_heads <= 0) return UMIM_ERR_INVALID_ARG;
+  if (!kv8_supported(kv) || !heads_supported(n_q_heads, kv->n_kv_heads)) return UMIM_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= kv->n_layers) return UMIM_ERR_INVALID_ARG;
+  if ((int64_t)batch * kv->n_kv_heads > (int64_t)1 << 24 ||
+      (int64_t)batch * max_pages > kMaxPageVisits / kv->n_kv_heads)
+    return UMIM_ERR_UNSUPPORTED;
+  if (batch == 0) return UMIM_OK;
+  if (!q || !block_table || !seq_lens || !out) return UMIM_ERR_INVALID_ARG;
+  if (!aligned(q, 8) || !aligned(out, 2)) return UMIM_ERR_INVALID_ARG;
+  const DeviceScope scope(stream);
+  const int sms = scope.sms();
+  if (!workspace || !aligned(workspace, 256) ||
+      workspace_bytes < decode_attention_kv8_workspace_bytes(batch, kv->n_kv_heads, kv->head_dim, sms))
+    return UMIM_ERR_WORKSPACE;
+  if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)kv->head_dim);
+  return decode_attention_kv8(q, n_q_heads, kv, layer, block_table, max_pages, seq_lens, batch, scale, out, workspace,
+                              dev_status, stream, sms);
+}
+
+size_t umim_decode_attention_shared_workspace_size(int32_t batch, int32_t n_prefixes, int32_t n_q_heads,
+                                                   int32_t n_kv_heads, int32_t head_dim) {
+  if (batch < 0 || n_prefixes < 1 || n_q_heads <= 0 || n_kv_heads <= 0 || (head_dim != 64 && head_dim != 128)) return 0;
+  return decode_attention_shared_workspace_bytes(batch, n_prefixes, n_q_heads, n_kv_heads, head_dim, sms_or_largest());
+}
+
+umim_status umim_decode_attention_shared(const void *q, int32_t n_q_heads, const umim_paged_kv *kv, int32_t layer,
+                                         const int32_t *prefix_table, int32_t max_prefix_pages,
+                                         const int32_t *prefix_lens, const int32_t *prefix_offsets,
+                                         int32_t n_prefixes, const int32_t *block_table, int32_t max_pages,
+                                         const int32_t *seq_lens, int32_t batch, float scale, void *out,
+                                         void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                         cudaStream_t stream) {
+  if (!kv_ok(kv)) return UMIM_ERR_INVALID_ARG;
+  if (!kv_supported(kv)) return UMIM_ERR_UNSUPPORTED;
+  return shared_checked(q, n_q_heads, kv->base, nullptr, kv->n_layers, kv->n_pages, kv->n_kv_heads, kv->head_dim, layer,
+                        prefix_table, max_prefix_pages, prefix_lens, prefix_offsets, n_prefixes, block_table, max_pages,
+                        seq_lens, batch, scale, out, workspace, workspace_bytes, dev_status, stream);
+}
+
+umim_status umim_decode_attention_shared_kv8(const void *q, int32_t n_q_heads, const umim_paged_kv8 *kv,
+                                             int32_t layer, const int32_t *prefix_table, int32_t max_prefix_pages,
+                                             const int32_t *prefix_lens, const int32_t *prefix_offsets,
+                                             int32_t n_prefixes, const int32_t *block_table, int32_t max_pages,
+                                             const int32_t *seq_lens, int32_t batch, float scale, void *out,
+                                             void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                             cudaStream_t stream) {
+  if (!kv8_ok(kv)) return UMIM_ERR_INVALID_ARG;
+  if (!kv8_supported(kv)) return UMIM_ERR_UNSUPPORTED;
+  return shared_checked(q, n_q_heads, kv->values, kv->scales, kv->n_layers, kv->n_pages, kv->n_kv_heads, kv->head_dim,
+                        layer, prefix_table, max_prefix_pages, prefix_lens, prefix_offsets, n_prefixes, block_table,
+                        max_pages, seq_lens, batch, scale, out, workspace, workspace_bytes, dev_status, stream);
 }
 
 size_t umim_decode_layer_step_workspace_size(int32_t batch, int32_t n_kv_heads, int32_t head_dim) {

@@ -1,0 +1,893 @@
+// Decode attention over the 8-bit cache, and of groups of sequences that share
+// a prefix (16- or 8-bit cache).
+//
+//   out[b][h] = sum_j softmax_j(scale <q[b][h], K_j>) V_j,
+//   j over the entries of b's prefix and then b's own.
+//
+// The split is attention.cu's: (segment, page) pairs of the whole batch,
+// flattened, an equal contiguous range for every warp of a persistent grid, one
+// partial result (m, l, acc) a piece of a range that lies in one segment, merged by
+// a small kernel.  A segment is a list of pages with up to 16 query rows that
+// attend to all of it: the query heads of one KV head over a sequence's own
+// entries, or 16 of the rows (sequence, query head) of a group over the group's
+// prefix, so that a page of a prefix is read once for 16 rows.
+//
+// 8-bit pages.  K = 2^e k, V = 2^f v with e4m3 rows k, v:
+//   s_j = scale 2^e_j <q, k_j>,   out = sum_j (p_j 2^f_j) v_j / sum_j p_j,   p_j = exp(s_j - m).
+// k and v turn into fp16 exactly, two values an instruction, and the products run as
+// mma.sync m16n8k16 on fp16 with fp32 sums.  q is split into a power of two a row
+// and fp16 numbers below 2^15 (exact for all but elements below 2^-29 of the row's
+// largest, which lose at most 2^-40 of it).  The weights p_j 2^f_j are held relative to
+// their own largest: with t_j = s_j + f_j (log2) and n = max t_j, w_j = 2^(t_j - n + 15)
+// is at most 2^15 and is taken as two fp16 numbers, high part and remainder
+// (22 significant bits down to 2^-18 of the largest weight, 2^-40 of it below).
+// Up to eight query heads the two parts are rows 0-7 and 8-15 of one product.
+//
+// A lane's operands come as 16-byte pieces of rows: the head dimension that
+// a product sums over may run in any order, and so may the columns of the output
+// (q is read and the output written in that order).  For K a lane reads 16
+// values of one key; for V 16 values of four keys, whose bytes are paired key by
+// key before they are converted.  A page of 16 entries is 4 KB (D = 128): one TMA
+// copy (K and V, rows swizzled so that eight lanes' pieces meet no bank twice) and
+// one of its 32 scales.
+#include <cuda_fp16.h>
+
+#include "attention.cuh"
+#include "kv8.cuh"
+#include "mma.cuh"
+
+namespace umim {
+namespace {
+
+constexpr int kSharedMaxBatch = 4096;   // sequences and prefixes whose prefix sums lie beside the rings
+constexpr int kSharedMaxPrefixes = 512;
+
+struct PagesArgs {
+  const __nv_bfloat16 *q;
+  const int32_t *block_table, *seq_lens;
+  const int32_t *prefix_table, *prefix_lens, *prefix_offsets;   // shared prefixes only
+  int32_t B, Hq, Hkv, G, max_pages, n_pages, layer, n_layers;
+  int32_t n_prefixes, max_prefix_pages;
+  int32_t smem_plan;
+  float scale_log2;
+  int32_t *status;
+};
+
+// where prefix i's work and rows are (exclusive sums, and the offsets made to increase)
+struct PrefixPlan {
+  int32_t *pages;    // [n + 1] page visits of one KV head: pages x blocks of rows
+  int32_t *blocks;   // [n + 1] blocks of 16 rows
+  int32_t *first;    // [n + 1] first sequence
+};
+
+struct PagesWs {
+  AttnWs at;
+  PrefixPlan pre;
+};
+
+inline size_t prefix_plan_bytes(int n) { return n > 0 ? 3 * a256(sizeof(int32_t) * ((size_t)n + 1)) : 0; }
+
+// segments of a batch: (sequence, KV head), and (prefix, KV head, block of rows) at most
+inline size_t max_segments(int B, int n, int G, int Hkv) {
+  return (size_t)Hkv * (B + (n > 0 ? (size_t)n + (size_t)B * G / 16 : 0));
+}
+
+inline size_t pages_ws_bytes(int B, int n, int G, int Hkv, int D, int total_warps) {
+  const size_t pieces = max_segments(B, n, G, Hkv) + total_warps;
+  return a256(sizeof(AttnPlan)) + a256(sizeof(int32_t) * ((size_t)B + 1)) + a256(sizeof(float2) * pieces * 16) +
+         a256(sizeof(float) * pieces * 16 * D) + prefix_plan_bytes(n);
+}
+
+inline PagesWs pages_carve(void *ws, int B, int n, int G, int Hkv, int D, int total_warps) {
+  const size_t pieces = max_segments(B, n, G, Hkv) + total_warps;
+  char *p = static_cast<char *>(ws);
+  auto take = [&](size_t bytes) {
+    char *r = p;
+    p += a256(bytes);
+    return r;
+  };
+  PagesWs w{};
+  w.at.plan = reinterpret_cast<AttnPlan *>(take(sizeof(AttnPlan)));
+  w.at.pref = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * ((size_t)B + 1)));
+  w.at.part_ml = reinterpret_cast<float2 *>(take(sizeof(float2) * pieces * 16));
+  w.at.part_acc = reinterpret_cast<float *>(take(sizeof(float) * pieces * 16 * D));
+  if (n > 0) {
+    const size_t b = sizeof(int32_t) * ((size_t)n + 1);
+    w.pre.pages = reinterpret_cast<int32_t *>(take(b));
+    w.pre.blocks = reinterpret_cast<int32_t *>(take(b));
+    w.pre.first = reinterpret_cast<int32_t *>(take(b));
+  }
+  return w;
+}
+
+// The plan of the prefixes, by a CTA's first warp (a barrier follows at the caller's).
+// Offsets that decrease or leave [0, B] count as the largest before them, a
+// length outside the table as 0; both are recorded when `report` is set.
+__device__ __forceinline__ void plan_prefixes(const PagesArgs &a, const PrefixPlan &p, bool report) {
+  const int lane = threadIdx.x & 31, n = a.n_prefixes;
+  int most = 0, pages = 0, blocks = 0;
+  for (int i0 = 0; i0 <= n; i0 += 32) {
+    const int i = i0 + lane;
+    int o = i <= n ? (a.prefix_offsets ? a.prefix_offsets[i] : i * a.B) : 0;   // (no offsets: one prefix for all)
+    if (o < 0 || o > a.B) {
+      if (report) set_error(a.status, UMIM_ERR_INVALID_ARG);
+      o = 0;
+    }
+    int x = o;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) x = max(x, __shfl_up_sync(0xffffffffu, x, d));   // (lanes below d: their own)
+    x = max(x, most);
+    if (report && i <= n && x != o) set_error(a.status, UMIM_ERR_INVALID_ARG);
+    if (i <= n) p.first[i] = x;
+    most = __shfl_sync(0xffffffffu, x, 31);
+  }
+  __syncwarp();
+  for (int i0 = 0; i0 <= n; i0 += 32) {
+    const int i = i0 + lane;
+    int nb = 0, np = 0;
+    if (i < n) {
+      int L = a.prefix_lens[i];
+      if (L < 0 || (int64_t)L > (int64_t)a.max_prefix_pages * kPageSize) {
+        if (report) set_error(a.status, UMIM_ERR_INVALID_ARG);
+        L = 0;
+      }
+      nb = L > 0 ? ceil_div((p.first[i + 1] - p.first[i]) * a.G, 16) : 0;
+      np = nb * ceil_div(L, kPageSize);
+    }
+    int xb = nb, xp = np;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int yb = __shfl_up_sync(0xffffffffu, xb, d), yp = __shfl_up_sync(0xffffffffu, xp, d);
+      if (lane >= d) xb += yb, xp += yp;
+    }
+    if (i <= n) {
+      p.blocks[i] = blocks + xb - nb;
+      p.pages[i] = pages + xp - np;
+    }
+    blocks += __shfl_sync(0xffffffffu, xb, 31);
+    pages += __shfl_sync(0xffffffffu, xp, 31);
+  }
+}
+
+// the last i in [0, n) with at[i] * times <= x
+__device__ __forceinline__ int last_at_most(const int32_t *at, int n, int times, int x) {
+  int l = 0, h = n;
+  while (h - l > 1) {
+    const int m = (l + h) >> 1;
+    if (at[m] * times <= x) l = m;
+    else h = m;
+  }
+  return l;
+}
+
+// what a warp holds of a page: its layout in shared memory
+template <int D, int BITS>
+struct PageTile {
+  static constexpr int kTile = 16 * D * BITS / 8;                // bytes of K, and of V
+  static constexpr int kRow = D * BITS / 8 < 128 ? D * BITS / 8 : 128;   // bytes of a row in one box
+  static constexpr int kBoxes = D * BITS / 8 / kRow;             // boxes of [K, V][16 rows][kRow]
+  static constexpr int kStage = 2 * kTile;
+  static constexpr int kStages = kStage >= 8192 ? 2 : 4;
+  static constexpr int kScales = BITS == 8 ? 128 : 0;            // bytes of a stage's scales (32 used; TMA wants 128-byte steps)
+  static constexpr int kWarp = kStages * kStage;
+  static constexpr int kRings = kAttnWarps * kStages * (kStage + kScales);
+  // byte offset of 16-byte piece c of row r (of K; V kRow * 16 further) as TMA's
+  // swizzle for rows of 128 or 64 bytes puts it
+  static __device__ __forceinline__ uint32_t at(int r, int c) {
+    if constexpr (kRow == 128)
+      return (c >> 3) * (2 * 16 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+    else
+      return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
+  }
+};
+
+__device__ __forceinline__ uint4 lds_v4(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds_v2(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
+
+template <int BITS>
+__device__ __forceinline__ void mma_page(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (BITS == 8) mma_f16(c, a, b0, b1);
+  else mma_bf16(c, a, b0, b1);
+}
+
+// One segment as the warp that works on it sees it.
+struct Segment {
+  int i, g, blk;        // sequence or prefix, KV head, block of rows
+  bool prefix;
+  int n, len;           // pages, entries
+  const int32_t *table;
+};
+
+// R8 (8-bit cache, no prefixes): at most eight query rows, the weights' two parts in one product
+template <int D, int BITS, bool SHARED, bool R8>
+__global__ void __launch_bounds__(kAttnWarps * 32, 1)
+    attn_pages_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_constant__ CUtensorMap scale_map,
+                      PagesArgs a, PagesWs ws) {
+  using P = PageTile<D, BITS>;
+  static_assert(!R8 || BITS == 8, "");
+  constexpr int NT = D / 8;                // n-tiles of the output
+  constexpr int KC = D / 16;               // k-chunks of Q K^T
+  constexpr int NR = R8 ? 1 : 2;           // query rows of a lane
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ uint64_t bars[kAttnWarps][P::kStages];
+
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  const int gw = blockIdx.x * kAttnWarps + warp, total_warps = gridDim.x * kAttnWarps;
+  uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t *wbuf = base + warp * P::kWarp;
+  uint8_t *wscales = base + kAttnWarps * P::kWarp + warp * P::kStages * P::kScales;
+
+  if (lane == 0) {
+    for (int s = 0; s < P::kStages; ++s) mbar_init(&bars[warp][s], 1);
+    fence_mbar_init();
+    if (warp == 0) {
+      prefetch_tensormap(&kv_map);
+      if (BITS == 8) prefetch_tensormap(&scale_map);
+    }
+  }
+  __syncwarp();
+  griddep_wait();
+
+  const int G = a.G, Hkv = a.Hkv;
+  const int32_t *pref = ws.at.pref;
+  PrefixPlan pre = ws.pre;
+  int own;   // pages of the sequences' own entries, of one KV head
+  int32_t *plan = reinterpret_cast<int32_t *>(base + P::kRings);
+  if (SHARED) {
+    pre.pages = plan;
+    pre.blocks = plan + (a.n_prefixes + 1);
+    pre.first = plan + 2 * (a.n_prefixes + 1);
+    plan += 3 * (a.n_prefixes + 1);
+    if (warp == 0) plan_prefixes(a, pre, blockIdx.x == 0);
+  }
+  if (SHARED || a.smem_plan) {
+    own = plan_prefix<kAttnWarps * 32>(a.seq_lens, a.B, a.max_pages, plan, blockIdx.x == 0, a.status);
+    pref = plan;
+    if (blockIdx.x == 0) {   // for the combine kernel
+      for (int b = threadIdx.x; b <= a.B; b += kAttnWarps * 32) ws.at.pref[b] = plan[b];
+      if (SHARED)
+        for (int i = threadIdx.x; i <= a.n_prefixes; i += kAttnWarps * 32) {
+          ws.pre.pages[i] = pre.pages[i];
+          ws.pre.blocks[i] = pre.blocks[i];
+          ws.pre.first[i] = pre.first[i];
+        }
+    }
+  } else {
+    own = pref[a.B];
+  }
+  const int total = Hkv * (own + (SHARED ? pre.pages[a.n_prefixes] : 0));
+  const int W = max(1, ceil_div(total, total_warps));
+  if (blockIdx.x == 0 && threadIdx.x == 0) ws.at.plan->W = W;
+  const int start = (int)min((int64_t)gw * W, (int64_t)total);
+  const int end = min(total, start + W);
+  if (start >= end) return;
+
+  const uint64_t pol = policy_evict_first();
+
+  auto set_own = [&](Segment &s) {
+    s.n = pref[s.i + 1] - pref[s.i];
+    s.len = a.seq_lens[s.i];
+    s.table = a.block_table + (int64_t)s.i * a.max_pages;
+  };
+  auto blocks_of = [&](int i) { return pre.blocks[i + 1] - pre.blocks[i]; };
+  auto set_prefix = [&](Segment &s) {
+    s.len = a.prefix_lens[s.i];
+    s.n = ceil_div(s.len, kPageSize);
+    s.table = a.prefix_table + (int64_t)s.i * a.max_prefix_pages;
+  };
+  // the segment of a flattened position, and the page in it
+  auto locate = [&](int pos, Segment &s, int &pi) {
+    s.blk = 0;
+    s.prefix = SHARED && pos >= Hkv * own;
+    if (!s.prefix) {   // (sequences without pages share their successor's first)
+      s.i = last_at_most(pref, a.B, Hkv, pos);
+      set_own(s);
+      const int r = pos - Hkv * pref[s.i];
+      s.g = r / s.n;
+      pi = r - s.g * s.n;
+    } else {
+      pos -= Hkv * own;
+      s.i = last_at_most(pre.pages, a.n_prefixes, Hkv, pos);
+      set_prefix(s);
+      const int r = pos - Hkv * pre.pages[s.i], x = r / s.n, nb = blocks_of(s.i);
+      s.g = x / nb;
+      s.blk = x - s.g * nb;
+      pi = r - x * s.n;
+    }
+  };
+  // the segment behind s, which there is
+  auto advance = [&](Segment &s) {
+    if (SHARED && s.prefix) {
+      if (++s.blk < blocks_of(s.i)) return;
+      s.blk = 0;
+      if (++s.g < Hkv) return;
+      s.g = 0;
+      do ++s.i;
+      while (pre.pages[s.i + 1] == pre.pages[s.i]);
+      set_prefix(s);
+    } else {
+      if (++s.g < Hkv) return;
+      s.g = 0;
+      do ++s.i;
+      while (s.i < a.B && pref[s.i + 1] == pref[s.i]);
+      if (SHARED && s.i == a.B) {
+        s.prefix = true;
+        s.i = 0;
+        while (pre.pages[s.i + 1] == pre.pages[s.i]) ++s.i;
+        set_prefix(s);
+      } else {
+        set_own(s);
+      }
+    }
+  };
+  // its number: in the flattened order, so that number + warp is a piece of its own
+  auto number = [&](const Segment &s) {
+    if (SHARED && s.prefix) return Hkv * (a.B + pre.blocks[s.i]) + s.g * blocks_of(s.i) + s.blk;
+    return s.i * Hkv + s.g;
+  };
+  // query row r of 16 as a row of q, -1 for none
+  auto query_row = [&](const Segment &s, int r) {
+    if (SHARED && s.prefix) {
+      const int x = s.blk * 16 + r, b = pre.first[s.i] + x / G;
+      return b < pre.first[s.i + 1] ? (int64_t)b * a.Hq + s.g * G + x % G : int64_t(-1);
+    }
+    return r < G ? (int64_t)s.i * a.Hq + s.g * G + r : int64_t(-1);
+  };
+
+  // ---- compute cursor and loader cursor (every lane keeps both; one issues the copies) ----
+  Segment cs, ls;
+  int cpi, lpi;
+  locate(start, cs, cpi);
+  ls = cs;
+  lpi = cpi;
+  int ld_pos = start;
+  auto page_of = [&]() {
+    const int cols = SHARED && ls.prefix ? a.max_prefix_pages : a.max_pages;
+    return in_bounds(lpi, cols, a.status, kSitePagesTable) ? ls.table[lpi] : -1;
+  };
+  int next_page = page_of();   // looked up a copy ahead: the copy does not wait for the table
+  auto issue = [&](int stage) {
+    int c = a.layer * a.n_pages + next_page;
+    if (next_page < 0 || next_page >= a.n_pages) {
+      // a coordinate past the tensor's last page: the copy reads zeros
+      set_error(a.status, UMIM_ERR_INVALID_ARG);
+      c = a.n_layers * a.n_pages;
+    }
+    if (elect_one()) {
+      uint64_t *bar = &bars[warp][stage];
+      uint8_t *dst = wbuf + stage * P::kStage;
+      mbar_arrive_expect_tx(bar, P::kStage + (BITS == 8 ? 32 : 0));
+#pragma unroll
+      for (int x = 0; x < P::kBoxes; ++x)
+        tma_load_5d(dst + x * 32 * P::kRow, &kv_map, bar, x * (P::kRow * 8 / BITS), 0, ls.g, 0, c, pol);
+      if constexpr (BITS == 8) tma_load_4d(wscales + stage * P::kScales, &scale_map, bar, 0, ls.g, 0, c);
+    }
+    if (++ld_pos < end) {
+      if (++lpi == ls.n) {
+        lpi = 0;
+        advance(ls);
+      }
+      next_page = page_of();
+    }
+  };
+  for (int s = 0; s < P::kStages && ld_pos < end; ++s) issue(s);
+
+  // ---- compute state ----
+  const int qr = lane >> 2, qc = lane & 3;      // mma fragment row / column group
+  int64_t rows[NR];                             // rows of q
+  uint32_t qa[KC][2 * NR];
+  float q_scale[NR];                            // scale_log2, times the power of two taken out of the row
+  auto load_q = [&]() {
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+      rows[j] = query_row(cs, qr + 8 * j);
+      const __nv_bfloat16 *src = a.q + rows[j] * D;
+      q_scale[j] = a.scale_log2;
+      if constexpr (BITS == 16) {
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          const uint32_t *p = reinterpret_cast<const uint32_t *>(src + c * 16 + 2 * qc);
+          qa[c][j] = rows[j] >= 0 ? p[0] : 0u;
+          qa[c][j + NR] = rows[j] >= 0 ? p[4] : 0u;
+        }
+      } else {
+        // chunk c of the products: 4 elements of this lane's 16-byte pieces of K
+        uint2 x[KC];
+        uint32_t m = 0;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          const int piece = D == 128 ? qc * 2 + c / 4 : qc;
+          x[c] = make_uint2(0, 0);
+          if (rows[j] >= 0) x[c] = *reinterpret_cast<const uint2 *>(src + piece * 16 + c % 4 * 4);
+          m = __vmaxu2(m, __vmaxu2(x[c].x & 0x7fff7fff, x[c].y & 0x7fff7fff));
+        }
+        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        m = max(m & 0xffff, m >> 16) >> 7;   // the exponent field of the row's largest
+        // the largest to [2^14, 2^15); rows of zeros (or below 2^-86) and ones that hold no number by a fixed power
+        const uint32_t e = m == 255 ? 127u : max(m, 41u);
+        const float inv = __uint_as_float((268u - e) << 23);   // 2^(14 - (e - 127))
+        q_scale[j] *= __uint_as_float((e - 14) << 23);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          auto half2_of = [&](uint32_t v) {
+            const __half2 h = __floats2half2_rn(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv);
+            return *reinterpret_cast<const uint32_t *>(&h);
+          };
+          qa[c][j] = half2_of(x[c].x);
+          qa[c][j + NR] = half2_of(x[c].y);
+        }
+      }
+    }
+  };
+  load_q();
+  float acc[NT][4];
+  // a row's largest score and weight (log2), and sum of exp2(score - m)
+  float m[NR], n[NR], l[NR];
+  auto reset = [&]() {
+#pragma unroll
+    for (int j = 0; j < NR; ++j) m[j] = n[j] = -INFINITY, l[j] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+  };
+  reset();
+
+  auto flush = [&]() {
+    // complete the row sums across the 4 threads of each row
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+      l[j] += __shfl_xor_sync(0xffffffffu, l[j], 1);
+      l[j] += __shfl_xor_sync(0xffffffffu, l[j], 2);
+    }
+    const int64_t piece = number(cs) + gw;
+    if (!in_bounds(piece, (int64_t)Hkv * (a.B + (SHARED ? pre.blocks[a.n_prefixes] : 0)) + total_warps, a.status,
+                   kSitePagesPiece))
+      return;
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+      if (rows[j] < 0) continue;
+      const int64_t at = piece * 16 + qr + 8 * j;
+      if (qc == 0) ws.at.part_ml[at] = make_float2(m[j], l[j]);
+      float *dst = ws.at.part_acc + at * D;
+      if constexpr (BITS == 16) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          *reinterpret_cast<float2 *>(dst + t * 8 + 2 * qc) = make_float2(acc[t][2 * j], acc[t][2 * j + 1]);
+      } else {
+        // from units of 2^(n - 15) to those of the row sum (n - m is a cache row's exponent at most)
+        const float up = exp2f((n[j] == -INFINITY ? 0.f : n[j]) - (m[j] == -INFINITY ? 0.f : m[j]));
+        auto out = [&](int t, int c) {
+          const float x = R8 ? acc[t][c] + acc[t][2 + c] : acc[t][2 * j + c];
+          return x * 0x1p-15f * up;
+        };
+#pragma unroll
+        for (int c = 0; c < 2; ++c)   // column t of piece 2 qc + c
+#pragma unroll
+          for (int t = 0; t < NT; t += 4)
+            *reinterpret_cast<float4 *>(dst + (2 * qc + c) * NT + t) =
+                make_float4(out(t, c), out(t + 1, c), out(t + 2, c), out(t + 3, c));
+      }
+    }
+  };
+
+  int it = 0;
+  for (int pos = start; pos < end; ++pos, ++it) {
+    if (cpi == cs.n) {   // next segment
+      flush();
+      cpi = 0;
+      advance(cs);
+      load_q();
+      reset();
+    }
+    const int stage = it % P::kStages;
+    const uint32_t parity = (it / P::kStages) & 1;
+    if (!mbar_wait(&bars[warp][stage], parity)) {
+      set_error(a.status, UMIM_ERR_TIMEOUT);
+      // let the copies still in flight land (each wait bounded) before leaving
+      for (int k = 1; k < P::kStages && pos + k < ld_pos; ++k)
+        mbar_wait(&bars[warp][(it + k) % P::kStages], ((it + k) / P::kStages) & 1);
+      return;
+    }
+    const uint32_t ks = smem_u32(wbuf + stage * P::kStage), vs = ks + 16 * P::kRow;
+    const uint32_t sc = smem_u32(wscales + stage * P::kScales);
+    const int nvalid = min(16, cs.len - cpi * 16);
+    ++cpi;
+
+    // S = Q K^T, 16 keys as two n-tiles of 8; even and odd chunks apart, to halve the dependent chain
+    float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    float s2[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    auto q_of = [&](int c, uint32_t (&f)[4]) {
+      f[0] = qa[c][0], f[2] = qa[c][NR];
+      f[1] = R8 ? 0u : qa[c][NR - 1], f[3] = R8 ? 0u : qa[c][2 * NR - 1];
+    };
+    if constexpr (BITS == 16) {
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        uint32_t b0, b1, b2, b3, f[4];
+        q_of(c, f);
+        ldsm_x4(ks + P::at((lane & 7) + ((lane >> 4) << 3), 2 * c + ((lane >> 3) & 1)), b0, b1, b2, b3);
+        mma_bf16(c & 1 ? s2[0] : s[0], f, b0, b1);
+        mma_bf16(c & 1 ? s2[1] : s[1], f, b2, b3);
+      }
+    } else {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int t = 0; t < D / 64; ++t) {
+          const uint4 x = lds_v4(ks + P::at(nt * 8 + qr, D == 128 ? qc * 2 + t : qc));
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t f[4];
+            q_of(t * 4 + w, f);
+            mma_f16(w & 1 ? s2[nt] : s[nt], f, f16x2_of_e4m3x2(xs[w]), f16x2_of_e4m3x2(xs[w] >> 16));
+          }
+        }
+    }
+    // to log2 units; keys past the end masked.  This lane's keys are nt * 8 + 2 qc + {0, 1}.
+    float w[2][4];   // weights' exponents (8-bit), then the weights
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      float ke[2] = {1.f, 1.f}, ve[2] = {0.f, 0.f};
+      if constexpr (BITS == 8) {
+        const uint32_t kc = lds_u16(sc + nt * 8 + 2 * qc), vc = lds_u16(sc + 16 + nt * 8 + 2 * qc);
+        ke[0] = e8m0_value(kc & 0xff), ke[1] = e8m0_value(kc >> 8);
+        const uint32_t v0 = vc & 0xff, v1 = vc >> 8;
+        ve[0] = v0 == 255 ? NAN : (float)((int)v0 - 127), ve[1] = v1 == 255 ? NAN : (float)((int)v1 - 127);
+      }
+#pragma unroll
+      for (int e = 0; e < 2 * NR; ++e) {
+        const bool live = nt * 8 + 2 * qc + (e & 1) < nvalid;
+        const float x = (s[nt][e] + s2[nt][e]) * q_scale[e >> 1] * ke[e & 1];
+        s[nt][e] = live ? x : -INFINITY;
+        w[nt][e] = live ? x + ve[e & 1] : -INFINITY;
+      }
+    }
+    bool moved = false;
+    float c[NR];
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+      auto row_max = [&](const float (&x)[2][4]) {
+        float y = fmaxf(fmaxf(x[0][2 * j], x[0][2 * j + 1]), fmaxf(x[1][2 * j], x[1][2 * j + 1]));
+        y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
+        return fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
+      };
+      const float m_was = m[j], n_was = n[j];
+      m[j] = fmaxf(m[j], row_max(s));
+      n[j] = BITS == 8 ? fmaxf(n[j], row_max(w)) : m[j];
+      // no finite score so far: weights from 0, so that a score of -inf weighs 0 and NaN stays NaN
+      const float m0 = m[j] == -INFINITY ? 0.f : m[j], n0 = n[j] == -INFINITY ? 0.f : n[j];
+      c[j] = exp2f(n_was - n0);
+      moved = moved || c[j] != 1.f;
+      float sum = 0.f;
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 2 * j; e < 2 * j + 2; ++e) {
+          const float p = exp2f(s[nt][e] - m0);
+          sum += p;
+          w[nt][e] = BITS == 8 ? exp2f(w[nt][e] - n0 + 15.f) : p;
+        }
+      l[j] = l[j] * exp2f(m_was - m0) + sum;
+    }
+    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        acc[t][0] *= c[0];
+        acc[t][1] *= c[0];
+        acc[t][2] *= c[NR - 1];
+        acc[t][3] *= c[NR - 1];
+      }
+    }
+    // the weights as the A operand: a high part and what it leaves
+    uint32_t ph[4], pl[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {   // rows qr, qr + 8 of keys 0-7, then of keys 8-15
+      if (R8 && (r & 1)) continue;
+      const float x = w[r >> 1][2 * (r & 1)], y = w[r >> 1][2 * (r & 1) + 1];
+      if constexpr (BITS == 8) {
+        const __half2 h = __floats2half2_rn(x, y);
+        const __half2 rest = __floats2half2_rn(x - __low2float(h), y - __high2float(h));
+        ph[r] = *reinterpret_cast<const uint32_t *>(&h);
+        pl[r] = *reinterpret_cast<const uint32_t *>(&rest);
+      } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        ph[r] = *reinterpret_cast<const uint32_t *>(&h);
+        pl[r] = pack_bf16(x - __low2float(h), y - __high2float(h));
+      }
+    }
+    if constexpr (R8) ph[1] = pl[0], ph[3] = pl[2];
+    // O += P V
+    if constexpr (BITS == 16) {
+      if (nvalid < 16) {
+        // zero V rows past the end so that 0 * garbage cannot make a NaN
+        for (int idx = lane; idx < (16 - nvalid) * (D / 8); idx += 32) {
+          const uint32_t at = vs + P::at(nvalid + idx / (D / 8), idx % (D / 8));
+          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+        }
+        // order these generic-proxy writes before the next TMA write of the stage
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        uint32_t b0, b1, b2, b3;
+        ldsm_x4_t(vs + P::at((lane & 7) + (((lane >> 3) & 1) << 3), 2 * j + (lane >> 4)), b0, b1, b2, b3);
+        mma_bf16(acc[2 * j], ph, b0, b1);
+        mma_bf16(acc[2 * j + 1], ph, b2, b3);
+        mma_bf16(acc[2 * j], pl, b0, b1);
+        mma_bf16(acc[2 * j + 1], pl, b2, b3);
+      }
+    } else {
+      // column t of n-tile t is value t of this lane's piece qr (D / 8 values) of a row
+      uint32_t v[4][NT / 4];   // keys 2 qc, 2 qc + 1, 2 qc + 8, 2 qc + 9
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int key = 2 * qc + (k & 1) + (k >> 1) * 8;
+        if constexpr (D == 128) {
+          const uint4 x = lds_v4(vs + P::at(key, qr));
+          v[k][0] = x.x, v[k][1] = x.y, v[k][2] = x.z, v[k][3] = x.w;
+        } else {
+          const uint2 x = lds_v2(vs + P::at(key, qr >> 1) + (qr & 1) * 8);
+          v[k][0] = x.x, v[k][1] = x.y;
+        }
+        if (nvalid < 16 && key >= nvalid) {   // 0 * garbage must not make a NaN
+#pragma unroll
+          for (int i = 0; i < NT / 4; ++i) v[k][i] = 0;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NT / 4; ++i) {
+        const uint32_t a01 = __byte_perm(v[0][i], v[1][i], 0x5140), a23 = __byte_perm(v[0][i], v[1][i], 0x7362);
+        const uint32_t b01 = __byte_perm(v[2][i], v[3][i], 0x5140), b23 = __byte_perm(v[2][i], v[3][i], 0x7362);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t lo = (x < 2 ? a01 : a23) >> (x & 1) * 16, hi = (x < 2 ? b01 : b23) >> (x & 1) * 16;
+          const uint32_t f0 = f16x2_of_e4m3x2(lo), f1 = f16x2_of_e4m3x2(hi);
+          mma_f16(acc[i * 4 + x], ph, f0, f1);
+          if constexpr (!R8) mma_f16(acc[i * 4 + x], pl, f0, f1);
+        }
+      }
+    }
+    __syncwarp();
+    // refill this stage
+    if (ld_pos < end) issue(stage);
+  }
+  flush();
+}
+
+// ---------------------------------------------------------------------------
+// combine for shared prefixes: WPR warps per (b, query head) row, over the pieces
+// of its own entries' segment and then of its prefix's block
+// ---------------------------------------------------------------------------
+template <int D, int WPR>
+__global__ void __launch_bounds__(kCombineThreads)
+    shared_combine_kernel(PagesWs ws, int B, int n_prefixes, int Hq, int Hkv, int G, __nv_bfloat16 *out) {
+  constexpr int E = D / 32;
+  constexpr int kWarps = kCombineThreads / 32, RPB = kWarps / WPR;   // rows per CTA
+  __shared__ float s_m[kWarps], s_l[kWarps];
+  __shared__ float s_acc[WPR > 1 ? kWarps : 1][D];
+  griddep_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row_g = blockIdx.x * RPB + warp / WPR, sub = warp % WPR;
+  const bool live = row_g < B * Hq;
+  float M = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  bool any = false;
+  if (live) {
+    const int b = row_g / Hq, h = row_g % Hq, g = h / G, W = ws.at.plan->W;
+    // pieces of the segment that takes n positions from `at` on: seg + w for the warps w that meet them
+    auto merge = [&](int seg, int at, int n, int row) {
+      if (n <= 0) return;
+      any = true;
+      const int w0 = at / W, w1 = (at + n - 1) / W;
+      merge_pieces<E>(ws.at.part_ml, ws.at.part_acc, (int64_t)(seg + w0) * 16 + row, 16, w1 - w0 + 1, sub, WPR, M, l, o);
+    };
+    const int first = ws.at.pref[b], n = ws.at.pref[b + 1] - first;
+    merge(b * Hkv + g, Hkv * first + g * n, n, h % G);
+    const int i = last_at_most(ws.pre.first, n_prefixes, 1, b);
+    if (b >= ws.pre.first[i] && b < ws.pre.first[i + 1]) {
+      const int nb = ws.pre.blocks[i + 1] - ws.pre.blocks[i];
+      if (nb > 0) {
+        const int x = (b - ws.pre.first[i]) * G + h % G;
+        const int np = (ws.pre.pages[i + 1] - ws.pre.pages[i]) / nb;
+        merge(Hkv * (B + ws.pre.blocks[i]) + g * nb + x / 16,
+              Hkv * (ws.at.pref[B] + ws.pre.pages[i]) + (g * nb + x / 16) * np, np, x % 16);
+      }
+    }
+  }
+  if constexpr (WPR > 1) {
+    if (lane == 0) {
+      s_m[warp] = M;
+      s_l[warp] = l;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_acc[warp][lane * E + e] = o[e];
+    __syncthreads();
+    if (sub != 0) return;
+    float Mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) Mx = fmaxf(Mx, s_m[warp + w]);
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    if (Mx == -INFINITY) Mx = 0.f;
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) {
+      const float c = exp2f(s_m[warp + w] - Mx);
+      l += c * s_l[warp + w];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += c * s_acc[warp + w][lane * E + e];
+    }
+  }
+  if (!live) return;
+  const float inv = any ? 1.f / l : 0.f;   // (no entries: zeros)
+  __nv_bfloat16 *dst = out + (int64_t)row_g * D + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) dst[e] = __float2bfloat16_rn(o[e] * inv);
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+// a cache of either kind
+struct CacheView {
+  void *values, *scales;   // scales null: bf16
+  int n_layers, n_pages, n_kv_heads;
+};
+
+template <int D, int BITS>
+bool encode_maps(const CacheView &kv, CUtensorMap *values, CUtensorMap *scales) {
+  using P = PageTile<D, BITS>;
+  EncodeTiledFn enc = get_encode_tiled();
+  if (!enc) return false;
+  const cuuint64_t H = kv.n_kv_heads, N = (cuuint64_t)kv.n_layers * (cuuint64_t)kv.n_pages, row = D * BITS / 8;
+  const cuuint64_t dims[5] = {(cuuint64_t)D, 16, H, 2, N};
+  const cuuint64_t strides[4] = {row, 16 * row, H * 16 * row, 2 * H * 16 * row};
+  const cuuint32_t box[5] = {(cuuint32_t)(P::kRow * 8 / BITS), 16, 1, 2, 1};
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  if (enc(values, BITS == 8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, kv.values, dims,
+          strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+          P::kRow == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return false;
+  *scales = *values;
+  if (BITS == 16) return true;
+  const cuuint64_t sdims[4] = {16, H, 2, N}, sstrides[3] = {16, 16 * H, 32 * H};
+  const cuuint32_t sbox[4] = {16, 1, 2, 1};
+  return enc(scales, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, kv.scales, sdims, sstrides, sbox, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int BITS, bool SHARED>
+umim_status run_pages(const CacheView &kv, PagesArgs a, void *out, void *workspace, cudaStream_t stream, int num_sms) {
+  using P = PageTile<D, BITS>;
+  CUtensorMap map, scale_map;
+  if (!encode_maps<D, BITS>(kv, &map, &scale_map)) return UMIM_ERR_CUDA;
+  a.n_layers = kv.n_layers;
+  a.n_pages = kv.n_pages;
+  a.Hkv = kv.n_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  const int total_warps = std::max(1, num_sms) * kAttnWarps;
+  const PagesWs ws = pages_carve(workspace, a.B, SHARED ? a.n_prefixes : 0, a.G, a.Hkv, D, total_warps);
+  a.smem_plan = a.B <= kSmemPlanBatch ? 1 : 0;
+  if (!a.smem_plan) {   // (never with prefixes: their batch is limited)
+    trace_mark(stream, "attention.plan");
+    if (launch_pdl(attn_plan_kernel, dim3(1), dim3(kPlanThreadsA), 0, stream, a.seq_lens, a.B, a.max_pages, ws.at,
+                   a.status) != cudaSuccess)
+      return UMIM_ERR_CUDA;
+  }
+  constexpr size_t kBase = P::kRings + 1024;
+  const size_t plan = a.smem_plan ? sizeof(int32_t) * ((size_t)a.B + 1 + (SHARED ? 3 * ((size_t)a.n_prefixes + 1) : 0)) : 0;
+  constexpr size_t kMost = kBase + sizeof(int32_t) * (kSmemPlanBatch + 1 + (SHARED ? 3 * (kSharedMaxPrefixes + 1) : 0));
+  static_assert(kMost + 1024 <= 232448 && kSharedMaxBatch <= kSmemPlanBatch, "shared memory of a CTA");
+  auto kern = attn_pages_kernel<D, BITS, SHARED, false>;
+  if constexpr (BITS == 8 && !SHARED)
+    if (a.G <= 8) kern = attn_pages_kernel<D, BITS, SHARED, true>;
+  if (!allow_smem(kern, kMost)) return UMIM_ERR_CUDA;
+  trace_mark(stream, SHARED ? "attention.shared" : "attention.decode_kv8");
+  if (launch_pdl(kern, dim3((unsigned)(total_warps / kAttnWarps)), dim3(kAttnWarps * 32), kBase + plan, stream, map,
+                 scale_map, a, ws) != cudaSuccess)
+    return UMIM_ERR_CUDA;
+  trace_mark(stream, "attention.combine");
+  __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out);
+  if constexpr (SHARED) {
+    // a row merges the pieces of two segments
+    const int wpr = combine_warps(2 + total_warps / std::max(1, (a.n_prefixes + a.B) * a.Hkv) * 2);
+    const int rows = kCombineThreads / 32 / wpr;
+    auto comb = wpr == 8 ? shared_combine_kernel<D, 8>
+                : wpr == 4 ? shared_combine_kernel<D, 4>
+                : wpr == 2 ? shared_combine_kernel<D, 2> : shared_combine_kernel<D, 1>;
+    if (launch_pdl(comb, dim3((unsigned)((a.B * a.Hq + rows - 1) / rows)), dim3(kCombineThreads), 0, stream, ws, a.B,
+                   a.n_prefixes, a.Hq, a.Hkv, a.G, o) != cudaSuccess)
+      return UMIM_ERR_CUDA;
+  } else {
+    const int wpr = combine_warps(1 + total_warps / std::max(1, a.B * a.Hkv));
+    const int rows = kCombineThreads / 32 / wpr;
+    auto comb = wpr == 8 ? attn_combine_kernel<D, 8>
+                : wpr == 4 ? attn_combine_kernel<D, 4>
+                : wpr == 2 ? attn_combine_kernel<D, 2> : attn_combine_kernel<D, 1>;
+    if (launch_pdl(comb, dim3((unsigned)((a.B * a.Hq + rows - 1) / rows)), dim3(kCombineThreads), 0, stream, ws.at, a.B,
+                   a.Hq, a.Hkv, a.G, o) != cudaSuccess)
+      return UMIM_ERR_CUDA;
+  }
+  trace_mark(stream, nullptr);
+  return cudaGetLastError() == cudaSuccess ? UMIM_OK : UMIM_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t decode_attention_kv8_workspace_bytes(int B, int Hkv, int D, int num_sms) {
+  return pages_ws_bytes(B, 0, 1, Hkv, D, std::max(1, num_sms) * kAttnWarps);
+}
+
+size_t decode_attention_shared_workspace_bytes(int B, int n, int Hq, int Hkv, int D, int num_sms) {
+  return pages_ws_bytes(B, std::max(1, n), Hq / Hkv, Hkv, D, std::max(1, num_sms) * kAttnWarps);
+}
+
+umim_status decode_attention_kv8(const void *q, int Hq, const umim_paged_kv8 *kv, int layer, const int32_t *block_table,
+                                 int max_pages, const int32_t *seq_lens, int B, float scale, void *out, void *workspace,
+                                 int32_t *status, cudaStream_t stream, int num_sms) {
+  PagesArgs a{};
+  a.q = static_cast<const __nv_bfloat16 *>(q);
+  a.block_table = block_table;
+  a.seq_lens = seq_lens;
+  a.B = B;
+  a.Hq = Hq;
+  a.max_pages = max_pages;
+  a.layer = layer;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.status = status;
+  const CacheView c{kv->values, kv->scales, kv->n_layers, kv->n_pages, kv->n_kv_heads};
+  return kv->head_dim == 128 ? run_pages<128, 8, false>(c, a, out, workspace, stream, num_sms)
+                             : run_pages<64, 8, false>(c, a, out, workspace, stream, num_sms);
+}
+
+bool decode_attention_shared_supported(int B, int n) { return B <= kSharedMaxBatch && n <= kSharedMaxPrefixes; }
+
+// scales null: a bf16 cache
+umim_status decode_attention_shared(const void *q, int Hq, void *values, void *scales, int n_layers, int n_pages,
+                                    int Hkv, int D, int layer, const int32_t *prefix_table, int max_prefix_pages,
+                                    const int32_t *prefix_lens, const int32_t *prefix_offsets, int n_prefixes,
+                                    const int32_t *block_table, int max_pages, const int32_t *seq_lens, int B,
+                                    float scale, void *out, void *workspace, int32_t *status, cudaStream_t stream,
+                                    int num_sms) {
+  PagesArgs a{};
+  a.q = static_cast<const __nv_bfloat16 *>(q);
+  a.block_table = block_table;
+  a.seq_lens = seq_lens;
+  a.prefix_table = prefix_table;
+  a.prefix_lens = prefix_lens;
+  a.prefix_offsets = prefix_offsets;
+  a.n_prefixes = n_prefixes;
+  a.max_prefix_pages = max_prefix_pages;
+  a.B = B;
+  a.Hq = Hq;
+  a.max_pages = max_pages;
+  a.layer = layer;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.status = status;
+  const CacheView c{values, scales, n_layers, n_pages, Hkv};
+  if (scales == nullptr)
+    return D == 128 ? run_pages<128, 16, true>(c, a, out, workspace, stream, num_sms)
+                    : run_pages<64, 16, true>(c, a, out, workspace, stream, num_sms);
+  return D == 128 ? run_pages<128, 8, true>(c, a, out, workspace, stream, num_sms)
+                  : run_pages<64, 8, true>(c, a, out, workspace, stream, num_sms);
+}
+
+}  // namespace umim

@@ -78,7 +78,11 @@ enum DebugSite : int32_t {
   kSiteTopkEntry = 26,
   kSiteLogprobSegment = 27,
   kSiteLogprobRank = 28,
-  kSiteCount = 29
+  kSiteKv8Dst = 29,
+  kSiteKv8Src = 30,
+  kSitePagesTable = 31,
+  kSitePagesPiece = 32,
+  kSiteCount = 33
 };
 
 // true when 0 <= i < n; in the debug build a false result is recorded
@@ -250,6 +254,16 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, u
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
       " [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(smem_u32(bar)), "l"(policy)
+      : "memory");
+}
+
+// (for small pieces that another block's copy reads the neighbours of: no cache hint)
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, uint64_t *bar, int c0, int c1, int c2,
+                                            int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar))
       : "memory");
 }
 
