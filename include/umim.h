@@ -494,7 +494,7 @@ umim_status umim_decode_attention_kv8(const void *q, int32_t n_q_heads, const um
  * over tables that hold the prefix's pages first, but for rounding, and prefix
  * lengths need not be multiples of 16.
  *
- * q               device bf16 [batch][n_q_heads][head_dim], 8-B aligned
+ * q               device bf16 [batch][n_q_heads][head_dim], 16-B aligned
  * prefix_table    device int32 [n_prefixes][max_prefix_pages]
  * prefix_lens     device int32 [n_prefixes]
  * prefix_offsets  device int32 [n_prefixes + 1], nondecreasing in [0, batch],

@@ -457,6 +457,8 @@ const char *umim_debug_site_name(int32_t status) {
       "kv8.src",
       "attention_pages.block_table",
       "attention_pages.piece",
+      "attention_prefix.block_table",
+      "attention_prefix.piece",
   };
   const int site = (status >> 8) & 0xffffff;
   return site < kSiteCount ? names[site] : "";
@@ -674,7 +676,7 @@ umim_status shared_checked(const void *q, int32_t n_q_heads, void *values, void 
     return UMIM_ERR_UNSUPPORTED;
   if (batch == 0) return UMIM_OK;
   if (!q || !prefix_table || !prefix_lens || !block_table || !seq_lens || !out) return UMIM_ERR_INVALID_ARG;
-  if (!aligned(q, 8) || !aligned(out, 2)) return UMIM_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 2)) return UMIM_ERR_INVALID_ARG;
   const DeviceScope scope(stream);
   const int sms = scope.sms();
   if (!workspace || !aligned(workspace, 256) ||
@@ -751,6 +753,7 @@ umim_status umim_decode_attention_kv8(const void *q, int32_t n_q_heads, const um
 size_t umim_decode_attention_shared_workspace_size(int32_t batch, int32_t n_prefixes, int32_t n_q_heads,
                                                    int32_t n_kv_heads, int32_t head_dim) {
   if (batch < 0 || n_prefixes < 1 || n_q_heads <= 0 || n_kv_heads <= 0 || (head_dim != 64 && head_dim != 128)) return 0;
+  if (!heads_supported(n_q_heads, n_kv_heads)) return 0;
   return decode_attention_shared_workspace_bytes(batch, n_prefixes, n_q_heads, n_kv_heads, head_dim, sms_or_largest());
 }
 

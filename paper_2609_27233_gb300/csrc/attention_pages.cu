@@ -32,133 +32,12 @@
 // one of its 32 scales.
 #include <cuda_fp16.h>
 
-#include "attention.cuh"
+#include "attention_pages.cuh"
 #include "kv8.cuh"
 #include "mma.cuh"
 
 namespace umim {
 namespace {
-
-constexpr int kSharedMaxBatch = 4096;   // sequences and prefixes whose prefix sums lie beside the rings
-constexpr int kSharedMaxPrefixes = 512;
-
-struct PagesArgs {
-  const __nv_bfloat16 *q;
-  const int32_t *block_table, *seq_lens;
-  const int32_t *prefix_table, *prefix_lens, *prefix_offsets;   // shared prefixes only
-  int32_t B, Hq, Hkv, G, max_pages, n_pages, layer, n_layers;
-  int32_t n_prefixes, max_prefix_pages;
-  int32_t smem_plan;
-  float scale_log2;
-  int32_t *status;
-};
-
-// where prefix i's work and rows are (exclusive sums, and the offsets made to increase)
-struct PrefixPlan {
-  int32_t *pages;    // [n + 1] page visits of one KV head: pages x blocks of rows
-  int32_t *blocks;   // [n + 1] blocks of 16 rows
-  int32_t *first;    // [n + 1] first sequence
-};
-
-struct PagesWs {
-  AttnWs at;
-  PrefixPlan pre;
-};
-
-inline size_t prefix_plan_bytes(int n) { return n > 0 ? 3 * a256(sizeof(int32_t) * ((size_t)n + 1)) : 0; }
-
-// segments of a batch: (sequence, KV head), and (prefix, KV head, block of rows) at most
-inline size_t max_segments(int B, int n, int G, int Hkv) {
-  return (size_t)Hkv * (B + (n > 0 ? (size_t)n + (size_t)B * G / 16 : 0));
-}
-
-inline size_t pages_ws_bytes(int B, int n, int G, int Hkv, int D, int total_warps) {
-  const size_t pieces = max_segments(B, n, G, Hkv) + total_warps;
-  return a256(sizeof(AttnPlan)) + a256(sizeof(int32_t) * ((size_t)B + 1)) + a256(sizeof(float2) * pieces * 16) +
-         a256(sizeof(float) * pieces * 16 * D) + prefix_plan_bytes(n);
-}
-
-inline PagesWs pages_carve(void *ws, int B, int n, int G, int Hkv, int D, int total_warps) {
-  const size_t pieces = max_segments(B, n, G, Hkv) + total_warps;
-  char *p = static_cast<char *>(ws);
-  auto take = [&](size_t bytes) {
-    char *r = p;
-    p += a256(bytes);
-    return r;
-  };
-  PagesWs w{};
-  w.at.plan = reinterpret_cast<AttnPlan *>(take(sizeof(AttnPlan)));
-  w.at.pref = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * ((size_t)B + 1)));
-  w.at.part_ml = reinterpret_cast<float2 *>(take(sizeof(float2) * pieces * 16));
-  w.at.part_acc = reinterpret_cast<float *>(take(sizeof(float) * pieces * 16 * D));
-  if (n > 0) {
-    const size_t b = sizeof(int32_t) * ((size_t)n + 1);
-    w.pre.pages = reinterpret_cast<int32_t *>(take(b));
-    w.pre.blocks = reinterpret_cast<int32_t *>(take(b));
-    w.pre.first = reinterpret_cast<int32_t *>(take(b));
-  }
-  return w;
-}
-
-// The plan of the prefixes, by a CTA's first warp (a barrier follows at the caller's).
-// Offsets that decrease or leave [0, B] count as the largest before them, a
-// length outside the table as 0; both are recorded when `report` is set.
-__device__ __forceinline__ void plan_prefixes(const PagesArgs &a, const PrefixPlan &p, bool report) {
-  const int lane = threadIdx.x & 31, n = a.n_prefixes;
-  int most = 0, pages = 0, blocks = 0;
-  for (int i0 = 0; i0 <= n; i0 += 32) {
-    const int i = i0 + lane;
-    int o = i <= n ? (a.prefix_offsets ? a.prefix_offsets[i] : i * a.B) : 0;   // (no offsets: one prefix for all)
-    if (o < 0 || o > a.B) {
-      if (report) set_error(a.status, UMIM_ERR_INVALID_ARG);
-      o = 0;
-    }
-    int x = o;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) x = max(x, __shfl_up_sync(0xffffffffu, x, d));   // (lanes below d: their own)
-    x = max(x, most);
-    if (report && i <= n && x != o) set_error(a.status, UMIM_ERR_INVALID_ARG);
-    if (i <= n) p.first[i] = x;
-    most = __shfl_sync(0xffffffffu, x, 31);
-  }
-  __syncwarp();
-  for (int i0 = 0; i0 <= n; i0 += 32) {
-    const int i = i0 + lane;
-    int nb = 0, np = 0;
-    if (i < n) {
-      int L = a.prefix_lens[i];
-      if (L < 0 || (int64_t)L > (int64_t)a.max_prefix_pages * kPageSize) {
-        if (report) set_error(a.status, UMIM_ERR_INVALID_ARG);
-        L = 0;
-      }
-      nb = L > 0 ? ceil_div((p.first[i + 1] - p.first[i]) * a.G, 16) : 0;
-      np = nb * ceil_div(L, kPageSize);
-    }
-    int xb = nb, xp = np;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int yb = __shfl_up_sync(0xffffffffu, xb, d), yp = __shfl_up_sync(0xffffffffu, xp, d);
-      if (lane >= d) xb += yb, xp += yp;
-    }
-    if (i <= n) {
-      p.blocks[i] = blocks + xb - nb;
-      p.pages[i] = pages + xp - np;
-    }
-    blocks += __shfl_sync(0xffffffffu, xb, 31);
-    pages += __shfl_sync(0xffffffffu, xp, 31);
-  }
-}
-
-// the last i in [0, n) with at[i] * times <= x
-__device__ __forceinline__ int last_at_most(const int32_t *at, int n, int times, int x) {
-  int l = 0, h = n;
-  while (h - l > 1) {
-    const int m = (l + h) >> 1;
-    if (at[m] * times <= x) l = m;
-    else h = m;
-  }
-  return l;
-}
 
 // what a warp holds of a page: its layout in shared memory
 template <int D, int BITS>
@@ -240,6 +119,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   }
   __syncwarp();
   griddep_wait();
+  // the tensor cores' kernel, if that follows, starts as this one's CTAs leave; it reads nothing of this one's
+  if (SHARED) griddep_launch();
 
   const int G = a.G, Hkv = a.Hkv;
   const int32_t *pref = ws.at.pref;
@@ -247,11 +128,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   int own;   // pages of the sequences' own entries, of one KV head
   int32_t *plan = reinterpret_cast<int32_t *>(base + P::kRings);
   if (SHARED) {
-    pre.pages = plan;
-    pre.blocks = plan + (a.n_prefixes + 1);
-    pre.first = plan + 2 * (a.n_prefixes + 1);
+    pre = plan_at(plan, a.n_prefixes);
     plan += 3 * (a.n_prefixes + 1);
-    if (warp == 0) plan_prefixes(a, pre, blockIdx.x == 0);
+    if (warp == 0)
+      plan_prefixes(a, pre, blockIdx.x == 0, [&](int sequences, int len) {
+        const int rows = sequences * G, nb = rows > a.most_rows ? 0 : ceil_div(rows, 16);
+        return make_int2(nb, nb * ceil_div(len, kPageSize));
+      });
   }
   if (SHARED || a.smem_plan) {
     own = plan_prefix<kAttnWarps * 32>(a.seq_lens, a.B, a.max_pages, plan, blockIdx.x == 0, a.status);
@@ -675,7 +558,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
 // ---------------------------------------------------------------------------
 template <int D, int WPR>
 __global__ void __launch_bounds__(kCombineThreads)
-    shared_combine_kernel(PagesWs ws, int B, int n_prefixes, int Hq, int Hkv, int G, __nv_bfloat16 *out) {
+    shared_combine_kernel(PagesWs ws, bool tc, int B, int n_prefixes, int Hq, int Hkv, int G, __nv_bfloat16 *out) {
   constexpr int E = D / 32;
   constexpr int kWarps = kCombineThreads / 32, RPB = kWarps / WPR;   // rows per CTA
   __shared__ float s_m[kWarps], s_l[kWarps];
@@ -701,12 +584,26 @@ __global__ void __launch_bounds__(kCombineThreads)
     merge(b * Hkv + g, Hkv * first + g * n, n, h % G);
     const int i = last_at_most(ws.pre.first, n_prefixes, 1, b);
     if (b >= ws.pre.first[i] && b < ws.pre.first[i + 1]) {
-      const int nb = ws.pre.blocks[i + 1] - ws.pre.blocks[i];
+      const int nb = ws.pre.blocks[i + 1] - ws.pre.blocks[i], bi = b - ws.pre.first[i];
+      const int ns = tc ? ws.tc.blocks[i + 1] - ws.tc.blocks[i] : 0;
       if (nb > 0) {
-        const int x = (b - ws.pre.first[i]) * G + h % G;
+        const int x = bi * G + h % G;
         const int np = (ws.pre.pages[i + 1] - ws.pre.pages[i]) / nb;
         merge(Hkv * (B + ws.pre.blocks[i]) + g * nb + x / 16,
               Hkv * (ws.at.pref[B] + ws.pre.pages[i]) + (g * nb + x / 16) * np, np, x % 16);
+      } else if (ns > 0) {
+        // two pieces a CTA: of the pair's row tiles, or of one tile's even and odd key tiles
+        const int spt = tile_sequences(G), tiles = ceil_div(ws.pre.first[i + 1] - ws.pre.first[i], spt);
+        const int work = ws.tc.pages[i + 1] - ws.tc.pages[i], keys = work / tiles;
+        const int s = bi / spt / 2, row = bi % spt * G + h % G, width = 2 * s + 1 < tiles ? 2 : 1;
+        const int at = Hkv * ws.tc.pages[i] + g * work + s * 2 * keys, W = *ws.tc_W;
+        const int c0 = at / W, c1 = (at + (keys - 1) * width) / W;
+        const int64_t piece = 2 * (int64_t)(Hkv * ws.tc.blocks[i] + g * ns + s + c0);
+        any = true;
+        if (width == 2)
+          merge_pieces<E>(ws.tc_ml, ws.tc_acc, (piece + bi / spt % 2) * kTcRows + row, 2 * kTcRows, c1 - c0 + 1, sub, WPR, M, l, o);
+        else
+          merge_pieces<E>(ws.tc_ml, ws.tc_acc, piece * kTcRows + row, kTcRows, 2 * (c1 - c0 + 1), sub, WPR, M, l, o);
       }
     }
   }
@@ -744,12 +641,6 @@ __global__ void __launch_bounds__(kCombineThreads)
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-// a cache of either kind
-struct CacheView {
-  void *values, *scales;   // scales null: bf16
-  int n_layers, n_pages, n_kv_heads;
-};
-
 template <int D, int BITS>
 bool encode_maps(const CacheView &kv, CUtensorMap *values, CUtensorMap *scales) {
   using P = PageTile<D, BITS>;
@@ -784,7 +675,10 @@ umim_status run_pages(const CacheView &kv, PagesArgs a, void *out, void *workspa
   a.Hkv = kv.n_kv_heads;
   a.G = a.Hq / a.Hkv;
   const int total_warps = std::max(1, num_sms) * kAttnWarps;
-  const PagesWs ws = pages_carve(workspace, a.B, SHARED ? a.n_prefixes : 0, a.G, a.Hkv, D, total_warps);
+  PagesWs ws;
+  pages_carve(workspace, &ws, a.B, SHARED ? a.n_prefixes : 0, a.G, a.Hkv, D, num_sms);
+  const bool tc = SHARED && a.B * a.G > kTcMinRows;
+  a.most_rows = tc ? kTcMinRows : INT32_MAX;
   a.smem_plan = a.B <= kSmemPlanBatch ? 1 : 0;
   if (!a.smem_plan) {   // (never with prefixes: their batch is limited)
     trace_mark(stream, "attention.plan");
@@ -804,6 +698,10 @@ umim_status run_pages(const CacheView &kv, PagesArgs a, void *out, void *workspa
   if (launch_pdl(kern, dim3((unsigned)(total_warps / kAttnWarps)), dim3(kAttnWarps * 32), kBase + plan, stream, map,
                  scale_map, a, ws) != cudaSuccess)
     return UMIM_ERR_CUDA;
+  if (tc) {
+    trace_mark(stream, "attention.prefix");
+    if (!prefix_tc_launch(kv, D, a, ws, stream, num_sms)) return UMIM_ERR_CUDA;
+  }
   trace_mark(stream, "attention.combine");
   __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out);
   if constexpr (SHARED) {
@@ -813,8 +711,8 @@ umim_status run_pages(const CacheView &kv, PagesArgs a, void *out, void *workspa
     auto comb = wpr == 8 ? shared_combine_kernel<D, 8>
                 : wpr == 4 ? shared_combine_kernel<D, 4>
                 : wpr == 2 ? shared_combine_kernel<D, 2> : shared_combine_kernel<D, 1>;
-    if (launch_pdl(comb, dim3((unsigned)((a.B * a.Hq + rows - 1) / rows)), dim3(kCombineThreads), 0, stream, ws, a.B,
-                   a.n_prefixes, a.Hq, a.Hkv, a.G, o) != cudaSuccess)
+    if (launch_pdl(comb, dim3((unsigned)((a.B * a.Hq + rows - 1) / rows)), dim3(kCombineThreads), 0, stream, ws, tc,
+                   a.B, a.n_prefixes, a.Hq, a.Hkv, a.G, o) != cudaSuccess)
       return UMIM_ERR_CUDA;
   } else {
     const int wpr = combine_warps(1 + total_warps / std::max(1, a.B * a.Hkv));
@@ -833,11 +731,11 @@ umim_status run_pages(const CacheView &kv, PagesArgs a, void *out, void *workspa
 }  // namespace
 
 size_t decode_attention_kv8_workspace_bytes(int B, int Hkv, int D, int num_sms) {
-  return pages_ws_bytes(B, 0, 1, Hkv, D, std::max(1, num_sms) * kAttnWarps);
+  return pages_carve(nullptr, nullptr, B, 0, 1, Hkv, D, num_sms);
 }
 
 size_t decode_attention_shared_workspace_bytes(int B, int n, int Hq, int Hkv, int D, int num_sms) {
-  return pages_ws_bytes(B, std::max(1, n), Hq / Hkv, Hkv, D, std::max(1, num_sms) * kAttnWarps);
+  return pages_carve(nullptr, nullptr, B, std::max(1, n), Hq / Hkv, Hkv, D, num_sms);
 }
 
 umim_status decode_attention_kv8(const void *q, int Hq, const umim_paged_kv8 *kv, int layer, const int32_t *block_table,

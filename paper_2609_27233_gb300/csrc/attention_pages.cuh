@@ -1,0 +1,169 @@
+// What the kernels of attention over the 8-bit cache and over shared prefixes
+// have in common: their arguments, workspace, and the plan of the prefixes.
+#pragma once
+
+#include "attention.cuh"
+
+namespace umim {
+
+constexpr int kSharedMaxBatch = 4096;   // sequences and prefixes whose prefix sums lie in shared memory
+constexpr int kSharedMaxPrefixes = 512;
+
+struct PagesArgs {
+  const __nv_bfloat16 *q;
+  const int32_t *block_table, *seq_lens;
+  const int32_t *prefix_table, *prefix_lens, *prefix_offsets;   // shared prefixes only
+  int32_t B, Hq, Hkv, G, max_pages, n_pages, layer, n_layers;
+  int32_t n_prefixes, max_prefix_pages;
+  int32_t smem_plan;
+  int32_t most_rows;   // prefixes of more rows (sequence, query head of one KV head) are the tensor cores' (attention_prefix.cu)
+  float scale_log2;
+  int32_t *status;
+};
+
+// a cache of either kind
+struct CacheView {
+  void *values, *scales;   // scales null: bf16
+  int n_layers, n_pages, n_kv_heads;
+};
+
+// Where a prefix's work and rows are: exclusive sums over the prefixes, and the
+// offsets made to increase.  [n + 1] each.
+struct PrefixPlan {
+  int32_t *first;    // first sequence
+  int32_t *blocks;   // blocks of 16 rows; for the tensor cores, segments of one or two tiles of 128 rows
+  int32_t *pages;    // page visits of one KV head (pages x blocks); for the tensor cores, key tiles x row tiles
+};
+
+// ---------------------------------------------------------------------------
+// prefixes with many rows, on the tensor cores
+// ---------------------------------------------------------------------------
+constexpr int kTcRows = 128, kTcKeys = 128;
+// More rows than this go there: a tile of 128 rows costs the same with fewer rows in it.
+constexpr int kTcMinRows = 32;
+
+__host__ __device__ inline int tile_sequences(int G) { return kTcRows / G; }   // whole sequences a tile of rows
+
+// segments at most (of one KV head): pairs of row tiles, and a single one a prefix
+inline int64_t tc_max_segments(int B, int n, int G) {
+  return B / (2 * tile_sequences(G)) + std::min<int64_t>(n, (int64_t)B * G / (kTcMinRows + 1)) + 1;
+}
+
+struct PagesWs {
+  AttnWs at;
+  PrefixPlan pre, tc;
+  int32_t *tc_W;         // key tiles x row tiles of a CTA
+  float2 *tc_ml;         // [pieces][128]
+  float *tc_acc;         // [pieces][128][D]
+};
+
+// segments of a batch: (sequence, KV head), and (prefix, KV head, block of rows) at most
+inline size_t max_segments(int B, int n, int G, int Hkv) {
+  return (size_t)Hkv * (B + (n > 0 ? (size_t)n + (size_t)B * G / 16 : 0));
+}
+
+// n = 0: no prefixes.  With base null the sizes only; returns the bytes.
+inline size_t pages_carve(void *base, PagesWs *ws, int B, int n, int G, int Hkv, int D, int num_sms) {
+  char *p = static_cast<char *>(base);
+  size_t bytes = 0;
+  auto take = [&](size_t b) {
+    char *r = p + bytes;
+    bytes += a256(b);
+    return r;
+  };
+  const size_t pieces = max_segments(B, n, G, Hkv) + (size_t)std::max(1, num_sms) * kAttnWarps;
+  PagesWs w{};
+  w.at.plan = reinterpret_cast<AttnPlan *>(take(sizeof(AttnPlan)));
+  w.at.pref = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * ((size_t)B + 1)));
+  w.at.part_ml = reinterpret_cast<float2 *>(take(sizeof(float2) * pieces * 16));
+  w.at.part_acc = reinterpret_cast<float *>(take(sizeof(float) * pieces * 16 * D));
+  if (n > 0) {
+    const size_t b = sizeof(int32_t) * ((size_t)n + 1);
+    for (PrefixPlan *x : {&w.pre, &w.tc}) {
+      x->first = reinterpret_cast<int32_t *>(take(b));
+      x->blocks = reinterpret_cast<int32_t *>(take(b));
+      x->pages = reinterpret_cast<int32_t *>(take(b));
+    }
+    w.tc_W = reinterpret_cast<int32_t *>(take(sizeof(int32_t)));
+    if ((int64_t)B * G > kTcMinRows) {
+      const size_t tc = 2 * ((size_t)Hkv * tc_max_segments(B, n, G) + std::max(1, num_sms));
+      w.tc_ml = reinterpret_cast<float2 *>(take(sizeof(float2) * tc * kTcRows));
+      w.tc_acc = reinterpret_cast<float *>(take(sizeof(float) * tc * kTcRows * D));
+    }
+  }
+  if (ws) *ws = w;
+  return bytes;
+}
+
+// ---------------------------------------------------------------------------
+// plan
+// ---------------------------------------------------------------------------
+// The plan of the prefixes, by a CTA's first warp (a barrier follows at the
+// caller's).  Offsets that decrease or leave [0, B] count as the largest before
+// them, a length outside the table as 0; both are recorded when `report` is set.
+// work(rows' sequences, entries): (blocks, page visits).
+template <typename Work>
+__device__ __forceinline__ void plan_prefixes(const PagesArgs &a, const PrefixPlan &p, bool report, Work work) {
+  const int lane = threadIdx.x & 31, n = a.n_prefixes;
+  int most = 0, pages = 0, blocks = 0;
+  for (int i0 = 0; i0 <= n; i0 += 32) {
+    const int i = i0 + lane;
+    int o = i <= n ? (a.prefix_offsets ? a.prefix_offsets[i] : i * a.B) : 0;   // (no offsets: one prefix for all)
+    if (o < 0 || o > a.B) {
+      if (report) set_error(a.status, UMIM_ERR_INVALID_ARG);
+      o = 0;
+    }
+    int x = o;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) x = max(x, __shfl_up_sync(0xffffffffu, x, d));   // (lanes below d: their own)
+    x = max(x, most);
+    if (report && i <= n && x != o) set_error(a.status, UMIM_ERR_INVALID_ARG);
+    if (i <= n) p.first[i] = x;
+    most = __shfl_sync(0xffffffffu, x, 31);
+  }
+  __syncwarp();
+  for (int i0 = 0; i0 <= n; i0 += 32) {
+    const int i = i0 + lane;
+    int2 w = make_int2(0, 0);
+    if (i < n) {
+      const int L = a.prefix_lens[i];
+      if (L < 0 || (int64_t)L > (int64_t)a.max_prefix_pages * kPageSize) {
+        if (report) set_error(a.status, UMIM_ERR_INVALID_ARG);
+      } else if (L > 0) {
+        w = work(p.first[i + 1] - p.first[i], L);
+      }
+    }
+    int xb = w.x, xp = w.y;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int yb = __shfl_up_sync(0xffffffffu, xb, d), yp = __shfl_up_sync(0xffffffffu, xp, d);
+      if (lane >= d) xb += yb, xp += yp;
+    }
+    if (i <= n) {
+      p.blocks[i] = blocks + xb - w.x;
+      p.pages[i] = pages + xp - w.y;
+    }
+    blocks += __shfl_sync(0xffffffffu, xb, 31);
+    pages += __shfl_sync(0xffffffffu, xp, 31);
+  }
+}
+
+// the last i in [0, n) with at[i] * times <= x
+__device__ __forceinline__ int last_at_most(const int32_t *at, int n, int times, int x) {
+  int l = 0, h = n;
+  while (h - l > 1) {
+    const int m = (l + h) >> 1;
+    if (at[m] * times <= x) l = m;
+    else h = m;
+  }
+  return l;
+}
+
+// a plan in shared memory: [3][n + 1] from `mem` on
+__device__ __forceinline__ PrefixPlan plan_at(int32_t *mem, int n) {
+  return PrefixPlan{mem, mem + (n + 1), mem + 2 * (n + 1)};
+}
+
+bool prefix_tc_launch(const CacheView &kv, int D, const PagesArgs &a, const PagesWs &ws, cudaStream_t stream, int num_sms);
+
+}  // namespace umim

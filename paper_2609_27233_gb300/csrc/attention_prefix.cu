@@ -1,0 +1,588 @@
+// Attention of many query rows over a shared prefix, on the 5th-generation tensor
+// cores: the part of umim_decode_attention_shared that is no longer bound by the
+// cache's bytes.  The rows (sequence, query head) of a group that share a KV head
+// are the rows of a matrix Q, and
+//     S = Q K^T,   P = exp2(scale S - m),   O = P V,   l = sum P
+// over a range of the prefix's entries is one partial result (m, l, O) a row,
+// which the combine kernel (attention_pages.cu) joins with the row's others.
+//
+// Work: a row tile is 128 rows (whole sequences), a key tile 128 entries (8 pages).  A
+// segment is a pair of row tiles, or a single one, of a prefix and KV head;
+// (segment, key tile) pairs are flattened, weighted by their row tiles, and every
+// CTA of a persistent grid takes an equal contiguous range.  A CTA holds two slots,
+// each with S and O in tensor memory, four softmax warps (a thread a row) and an
+// issuing warp: the pair's row tiles over the same key tiles, or one row tile's even
+// and odd key tiles.  The slots take turns on the tensor cores (one's O += P V and
+// next S while the other's softmax runs), as two heads do in prefill.cu.
+//
+// P is taken as a bf16 number and a bf16 remainder, two products with V each (17
+// significant bits; one bf16 P would cost as much as the output's own rounding):
+// 512 + 1024 cycles of tensor cores a tile of 128 x 128 x 128.  P lies over the half of S
+// that it came from (64 columns of S: 32 of P, 32 of its remainder).  K and V are
+// read from the pages as they lie: K is K-major, V MN-major (64 columns of the head
+// dimension x 8 entries a swizzle atom), so nothing is transposed.
+//
+// 16-bit pages: two 128-byte boxes of 16 rows each for K and for V, straight into
+// the operands' place.  The last page is loaded from row n - 16 on where it holds n <
+// 16 entries: TMA reads rows before the first as zeros, so that nothing behind the
+// prefix's end is ever read; S is masked there.
+// 8-bit pages: e4m3 rows and scales into a ring, from which four warps make the bf16
+// operands, value * 2^e (exact), zeros behind the end.
+#include <cuda_fp16.h>
+
+#include "attention_pages.cuh"
+#include "kv8.cuh"
+#include "tmem.cuh"
+
+namespace umim {
+namespace {
+
+constexpr uint32_t kTcTmemCols = 512;   // S of the slots at 0 and 128, O at 256 and 384
+constexpr int kRawStages = 3;           // 8-bit: K and V tiles as they come, in turn
+
+// shared memory (bytes, every piece 1024-aligned but the scales)
+template <int D, int BITS>
+struct TcSmem {
+  static constexpr int kTile = 128 * D * 2;               // Q of a slot, K, V: D / 64 atoms of [128 rows][128 B]
+  static constexpr int kKStages = BITS == 8 ? 1 : 2, kVStages = 2;
+  static constexpr int kRaw = BITS == 8 ? 128 * D : 0;
+  static constexpr int kK = 2 * kTile;
+  static constexpr int kV = kK + kKStages * kTile;
+  static constexpr int kRawAt = kV + kVStages * kTile;
+  static constexpr int kScales = kRawAt + kRawStages * kRaw;              // [stage][8 pages][128 B], 16 used
+  static constexpr int kPlan = kScales + (BITS == 8 ? kRawStages * 8 * 128 : 0);
+  static constexpr int kMost = kPlan + 12 * (kSharedMaxPrefixes + 1) + 1024;
+};
+template <int BITS>
+constexpr int kTcThreads = BITS == 8 ? 480 : 352;   // warp 0 copies, 1-2 products, 3-10 softmax, 11-14 8-bit values
+
+// one CTA's part of a segment
+struct TcUnit {
+  int i, g, tile;     // prefix, KV head, first row tile
+  bool two;           // a pair of row tiles
+  int seg;            // segment, over all
+  int len;            // the prefix's entries
+  int t0, t1;         // key tiles
+};
+
+// The unit at position x of [x, end), and where the next one starts; false behind the last.
+__device__ __forceinline__ bool unit_at(const PagesArgs &a, const PrefixPlan &p, int &x, int end, TcUnit &u) {
+  while (x < end) {
+    u.i = last_at_most(p.pages, a.n_prefixes, a.Hkv, x);
+    const int work = p.pages[u.i + 1] - p.pages[u.i], ns = p.blocks[u.i + 1] - p.blocks[u.i];
+    u.len = a.prefix_lens[u.i];
+    const int keys = ceil_div(u.len, kTcKeys), tiles = work / keys;
+    int r = x - a.Hkv * p.pages[u.i];
+    u.g = r / work;
+    r -= u.g * work;
+    const int s = r / (2 * keys);
+    u.tile = 2 * s;
+    u.two = 2 * s + 1 < tiles;
+    u.seg = a.Hkv * p.blocks[u.i] + u.g * ns + s;
+    const int width = u.two ? 2 : 1, at = x - (r - 2 * s * keys), stop = min(end, at + keys * width);
+    u.t0 = ceil_div(x - at, width);
+    u.t1 = min(keys, ceil_div(stop - at, width));
+    x = stop;
+    if (u.t0 < u.t1) return true;
+  }
+  return false;
+}
+
+// a tile's 32 columns from x on whose positions lie in [lo, hi)
+__device__ __forceinline__ uint32_t columns_in(int x, int lo, int hi) {
+  lo = max(lo - x, 0), hi = min(hi - x, 32);
+  return hi > lo ? (~0u >> (32 - (hi - lo))) << lo : 0u;
+}
+
+// D x 128 keys, MN-major in 128-byte swizzle atoms of 64 columns x 8 keys: 1024 bytes to
+// the next 8 keys, kTcKeys * 128 to the next 64 columns
+__device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t smem_addr) {
+  return sw128_kmajor_desc(smem_addr) + ((uint64_t)(kTcKeys * 128 / 16 - 1) << 16);   // (the K-major one's field is 1)
+}
+constexpr uint32_t kBMnMajor = 1u << 16;   // instruction descriptor: B is MN-major
+
+template <int D, int BITS>
+__global__ void __launch_bounds__(kTcThreads<BITS>, 1)
+    prefix_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap kv_map,
+                     const __grid_constant__ CUtensorMap scale_map, PagesArgs a, PagesWs ws) {
+  using L = TcSmem<D, BITS>;
+  constexpr int DA = D / 64;
+  constexpr int KS = L::kKStages, VS = L::kVStages;
+  extern __shared__ __align__(1024) uint8_t tc_raw[];
+  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2],
+      p_full[2][2], pv_done[2], o_free[2], turn[2], mma_done[2], raw_full[kRawStages], raw_empty[kRawStages];
+  __shared__ uint32_t tmem_base;
+  __shared__ int s_abort;
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(tc_raw) + 1023) & ~uintptr_t(1023));
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&k_full[s], BITS == 8 ? 4 : 1);
+      mbar_init(&k_empty[s], 2);   // read by both slots' products, or twice by one's
+      mbar_init(&v_full[s], BITS == 8 ? 4 : 1);
+      mbar_init(&v_empty[s], 2);
+      mbar_init(&q_full[s], 1);
+      mbar_init(&q_empty[s], 1);     // a unit's S products have read the slot's Q
+      mbar_init(&s_full[s], 1);
+      mbar_init(&p_full[s][0], 4);   // keys 0-63 of P ready (the slot's four softmax warps)
+      mbar_init(&p_full[s][1], 4);   // keys 64-127
+      mbar_init(&pv_done[s], 1);     // a tile's P V product has landed
+      mbar_init(&o_free[s], 4);      // a unit's epilogue has read O
+      mbar_init(&turn[s], 1);        // the other slot's products are issued
+      mbar_init(&mma_done[s], 1);
+    }
+    for (int s = 0; s < kRawStages; ++s) {
+      mbar_init(&raw_full[s], 1);
+      mbar_init(&raw_empty[s], 4);
+    }
+    fence_mbar_init();
+    prefetch_tensormap(&q_map);
+    prefetch_tensormap(&kv_map);
+    if (BITS == 8) prefetch_tensormap(&scale_map);
+  }
+  if (warp == 1) {
+    tmem_alloc(&tmem_base, kTcTmemCols);
+    tmem_relinquish();
+  }
+  const PrefixPlan plan = plan_at(reinterpret_cast<int32_t *>(smem + L::kPlan), a.n_prefixes);
+  const int spt = tile_sequences(a.G);   // sequences of a row tile
+  // Nothing here waits for the kernel before: this one's inputs and workspace were
+  // free when that one let it start (its own wait was over), and it waits at its end
+  // for that one, for the combine kernel behind both.
+  if (warp == 2)
+    plan_prefixes(a, plan, false, [&](int sequences, int len) {   // (the kernel before reports)
+      const int tiles = sequences * a.G > a.most_rows ? ceil_div(sequences, spt) : 0;
+      return make_int2((tiles + 1) / 2, tiles * ceil_div(len, kTcKeys));
+    });
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base;
+  const int total = a.Hkv * plan.pages[a.n_prefixes];
+  const int W = max(2, ceil_div(total, (int)gridDim.x));   // (2: every CTA between a segment's first and last has a tile of it)
+  const int start = (int)min((int64_t)blockIdx.x * W, (int64_t)total), end = min(start + W, total);
+  if (blockIdx.x == 0) {   // for the combine kernel
+    for (int i = threadIdx.x; i <= a.n_prefixes; i += kTcThreads<BITS>) {
+      ws.tc.blocks[i] = plan.blocks[i];
+      ws.tc.pages[i] = plan.pages[i];
+    }
+    if (threadIdx.x == 0) *ws.tc_W = W;
+  }
+
+  // a warp that gave up tells the others, so that no wait is left to time out on its own
+  auto aborted = [&]() { return *reinterpret_cast<volatile int *>(&s_abort) != 0; };
+  auto give_up = [&]() {
+    set_error(a.status, UMIM_ERR_TIMEOUT);
+    *reinterpret_cast<volatile int *>(&s_abort) = 1;
+  };
+  // the whole warp waits, and goes on only if all of it saw the phase
+  auto wwait = [&](uint64_t *m, uint32_t parity) {
+    return __all_sync(0xffffffffu, !aborted() && mbar_wait(m, parity)) != 0;
+  };
+
+  if (warp == 0) {
+    // ---- copies: lanes 0-7 a page each (two boxes of it in lanes 0-15 for 16-bit
+    // pages of 128 columns), lanes 8-15 the scales of 8-bit pages ----
+    int nq = 0, pos = 0;   // units, and key tiles
+    bool ok = true;
+    TcUnit u;
+    for (int x = start; ok && unit_at(a, plan, x, end, u);) {
+      const int n_pages = ceil_div(u.len, kPageSize), part = u.len % kPageSize;
+      const int32_t *table = a.prefix_table + (int64_t)u.i * a.max_prefix_pages;
+      for (int t = 0; t < 2 && ok; ++t) {
+        if (nq > 0) ok = wwait(&q_empty[t], (uint32_t)(nq - 1) & 1u);
+        if (ok && lane == 0) {
+          mbar_arrive_expect_tx(&q_full[t], DA * spt * a.G * 128);
+#pragma unroll
+          for (int d = 0; d < DA; ++d)
+            tma_load_4d(smem + t * L::kTile + d * (kTcRows * 128), &q_map, &q_full[t], d * 64, 0, u.g,
+                        plan.first[u.i] + (u.tile + (u.two ? t : 0)) * spt);
+        }
+      }
+      ++nq;
+      const int pg = lane & 7;
+      for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
+        const int at = j * 8 + pg;
+        int c = a.n_layers * a.n_pages;   // a coordinate past the tensor's last page: the copy reads zeros
+        if (at < n_pages && in_bounds(at, a.max_prefix_pages, a.status, kSitePrefixTable)) {
+          const int page = table[at];
+          if (page >= 0 && page < a.n_pages) c = a.layer * a.n_pages + page;
+          else set_error(a.status, UMIM_ERR_INVALID_ARG);
+        }
+        for (int kv = 0; kv < 2 && ok; ++kv) {
+          if constexpr (BITS == 16) {
+            const int s = pos & 1;
+            uint64_t *full = kv ? &v_full[s] : &k_full[s];
+            ok = wwait(kv ? &v_empty[s] : &k_empty[s], (uint32_t)(pos >> 1 & 1) ^ 1u);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_expect_tx(full, L::kTile);
+            __syncwarp();
+            if (lane < 8 * DA)
+              tma_load_5d(smem + (kv ? L::kV : L::kK) + s * L::kTile + (lane >> 3) * (kTcKeys * 128) + pg * (kPageSize * 128),
+                          &kv_map, full, (lane >> 3) * 64, at == n_pages - 1 && part ? part - kPageSize : 0, u.g, kv, c,
+                          policy_evict_last());
+          } else {
+            const int item = 2 * pos + kv, s = item % kRawStages;
+            ok = wwait(&raw_empty[s], (uint32_t)(item / kRawStages & 1) ^ 1u);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_expect_tx(&raw_full[s], L::kRaw + 8 * kPageSize);
+            __syncwarp();
+            if (lane < 8)
+              tma_load_5d(smem + L::kRawAt + s * L::kRaw + pg * (kPageSize * D), &kv_map, &raw_full[s], 0, 0, u.g, kv, c,
+                          policy_evict_last());
+            else if (lane < 16)
+              tma_load_4d(smem + L::kScales + (s * 8 + pg) * 128, &scale_map, &raw_full[s], 0, u.g, kv, c);
+          }
+        }
+      }
+    }
+    if (!ok) give_up();
+    // copies still in flight when a consumer gave up: wait for them (bounded).  The barriers
+    // only count what was armed, so a phase that has completed returns at once.
+    if (!ok) {
+      if constexpr (BITS == 16) {
+        for (int i = max(0, pos - 2); i <= pos; ++i) {
+          mbar_wait_for(&k_full[i & 1], (uint32_t)(i >> 1 & 1), 1000000);
+          mbar_wait_for(&v_full[i & 1], (uint32_t)(i >> 1 & 1), 1000000);
+        }
+      } else {
+        for (int i = max(0, 2 * pos - kRawStages); i <= 2 * pos + 1; ++i)
+          mbar_wait_for(&raw_full[i % kRawStages], (uint32_t)(i / kRawStages & 1), 1000000);
+      }
+      for (int t = 0; t < 2; ++t)
+        if (nq > 0) mbar_wait_for(&q_full[t], (uint32_t)(nq - 1) & 1u, 1000000);
+    }
+  } else if (warp <= 2) {
+    // ---- the products of slot t, turn by turn: O += P V of its tile before as the halves of P
+    // become ready, then S = Q K^T of its next tile once that has landed (P lies over S) ----
+    const int t = warp - 1;
+    if (elect_one()) {
+      constexpr uint32_t idesc_s = idesc_f32acc(kTcRows, kTcKeys, false);
+      constexpr uint32_t idesc_o = idesc_f32acc(kTcRows, D, false) | kBMnMajor;
+      const uint32_t t_s = tmem + t * kTcKeys, t_o = tmem + 256 + t * 128;
+      const uint64_t q_desc = sw128_kmajor_desc(smem_u32(smem) + t * L::kTile);
+      int turns = 0, ns = 0, nu = 0;   // turns taken, S issued, units with a tile of this slot
+      int pend = -1;                   // ring position of the tile whose P V is due
+      bool pend_first = false, pend_two = false;
+      bool landing = false;            // a P V product was issued and not waited for
+      auto commits = [&](uint64_t *bar, bool two) {   // the slot's part of a stage's two readers, or both
+        tc_commit(bar);
+        if (!two) tc_commit(bar);
+      };
+      // rp: ring position of the tile whose S is next, -1 for none; nq: the unit's Q
+      auto take_turn = [&](int rp, bool first, bool last, bool two, int nq) {
+        const bool due = pend >= 0;
+        const uint32_t pt = (uint32_t)(ns - 1) & 1u;
+        if (due) {
+          if (aborted() || !mbar_wait(&v_full[pend & 1], (uint32_t)(pend >> 1 & 1)) || !mbar_wait(&p_full[t][0], pt) ||
+              (pend_first && nu > 1 && !mbar_wait(&o_free[t], (uint32_t)nu & 1u)))
+            return false;
+        }
+        if ((t == 1 || turns > 0) && (aborted() || !mbar_wait(&turn[t], (uint32_t)(turns + t + 1) & 1u))) return false;
+        ++turns;
+        if (due) {
+          const uint64_t v_desc = sw128_mnmajor_desc(smem_u32(smem + L::kV + (pend & 1) * L::kTile));
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (h == 1 && !mbar_wait(&p_full[t][1], pt)) return false;
+            tc_fence_after();
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)   // 16 keys: a page
+                tc_mma_ts(t_o, t_s + h * 64 + part * 32 + kk * 8, v_desc + (h * 4 + kk) * (kPageSize * 128 / 16), idesc_o,
+                          !pend_first || h || part || kk ? 1u : 0u);
+          }
+          tc_commit(&pv_done[t]);
+          commits(&v_empty[pend & 1], pend_two);
+          pend = -1;
+          landing = true;
+        }
+        if (rp < 0) {
+          mbar_arrive(&turn[t ^ 1]);
+          return true;
+        }
+        if (aborted() || !mbar_wait(&k_full[rp % KS], (uint32_t)(rp / KS & 1)) ||
+            (first && !mbar_wait(&q_full[t], (uint32_t)nq & 1u)) || (landing && !mbar_wait(&pv_done[t], pt)))
+          return false;
+        landing = false;
+        const uint64_t k_desc = sw128_kmajor_desc(smem_u32(smem + L::kK + rp % KS * L::kTile));
+        tc_fence_after();
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          tc_mma_bf16(t_s, q_desc + (kk >> 2) * (kTcRows * 8) + (kk & 3) * 2,
+                      k_desc + (kk >> 2) * (kTcKeys * 8) + (kk & 3) * 2, idesc_s, kk != 0 ? 1u : 0u);
+        tc_commit(&s_full[t]);
+        mbar_arrive(&turn[t ^ 1]);
+        commits(&k_empty[rp % KS], two);
+        if (last) tc_commit(&q_empty[t]);   // the unit's S products have read Q
+        pend = rp;
+        pend_first = first;
+        pend_two = two;
+        nu += first;
+        ++ns;
+        return true;
+      };
+      bool ok = true;
+      int pos = 0, nq = 0;
+      TcUnit u;
+      for (int x = start; ok && unit_at(a, plan, x, end, u); ++nq) {
+        const int n = u.t1 - u.t0;
+        if (u.two) {
+          for (int i = 0; i < n && ok; ++i) ok = take_turn(pos + i, i == 0, i == n - 1, true, nq);
+        } else {
+          for (int i = t; i - t < n && ok; i += 2) ok = take_turn(i < n ? pos + i : -1, i == t, i + 2 >= n, false, nq);
+          if (ok && t >= n) {   // no tile of this slot's: its Q is in nobody's way
+            ok = mbar_wait(&q_full[t], (uint32_t)nq & 1u);
+            if (ok) mbar_arrive(&q_empty[t]);
+          }
+        }
+        pos += n;
+      }
+      if (ok && nq > 0) ok = take_turn(-1, false, false, false, 0);
+      if (!ok) give_up();
+      // every product this thread issued has finished before tensor memory is released
+      tc_commit(&mma_done[t]);
+      mbar_wait_for(&mma_done[t], 0, kWaitLimitNs);
+    }
+    __syncwarp();
+  } else if (warp <= 10) {
+    // ---- softmax and partial results of slot t: four warps, thread = query row ----
+    const int t = (warp - 3) >> 2;
+    const int quad = warp & 3;                 // tensor-memory lanes this warp may access
+    const int r = quad * 32 + lane;            // row within the tile
+    const uint32_t t_s = tmem + ((uint32_t)(quad * 32) << 16) + t * kTcKeys;
+    const uint32_t t_o = tmem + ((uint32_t)(quad * 32) << 16) + 256 + t * 128;
+    const float sl2 = a.scale_log2;
+    bool ok = true;
+    int ns = 0;
+    TcUnit u;
+    for (int x = start; ok && unit_at(a, plan, x, end, u);) {
+      const int row_tile = u.tile + (u.two ? t : 0), seq = plan.first[u.i] + row_tile * spt + r / a.G;
+      const bool live = r < spt * a.G && seq < plan.first[u.i + 1];
+      const bool any = __any_sync(0xffffffffu, live);   // (a warp without rows only keeps the others going)
+      float m_run = -INFINITY, l_run = 0.f;             // running max (log2 units, moved in steps > 8) and row sum
+      int mine = 0;                                     // tiles
+      for (int j = u.t0 + (u.two ? 0 : t); j < u.t1; j += u.two ? 1 : 2, ++mine, ++ns) {
+        ok = wwait(&s_full[t], (uint32_t)ns & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        if (!any) {
+          tc_fence_before();
+          __syncwarp();
+          if (elect_one()) mbar_arrive(&p_full[t][0]), mbar_arrive(&p_full[t][1]);
+          continue;
+        }
+        const int rem = u.len - j * kTcKeys;   // keys from here on
+        auto mask = [&](float (&s)[64], int x0) {
+          if (rem >= kTcKeys) return;
+          const int full = rem / kPageSize * kPageSize, part = rem % kPageSize;
+#pragma unroll
+          for (int x = 0; x < 64; x += 32) {
+            // 16-bit pages: the last page's entries are its last rows
+            const uint32_t bits = BITS == 8 ? columns_in(x0 + x, 0, rem)
+                                            : columns_in(x0 + x, 0, full) | columns_in(x0 + x, full + kPageSize - part, full + kPageSize);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) s[x + c] = bits >> c & 1u ? s[x + c] : -INFINITY;
+          }
+        };
+        auto largest = [&](const float (&s)[64]) {
+          float m4[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+          for (int c = 4; c < 64; c += 2) m4[(c >> 1) & 3] = max3f(m4[(c >> 1) & 3], s[c], s[c + 1]);
+          return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        };
+        float s[64];
+        tmem_ld_32x32b_x64(t_s + 64, s);
+        mask(s, 64);
+        float mx = largest(s);
+        tmem_ld_32x32b_x64(t_s, s);
+        mask(s, 0);
+        mx = fmaxf(mx, largest(s)) * sl2;
+        // move the running max only when it grows by more than 2^8
+        const bool grow = mx > m_run + 8.f;
+        float alpha = 1.f;
+        if (grow) {
+          alpha = (m_run == -INFINITY) ? 0.f : ex2_approx(m_run - mx);
+          m_run = mx;
+          l_run *= alpha;
+        }
+        const float nm = (m_run == -INFINITY) ? 0.f : -m_run;
+        const float2 sl2x2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm);
+        float2 la = make_float2(0.f, 0.f), lb = la;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (h == 1) {
+            tmem_ld_32x32b_x64(t_s + 64, s);
+            mask(s, 64);
+          }
+          float hi[32], lo[32];   // P (<= 2^8) in bf16 pairs, and what that leaves
+#pragma unroll
+          for (int c = 0; c < 64; c += 2) {
+            const float2 x = __ffma2_rn(make_float2(s[c], s[c + 1]), sl2x2, nm2);
+            const float2 y = make_float2(ex2_approx(x.x), ex2_approx(x.y));   // masked (-inf): 0
+            if (c & 2) lb = __fadd2_rn(lb, y);
+            else la = __fadd2_rn(la, y);
+            const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
+            const uint32_t p = *reinterpret_cast<const uint32_t *>(&b);
+            const __nv_bfloat162 d = __floats2bfloat162_rn(y.x - __uint_as_float(p << 16), y.y - __uint_as_float(p & 0xffff0000u));
+            hi[c / 2] = __uint_as_float(p);
+            lo[c / 2] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&d));
+          }
+          // O is rescaled before the tile's first product (the tile before's has landed: S followed it)
+          if (h == 0 && mine > 0 && __any_sync(0xffffffffu, grow)) {
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              float o[32];
+              tmem_ld_32x32b_x32(t_o + c * 32, o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] *= alpha;
+              tmem_st_32x32b_x32(t_o + c * 32, o);
+            }
+          }
+          // over the S columns they come from, which this thread has read
+          tmem_st_32x32b_x32(t_s + h * 64, hi);
+          tmem_st_32x32b_x32(t_s + h * 64 + 32, lo);
+          tc_fence_before();
+          __syncwarp();
+          if (elect_one()) mbar_arrive(&p_full[t][h]);
+        }
+        const float2 lab = __fadd2_rn(la, lb);
+        l_run += lab.x + lab.y;
+      }
+      if (!ok) break;
+      // the unit's partial result
+      const int64_t piece = 2 * ((int64_t)u.seg + blockIdx.x) + t, at = piece * kTcRows + r;
+      const bool store = live && in_bounds(piece, 2 * ((int64_t)a.Hkv * plan.blocks[a.n_prefixes] + gridDim.x), a.status,
+                                           kSitePrefixPiece);
+      if (store) ws.tc_ml[at] = make_float2(m_run, l_run);
+      float4 *dst = reinterpret_cast<float4 *>(ws.tc_acc + at * D);
+      if (mine > 0) {
+        ok = wwait(&pv_done[t], (uint32_t)(ns - 1) & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        if (any) {
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            float o[32];
+            tmem_ld_32x32b_x32(t_o + c * 32, o);
+            if (store)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) dst[c * 8 + i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&o_free[t]);
+      } else if (store) {
+        for (int i = 0; i < D / 4; ++i) dst[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    }
+    if (!ok) give_up();
+  } else {
+    // ---- 8-bit values to bf16 operands: a warp 32 keys, D / 8 lanes a key ----
+    if constexpr (BITS == 8) {
+      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+      const int w = warp - 11, part = lane % kLanes;
+      bool ok = true;
+      int pos = 0;
+      TcUnit u;
+      for (int x = start; ok && unit_at(a, plan, x, end, u);) {
+        for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
+          const int rem = u.len - j * kTcKeys;
+          for (int kv = 0; kv < 2; ++kv) {
+            const int item = 2 * pos + kv, s = item % kRawStages, stages = kv ? VS : KS, to = pos % stages;
+            ok = wwait(&raw_full[s], (uint32_t)(item / kRawStages & 1)) &&
+                 wwait(kv ? &v_empty[to] : &k_empty[to], (uint32_t)(pos / stages & 1) ^ 1u);
+            if (!ok) break;
+            const uint8_t *raw = smem + L::kRawAt + s * L::kRaw, *scales = smem + L::kScales + s * 8 * 128;
+            uint8_t *dst = smem + (kv ? L::kV : L::kK) + to * L::kTile + (part >> 3) * (kTcKeys * 128);
+#pragma unroll 4
+            for (int i = 0; i < 32; i += kAtOnce) {
+              const int key = w * 32 + i + lane / kLanes;
+              const uint2 v = *reinterpret_cast<const uint2 *>(raw + key * D + part * 8);
+              const float f = e8m0_value(scales[(key >> 4) * 128 + (key & 15)]);
+              const __nv_bfloat162 f2 = __floats2bfloat162_rn(f, f);   // exact
+              uint32_t out[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t h = f16x2_of_e4m3x2((e < 2 ? v.x : v.y) >> (e & 1) * 16);
+                const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+                const __nv_bfloat162 b = __hmul2(__floats2bfloat162_rn(y.x, y.y), f2);
+                out[e] = key < rem ? *reinterpret_cast<const uint32_t *>(&b) : 0u;
+              }
+              *reinterpret_cast<uint4 *>(dst + key * 128 + (((part & 7) ^ (key & 7)) << 4)) =
+                  make_uint4(out[0], out[1], out[2], out[3]);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (elect_one()) {
+              mbar_arrive(kv ? &v_full[to] : &k_full[to]);
+              mbar_arrive(&raw_empty[s]);
+            }
+          }
+        }
+      }
+      if (!ok) give_up();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTcTmemCols);
+  }
+  griddep_wait();
+}
+
+template <int D, int BITS>
+bool launch(const CacheView &kv, const PagesArgs &a, const PagesWs &ws, cudaStream_t stream, int num_sms) {
+  using L = TcSmem<D, BITS>;
+  static_assert(L::kMost + 1024 <= 232448, "shared memory of a CTA");
+  EncodeTiledFn enc = get_encode_tiled();
+  if (!enc) return false;
+  CUtensorMap q_map, kv_map, scale_map;
+  const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+  const cuuint64_t H = kv.n_kv_heads, N = (cuuint64_t)kv.n_layers * (cuuint64_t)kv.n_pages, row = D * BITS / 8, G = a.G;
+  const cuuint64_t q_dims[4] = {(cuuint64_t)D, G, H, (cuuint64_t)a.B};
+  const cuuint64_t q_strides[3] = {D * 2, G * D * 2, H * G * D * 2};
+  const cuuint32_t q_box[4] = {64, (cuuint32_t)G, 1, (cuuint32_t)tile_sequences(a.G)};
+  if (enc(&q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<__nv_bfloat16 *>(a.q), q_dims, q_strides, q_box, one,
+          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return false;
+  const cuuint64_t dims[5] = {(cuuint64_t)D, 16, H, 2, N};
+  const cuuint64_t strides[4] = {row, 16 * row, H * 16 * row, 2 * H * 16 * row};
+  const cuuint32_t box[5] = {BITS == 8 ? (cuuint32_t)D : 64, 16, 1, 1, 1};
+  if (enc(&kv_map, BITS == 8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, kv.values, dims,
+          strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+          BITS == 8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return false;
+  scale_map = kv_map;
+  if (BITS == 8) {
+    const cuuint64_t sdims[4] = {16, H, 2, N}, sstrides[3] = {16, 16 * H, 32 * H};
+    const cuuint32_t sbox[4] = {16, 1, 1, 1};
+    if (enc(&scale_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, kv.scales, sdims, sstrides, sbox, one,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return false;
+  }
+  auto kern = prefix_tc_kernel<D, BITS>;
+  if (!allow_smem(kern, L::kMost)) return false;
+  const size_t smem = L::kPlan + 1024 + 12 * ((size_t)a.n_prefixes + 1);
+  return launch_pdl(kern, dim3((unsigned)std::max(1, num_sms)), dim3(kTcThreads<BITS>), smem, stream, q_map, kv_map,
+                    scale_map, a, ws) == cudaSuccess;
+}
+
+}  // namespace
+
+bool prefix_tc_launch(const CacheView &kv, int D, const PagesArgs &a, const PagesWs &ws, cudaStream_t stream, int num_sms) {
+  if (kv.scales == nullptr)
+    return D == 128 ? launch<128, 16>(kv, a, ws, stream, num_sms) : launch<64, 16>(kv, a, ws, stream, num_sms);
+  return D == 128 ? launch<128, 8>(kv, a, ws, stream, num_sms) : launch<64, 8>(kv, a, ws, stream, num_sms);
+}
+
+}  // namespace umim

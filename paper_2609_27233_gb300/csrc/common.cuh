@@ -82,7 +82,9 @@ enum DebugSite : int32_t {
   kSiteKv8Src = 30,
   kSitePagesTable = 31,
   kSitePagesPiece = 32,
-  kSiteCount = 33
+  kSitePrefixTable = 33,
+  kSitePrefixPiece = 34,
+  kSiteCount = 35
 };
 
 // true when 0 <= i < n; in the debug build a false result is recorded
