@@ -121,13 +121,10 @@ static __global__ void __launch_bounds__(kPlanThreadsA)
 // ---------------------------------------------------------------------------
 constexpr int kCombineThreads = 256;
 
-// Merges the n partial results at rows first, first + stride, ... of a workspace, those that
-// warp `sub` of `step` takes, into a running (M, l, o); a lane holds E columns of o.
-template <int E>
-__device__ __forceinline__ void merge_pieces(const float2 *part_ml, const float *part_acc, int64_t first, int64_t stride,
-                                             int n, int sub, int step, float &M, float &l, float (&o)[E]) {
-  constexpr int D = 32 * E;
-  const int lane = threadIdx.x & 31;
+// Merges n partial results, those that warp `sub` of `step` takes, into a running (M, l, o);
+// a lane holds E columns of o.  ml(i), acc(i): where result i's (m, l) and this lane's columns are.
+template <int E, typename Ml, typename Acc>
+__device__ __forceinline__ void merge_pieces(int n, int sub, int step, float &M, float &l, float (&o)[E], Ml ml_of, Acc acc_of) {
   // pieces whose loads are in flight together: one at a time, a row of 76 pieces
   // (long context, 16.4 us with eight warps a row) waits for memory ten times over;
   // four at a time 8.3 us
@@ -137,17 +134,17 @@ __device__ __forceinline__ void merge_pieces(const float2 *part_ml, const float 
     float av[U][E];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t at = first + (int64_t)(pc + u * step) * stride;
       ml[u] = make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int e = 0; e < E; ++e) av[u][e] = 0.f;
       if (pc + u * step < n) {
-        ml[u] = part_ml[at];
+        ml[u] = *ml_of(pc + u * step);
+        const float *src = acc_of(pc + u * step);
         if constexpr (E == 4) {
-          const float4 f = *reinterpret_cast<const float4 *>(part_acc + at * D + lane * E);
+          const float4 f = *reinterpret_cast<const float4 *>(src);
           av[u][0] = f.x, av[u][1] = f.y, av[u][2] = f.z, av[u][3] = f.w;
         } else {
-          const float2 f = *reinterpret_cast<const float2 *>(part_acc + at * D + lane * E);
+          const float2 f = *reinterpret_cast<const float2 *>(src);
           av[u][0] = f.x, av[u][1] = f.y;
         }
       }
@@ -170,6 +167,16 @@ __device__ __forceinline__ void merge_pieces(const float2 *part_ml, const float 
     }
     M = nm;
   }
+}
+
+// the same for `n` consecutive pieces of 16 rows from row `first` on
+template <int E>
+__device__ __forceinline__ void merge_rows(const AttnWs &ws, int64_t first, int n, int sub, int step, float &M, float &l,
+                                           float (&o)[E]) {
+  const float2 *ml = ws.part_ml + first;
+  const float *acc = ws.part_acc + first * (32 * E) + (threadIdx.x & 31) * E;
+  merge_pieces<E>(n, sub, step, M, l, o, [&](int i) { return ml + (int64_t)i * 16; },
+                  [&](int i) { return acc + (int64_t)i * (16 * 32 * E); });
 }
 
 template <int D, int WPR>
@@ -198,7 +205,7 @@ __global__ void __launch_bounds__(kCombineThreads)
   float M = -INFINITY, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  merge_pieces<E>(ws.part_ml, ws.part_acc, (int64_t)p0 * 16 + row, 16, p1 - p0, sub, WPR, M, l, o);
+  merge_rows<E>(ws, (int64_t)p0 * 16 + row, p1 - p0, sub, WPR, M, l, o);
   if constexpr (WPR > 1) {
     if (lane == 0) {
       s_m[warp] = M;

@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(kCombineThreads)
       if (n <= 0) return;
       any = true;
       const int w0 = at / W, w1 = (at + n - 1) / W;
-      merge_pieces<E>(ws.at.part_ml, ws.at.part_acc, (int64_t)(seg + w0) * 16 + row, 16, w1 - w0 + 1, sub, WPR, M, l, o);
+      merge_rows<E>(ws.at, (int64_t)(seg + w0) * 16 + row, w1 - w0 + 1, sub, WPR, M, l, o);
     };
     const int first = ws.at.pref[b], n = ws.at.pref[b + 1] - first;
     merge(b * Hkv + g, Hkv * first + g * n, n, h % G);
@@ -600,10 +600,10 @@ __global__ void __launch_bounds__(kCombineThreads)
         const int c0 = at / W, c1 = (at + (keys - 1) * width) / W;
         const int64_t piece = 2 * (int64_t)(Hkv * ws.tc.blocks[i] + g * ns + s + c0);
         any = true;
-        if (width == 2)
-          merge_pieces<E>(ws.tc_ml, ws.tc_acc, (piece + bi / spt % 2) * kTcRows + row, 2 * kTcRows, c1 - c0 + 1, sub, WPR, M, l, o);
-        else
-          merge_pieces<E>(ws.tc_ml, ws.tc_acc, piece * kTcRows + row, kTcRows, 2 * (c1 - c0 + 1), sub, WPR, M, l, o);
+        const int64_t from = piece + (width == 2 ? bi / spt % 2 : 0);
+        merge_pieces<E>((c1 - c0 + 1) * (3 - width), sub, WPR, M, l, o,
+                        [&](int x) { return ws.tc_ml + (from + x * width) * kTcRows + row; },
+                        [&](int x) { return ws.tc_acc + tc_acc_at<D>(from + x * width, row, lane * E); });
       }
     }
   }

@@ -54,8 +54,17 @@ struct PagesWs {
   PrefixPlan pre, tc;
   int32_t *tc_W;         // key tiles x row tiles of a CTA
   float2 *tc_ml;         // [pieces][128]
-  float *tc_acc;         // [pieces][128][D]
+  float *tc_acc;         // [pieces][D / 8][128][8]
 };
+
+// Where column c of a row of a tensor-core kernel's piece is.  A warp there holds a row
+// a lane and stores eight columns of its 32 rows at once, a kilobyte in one piece; the
+// combine kernel reads whole 32-byte sectors.  (Rows of D columns one behind another
+// took 32 lines a store: 4 us of a call of 37.)
+template <int D>
+__host__ __device__ __forceinline__ int64_t tc_acc_at(int64_t piece, int row, int c) {
+  return piece * (kTcRows * D) + (c / 8) * (kTcRows * 8) + row * 8 + c % 8;
+}
 
 // segments of a batch: (sequence, KV head), and (prefix, KV head, block of rows) at most
 inline size_t max_segments(int B, int n, int G, int Hkv) {

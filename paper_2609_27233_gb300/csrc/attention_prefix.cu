@@ -94,6 +94,12 @@ __device__ __forceinline__ uint32_t columns_in(int x, int lo, int hi) {
   return hi > lo ? (~0u >> (32 - (hi - lo))) << lo : 0u;
 }
 
+__device__ __forceinline__ void st_global_v8(float *p, float a, float b, float c, float d, float e, float f, float g, float h) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(a), "f"(b), "f"(c), "f"(d),
+               "f"(e), "f"(f), "f"(g), "f"(h)
+               : "memory");
+}
+
 // D x 128 keys, MN-major in 128-byte swizzle atoms of 64 columns x 8 keys: 1024 bytes to
 // the next 8 keys, kTcKeys * 128 to the next 64 columns
 __device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t smem_addr) {
@@ -454,11 +460,11 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       }
       if (!ok) break;
       // the unit's partial result
-      const int64_t piece = 2 * ((int64_t)u.seg + blockIdx.x) + t, at = piece * kTcRows + r;
+      const int64_t piece = 2 * ((int64_t)u.seg + blockIdx.x) + t;
       const bool store = live && in_bounds(piece, 2 * ((int64_t)a.Hkv * plan.blocks[a.n_prefixes] + gridDim.x), a.status,
                                            kSitePrefixPiece);
-      if (store) ws.tc_ml[at] = make_float2(m_run, l_run);
-      float4 *dst = reinterpret_cast<float4 *>(ws.tc_acc + at * D);
+      if (store) ws.tc_ml[piece * kTcRows + r] = make_float2(m_run, l_run);
+      float *dst = ws.tc_acc + tc_acc_at<D>(piece, r, 0);
       if (mine > 0) {
         ok = wwait(&pv_done[t], (uint32_t)(ns - 1) & 1u);
         if (!ok) break;
@@ -470,14 +476,16 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             tmem_ld_32x32b_x32(t_o + c * 32, o);
             if (store)
 #pragma unroll
-              for (int i = 0; i < 8; ++i) dst[c * 8 + i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+              for (int i = 0; i < 4; ++i)
+                st_global_v8(dst + (c * 4 + i) * (kTcRows * 8), o[8 * i], o[8 * i + 1], o[8 * i + 2], o[8 * i + 3],
+                             o[8 * i + 4], o[8 * i + 5], o[8 * i + 6], o[8 * i + 7]);
           }
         }
         tc_fence_before();
         __syncwarp();
         if (elect_one()) mbar_arrive(&o_free[t]);
       } else if (store) {
-        for (int i = 0; i < D / 4; ++i) dst[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < D / 8; ++i) st_global_v8(dst + i * (kTcRows * 8), 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f);
       }
     }
     if (!ok) give_up();
