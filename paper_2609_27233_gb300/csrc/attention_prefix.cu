@@ -17,8 +17,8 @@
 //
 // P is taken as a bf16 number and a bf16 remainder, two products with V each (17
 // significant bits; one bf16 P would cost as much as the output's own rounding):
-// 512 + 1024 cycles of tensor cores a tile of 128 x 128 x 128.  P lies over the half of S
-// that it came from (64 columns of S: 32 of P, 32 of its remainder).  K and V are
+// 512 + 1024 cycles of tensor cores a tile of 128 x 128 x 128.  P lies over the S
+// that it came from (16 columns of S: 8 of P, 8 of its remainder).  K and V are
 // read from the pages as they lie: K is K-major, V MN-major (64 columns of the head
 // dimension x 8 entries a swizzle atom), so nothing is transposed.
 //
@@ -38,7 +38,7 @@ namespace umim {
 namespace {
 
 constexpr uint32_t kTcTmemCols = 512;   // S of the slots at 0 and 128, O at 256 and 384
-constexpr int kRawStages = 3;           // 8-bit: K and V tiles as they come, in turn
+constexpr int kRawK = 2, kRawV = 1, kRawStages = kRawK + kRawV;   // 8-bit: K and V tiles as they come
 
 // shared memory (bytes, every piece 1024-aligned but the scales)
 template <int D, int BITS>
@@ -53,8 +53,10 @@ struct TcSmem {
   static constexpr int kPlan = kScales + (BITS == 8 ? kRawStages * 8 * 128 : 0);
   static constexpr int kMost = kPlan + 12 * (kSharedMaxPrefixes + 1) + 1024;
 };
+// warps 0 and 3 copies, 1-2 products, 4-19 softmax (two warps a slot and 32 rows: 64 keys each), 20-27 8-bit values
+constexpr int kSoftmax = 4, kConvert = 20, kConverters = 8;
 template <int BITS>
-constexpr int kTcThreads = BITS == 8 ? 480 : 352;   // warp 0 copies, 1-2 products, 3-10 softmax, 11-14 8-bit values
+constexpr int kTcThreads = 32 * (BITS == 8 ? kConvert + kConverters : kConvert);
 
 // one CTA's part of a segment
 struct TcUnit {
@@ -116,7 +118,9 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   constexpr int KS = L::kKStages, VS = L::kVStages;
   extern __shared__ __align__(1024) uint8_t tc_raw[];
   __shared__ __align__(8) uint64_t q_full[2], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2],
-      p_full[2][2], pv_done[2], o_free[2], turn[2], mma_done[2], raw_full[kRawStages], raw_empty[kRawStages];
+      p_full[2][2], pv_done[2], o_free[2], turn[2], mma_done[2], raw_full[kRawStages], raw_empty[kRawStages],
+      met[2][4];
+  __shared__ float s_row[2][2][2][kTcRows];   // [tile's parity][slot][half]: a row's maximum, or sum
   __shared__ uint32_t tmem_base;
   __shared__ int s_abort;
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(tc_raw) + 1023) & ~uintptr_t(1023));
@@ -125,23 +129,24 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&k_full[s], BITS == 8 ? 4 : 1);
+      mbar_init(&k_full[s], BITS == 8 ? kConverters : 1);
       mbar_init(&k_empty[s], 2);   // read by both slots' products, or twice by one's
-      mbar_init(&v_full[s], BITS == 8 ? 4 : 1);
+      mbar_init(&v_full[s], BITS == 8 ? kConverters : 1);
       mbar_init(&v_empty[s], 2);
       mbar_init(&q_full[s], 1);
       mbar_init(&q_empty[s], 1);     // a unit's S products have read the slot's Q
       mbar_init(&s_full[s], 1);
-      mbar_init(&p_full[s][0], 4);   // keys 0-63 of P ready (the slot's four softmax warps)
+      mbar_init(&p_full[s][0], 4);   // keys 0-63 of P ready (four softmax warps)
       mbar_init(&p_full[s][1], 4);   // keys 64-127
       mbar_init(&pv_done[s], 1);     // a tile's P V product has landed
-      mbar_init(&o_free[s], 4);      // a unit's epilogue has read O
+      mbar_init(&o_free[s], 8);      // a unit's epilogue has read O
+      for (int q = 0; q < 4; ++q) mbar_init(&met[s][q], 2);   // the two warps of 32 rows have left each other something
       mbar_init(&turn[s], 1);        // the other slot's products are issued
       mbar_init(&mma_done[s], 1);
     }
     for (int s = 0; s < kRawStages; ++s) {
       mbar_init(&raw_full[s], 1);
-      mbar_init(&raw_empty[s], 4);
+      mbar_init(&raw_empty[s], kConverters);
     }
     fence_mbar_init();
     prefetch_tensormap(&q_map);
@@ -188,16 +193,24 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     return __all_sync(0xffffffffu, !aborted() && mbar_wait(m, parity)) != 0;
   };
 
-  if (warp == 0) {
-    // ---- copies: lanes 0-7 a page each (two boxes of it in lanes 0-15 for 16-bit
-    // pages of 128 columns), lanes 8-15 the scales of 8-bit pages ----
+  if (warp == 0 || warp == 3) {
+    // ---- copies, K's (and Q's) by one warp and V's by the other: lanes 0-7 a page each (two
+    // boxes of it in lanes 0-15 for 16-bit pages of 128 columns), lanes 8-15 the scales of
+    // 8-bit pages.  A box takes about 90 cycles to issue, so one warp would be busy
+    // for as long as the products of a tile take ----
+    const int kv = warp == 0 ? 0 : 1;
+    constexpr int kStagesK = BITS == 16 ? KS : kRawK, kStagesV = BITS == 16 ? VS : kRawV;
+    const int stages = kv ? kStagesV : kStagesK;
+    uint64_t *full = BITS == 16 ? (kv ? v_full : k_full) : kv ? raw_full + kRawK : raw_full;
+    uint64_t *empty = BITS == 16 ? (kv ? v_empty : k_empty) : kv ? raw_empty + kRawK : raw_empty;
+    uint8_t *to = smem + (BITS == 16 ? (kv ? L::kV : L::kK) : L::kRawAt + kv * kRawK * L::kRaw);
     int nq = 0, pos = 0;   // units, and key tiles
     bool ok = true;
     TcUnit u;
     for (int x = start; ok && unit_at(a, plan, x, end, u);) {
       const int n_pages = ceil_div(u.len, kPageSize), part = u.len % kPageSize;
       const int32_t *table = a.prefix_table + (int64_t)u.i * a.max_prefix_pages;
-      for (int t = 0; t < 2 && ok; ++t) {
+      for (int t = 0; t < 2 && ok && kv == 0; ++t) {
         if (nq > 0) ok = wwait(&q_empty[t], (uint32_t)(nq - 1) & 1u);
         if (ok && lane == 0) {
           mbar_arrive_expect_tx(&q_full[t], DA * spt * a.G * 128);
@@ -210,54 +223,39 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       ++nq;
       const int pg = lane & 7;
       for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
-        const int at = j * 8 + pg;
+        const int at = j * 8 + pg, s = pos % stages;
         int c = a.n_layers * a.n_pages;   // a coordinate past the tensor's last page: the copy reads zeros
         if (at < n_pages && in_bounds(at, a.max_prefix_pages, a.status, kSitePrefixTable)) {
           const int page = table[at];
           if (page >= 0 && page < a.n_pages) c = a.layer * a.n_pages + page;
           else set_error(a.status, UMIM_ERR_INVALID_ARG);
         }
-        for (int kv = 0; kv < 2 && ok; ++kv) {
-          if constexpr (BITS == 16) {
-            const int s = pos & 1;
-            uint64_t *full = kv ? &v_full[s] : &k_full[s];
-            ok = wwait(kv ? &v_empty[s] : &k_empty[s], (uint32_t)(pos >> 1 & 1) ^ 1u);
-            if (!ok) break;
-            if (lane == 0) mbar_arrive_expect_tx(full, L::kTile);
-            __syncwarp();
-            if (lane < 8 * DA)
-              tma_load_5d(smem + (kv ? L::kV : L::kK) + s * L::kTile + (lane >> 3) * (kTcKeys * 128) + pg * (kPageSize * 128),
-                          &kv_map, full, (lane >> 3) * 64, at == n_pages - 1 && part ? part - kPageSize : 0, u.g, kv, c,
-                          policy_evict_last());
-          } else {
-            const int item = 2 * pos + kv, s = item % kRawStages;
-            ok = wwait(&raw_empty[s], (uint32_t)(item / kRawStages & 1) ^ 1u);
-            if (!ok) break;
-            if (lane == 0) mbar_arrive_expect_tx(&raw_full[s], L::kRaw + 8 * kPageSize);
-            __syncwarp();
-            if (lane < 8)
-              tma_load_5d(smem + L::kRawAt + s * L::kRaw + pg * (kPageSize * D), &kv_map, &raw_full[s], 0, 0, u.g, kv, c,
-                          policy_evict_last());
-            else if (lane < 16)
-              tma_load_4d(smem + L::kScales + (s * 8 + pg) * 128, &scale_map, &raw_full[s], 0, u.g, kv, c);
-          }
+        ok = wwait(&empty[s], (uint32_t)(pos / stages & 1) ^ 1u);
+        if (!ok) break;
+        if constexpr (BITS == 16) {
+          if (lane == 0) mbar_arrive_expect_tx(&full[s], L::kTile);
+          __syncwarp();
+          if (lane < 8 * DA)
+            tma_load_5d(to + s * L::kTile + (lane >> 3) * (kTcKeys * 128) + pg * (kPageSize * 128), &kv_map, &full[s],
+                        (lane >> 3) * 64, at == n_pages - 1 && part ? part - kPageSize : 0, u.g, kv, c,
+                        policy_evict_last());
+        } else {
+          if (lane == 0) mbar_arrive_expect_tx(&full[s], L::kRaw + 8 * kPageSize);
+          __syncwarp();
+          if (lane < 8)
+            tma_load_5d(to + s * L::kRaw + pg * (kPageSize * D), &kv_map, &full[s], 0, 0, u.g, kv, c, policy_evict_last());
+          else if (lane < 16)
+            tma_load_4d(smem + L::kScales + ((kv * kRawK + s) * 8 + pg) * 128, &scale_map, &full[s], 0, u.g, kv, c);
         }
       }
     }
-    if (!ok) give_up();
-    // copies still in flight when a consumer gave up: wait for them (bounded).  The barriers
-    // only count what was armed, so a phase that has completed returns at once.
     if (!ok) {
-      if constexpr (BITS == 16) {
-        for (int i = max(0, pos - 2); i <= pos; ++i) {
-          mbar_wait_for(&k_full[i & 1], (uint32_t)(i >> 1 & 1), 1000000);
-          mbar_wait_for(&v_full[i & 1], (uint32_t)(i >> 1 & 1), 1000000);
-        }
-      } else {
-        for (int i = max(0, 2 * pos - kRawStages); i <= 2 * pos + 1; ++i)
-          mbar_wait_for(&raw_full[i % kRawStages], (uint32_t)(i / kRawStages & 1), 1000000);
-      }
-      for (int t = 0; t < 2; ++t)
+      give_up();
+      // copies still in flight when a consumer gave up: wait for them (bounded; a phase that has
+      // completed, or was never armed, costs no more than a millisecond)
+      for (int i = max(0, pos - stages); i <= pos; ++i)
+        mbar_wait_for(&full[i % stages], (uint32_t)(i / stages & 1), 1000000);
+      for (int t = 0; t < 2 && kv == 0; ++t)
         if (nq > 0) mbar_wait_for(&q_full[t], (uint32_t)(nq - 1) & 1u, 1000000);
     }
   } else if (warp <= 2) {
@@ -298,7 +296,8 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             for (int part = 0; part < 2; ++part)
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk)   // 16 keys: a page
-                tc_mma_ts(t_o, t_s + h * 64 + part * 32 + kk * 8, v_desc + (h * 4 + kk) * (kPageSize * 128 / 16), idesc_o,
+                tc_mma_ts(t_o, t_s + (h * 4 + kk) * 16 + part * 8,
+                          v_desc + (h * 4 + kk) * (kPageSize * 128 / 16), idesc_o,
                           !pend_first || h || part || kk ? 1u : 0u);
           }
           tc_commit(&pv_done[t]);
@@ -332,43 +331,58 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         return true;
       };
       bool ok = true;
-      int pos = 0, nq = 0;
+      int pos = 0, nq = 0, x = start;
       TcUnit u;
-      for (int x = start; ok && unit_at(a, plan, x, end, u); ++nq) {
-        const int n = u.t1 - u.t0;
-        if (u.two) {
-          for (int i = 0; i < n && ok; ++i) ok = take_turn(pos + i, i == 0, i == n - 1, true, nq);
-        } else {
-          for (int i = t; i - t < n && ok; i += 2) ok = take_turn(i < n ? pos + i : -1, i == t, i + 2 >= n, false, nq);
-          if (ok && t >= n) {   // no tile of this slot's: its Q is in nobody's way
-            ok = mbar_wait(&q_full[t], (uint32_t)nq & 1u);
-            if (ok) mbar_arrive(&q_empty[t]);
-          }
+      bool more = unit_at(a, plan, x, end, u);
+      for (int i = 0; ok;) {   // i: the unit's turns so far
+        const int n = more ? u.t1 - u.t0 : 0, step = u.two ? 1 : 2, at = u.two ? i : 2 * i + t;
+        const bool mine = more && at < n;
+        ok = take_turn(mine ? pos + at : -1, i == 0, at + step >= n, u.two, nq);
+        if (!more) break;   // (that was the last P V)
+        if (ok && i == 0 && !mine) {   // no tile of this slot's: its Q is in nobody's way
+          ok = mbar_wait(&q_full[t], (uint32_t)nq & 1u);
+          if (ok) mbar_arrive(&q_empty[t]);
         }
-        pos += n;
+        if (++i * step >= n) {
+          pos += n;
+          ++nq;
+          i = 0;
+          more = unit_at(a, plan, x, end, u);
+        }
       }
-      if (ok && nq > 0) ok = take_turn(-1, false, false, false, 0);
       if (!ok) give_up();
       // every product this thread issued has finished before tensor memory is released
       tc_commit(&mma_done[t]);
       mbar_wait_for(&mma_done[t], 0, kWaitLimitNs);
     }
     __syncwarp();
-  } else if (warp <= 10) {
-    // ---- softmax and partial results of slot t: four warps, thread = query row ----
-    const int t = (warp - 3) >> 2;
+  } else if (warp >= kSoftmax && warp < kConvert) {
+    // ---- softmax and partial results of slot t: a thread a query row and 64 of the tile's keys
+    // (with all 128 a tile's softmax took longer than the other slot's products) ----
+    const int t = (warp - kSoftmax) >> 3, half = (warp - kSoftmax) >> 2 & 1;
     const int quad = warp & 3;                 // tensor-memory lanes this warp may access
     const int r = quad * 32 + lane;            // row within the tile
-    const uint32_t t_s = tmem + ((uint32_t)(quad * 32) << 16) + t * kTcKeys;
+    const uint32_t t_s = tmem + ((uint32_t)(quad * 32) << 16) + t * kTcKeys + half * 64;
     const uint32_t t_o = tmem + ((uint32_t)(quad * 32) << 16) + 256 + t * 128;
     const float sl2 = a.scale_log2;
     bool ok = true;
-    int ns = 0;
+    int ns = 0, meets = 0;
+    // what the other warp of these rows left: a value a row
+    auto exchange = [&](float mine, float &other) {
+      float (&slot)[2][kTcRows] = s_row[meets & 1][t];
+      slot[half][r] = mine;
+      __syncwarp();
+      if (elect_one()) mbar_arrive(&met[t][quad]);
+      const bool came = wwait(&met[t][quad], (uint32_t)meets & 1u);
+      other = slot[half ^ 1][r];
+      ++meets;
+      return came;
+    };
     TcUnit u;
     for (int x = start; ok && unit_at(a, plan, x, end, u);) {
       const int row_tile = u.tile + (u.two ? t : 0), seq = plan.first[u.i] + row_tile * spt + r / a.G;
       const bool live = r < spt * a.G && seq < plan.first[u.i + 1];
-      const bool any = __any_sync(0xffffffffu, live);   // (a warp without rows only keeps the others going)
+      const bool any = __any_sync(0xffffffffu, live);   // (warps without rows only keep the others going)
       float m_run = -INFINITY, l_run = 0.f;             // running max (log2 units, moved in steps > 8) and row sum
       int mine = 0;                                     // tiles
       for (int j = u.t0 + (u.two ? 0 : t); j < u.t1; j += u.two ? 1 : 2, ++mine, ++ns) {
@@ -378,35 +392,35 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         if (!any) {
           tc_fence_before();
           __syncwarp();
-          if (elect_one()) mbar_arrive(&p_full[t][0]), mbar_arrive(&p_full[t][1]);
+          if (elect_one()) mbar_arrive(&p_full[t][half]);
           continue;
         }
-        const int rem = u.len - j * kTcKeys;   // keys from here on
-        auto mask = [&](float (&s)[64], int x0) {
-          if (rem >= kTcKeys) return;
-          const int full = rem / kPageSize * kPageSize, part = rem % kPageSize;
+        const int rem = u.len - j * kTcKeys - half * 64;   // keys from this warp's first on
+        auto mask = [&](float (&s)[32], int x) {
+          if (rem >= x + 32) return;
+          // 16-bit pages: the last page's entries are its last rows
+          const int left = max(rem, 0), full = left / kPageSize * kPageSize, part = left % kPageSize;
+          const uint32_t bits = BITS == 8 ? columns_in(x, 0, left)
+                                          : columns_in(x, 0, full) | columns_in(x, full + kPageSize - part, full + kPageSize);
 #pragma unroll
-          for (int x = 0; x < 64; x += 32) {
-            // 16-bit pages: the last page's entries are its last rows
-            const uint32_t bits = BITS == 8 ? columns_in(x0 + x, 0, rem)
-                                            : columns_in(x0 + x, 0, full) | columns_in(x0 + x, full + kPageSize - part, full + kPageSize);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) s[x + c] = bits >> c & 1u ? s[x + c] : -INFINITY;
-          }
+          for (int c = 0; c < 32; ++c) s[c] = bits >> c & 1u ? s[c] : -INFINITY;
         };
-        auto largest = [&](const float (&s)[64]) {
+        auto largest = [&](const float (&s)[32]) {
           float m4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-          for (int c = 4; c < 64; c += 2) m4[(c >> 1) & 3] = max3f(m4[(c >> 1) & 3], s[c], s[c + 1]);
+          for (int c = 4; c < 32; c += 2) m4[(c >> 1) & 3] = max3f(m4[(c >> 1) & 3], s[c], s[c + 1]);
           return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         };
-        float s[64];
-        tmem_ld_32x32b_x64(t_s + 64, s);
-        mask(s, 64);
-        float mx = largest(s);
-        tmem_ld_32x32b_x64(t_s, s);
+        float s[32];
+        tmem_ld_32x32b_x32(t_s + 32, s);
+        mask(s, 32);
+        float mx = largest(s), other;
+        tmem_ld_32x32b_x32(t_s, s);
         mask(s, 0);
-        mx = fmaxf(mx, largest(s)) * sl2;
+        mx = fmaxf(mx, largest(s));
+        ok = exchange(mx, other);
+        if (!ok) break;
+        mx = fmaxf(mx, other) * sl2;
         // move the running max only when it grows by more than 2^8
         const bool grow = mx > m_run + 8.f;
         float alpha = 1.f;
@@ -415,65 +429,73 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           m_run = mx;
           l_run *= alpha;
         }
+        // O is rescaled before the tile's first product, of half 0 (the tile before's has landed: S followed it)
+        if (half == 0 && mine > 0 && __any_sync(0xffffffffu, grow)) {
+#pragma unroll 1
+          for (int c = 0; c < D / 16; ++c) {
+            float o[16];
+            tmem_ld_32x32b_x16(t_o + c * 16, o);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] *= alpha;
+            tmem_put_32x32b_x16(t_o + c * 16, o);
+          }
+          tmem_wait_st();
+        }
         const float nm = (m_run == -INFINITY) ? 0.f : -m_run;
-        const float2 sl2x2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm);
+        const float2 sl2x2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm), minus = make_float2(-1.f, -1.f);
         float2 la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (h == 1) {
-            tmem_ld_32x32b_x64(t_s + 64, s);
-            mask(s, 64);
+            tmem_ld_32x32b_x32(t_s + 32, s);
+            mask(s, 32);
           }
-          float hi[32], lo[32];   // P (<= 2^8) in bf16 pairs, and what that leaves
 #pragma unroll
-          for (int c = 0; c < 64; c += 2) {
-            const float2 x = __ffma2_rn(make_float2(s[c], s[c + 1]), sl2x2, nm2);
-            const float2 y = make_float2(ex2_approx(x.x), ex2_approx(x.y));   // masked (-inf): 0
-            if (c & 2) lb = __fadd2_rn(lb, y);
-            else la = __fadd2_rn(la, y);
-            const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
-            const uint32_t p = *reinterpret_cast<const uint32_t *>(&b);
-            const __nv_bfloat162 d = __floats2bfloat162_rn(y.x - __uint_as_float(p << 16), y.y - __uint_as_float(p & 0xffff0000u));
-            hi[c / 2] = __uint_as_float(p);
-            lo[c / 2] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&d));
-          }
-          // O is rescaled before the tile's first product (the tile before's has landed: S followed it)
-          if (h == 0 && mine > 0 && __any_sync(0xffffffffu, grow)) {
-#pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-              float o[32];
-              tmem_ld_32x32b_x32(t_o + c * 32, o);
+          for (int g = 0; g < 2; ++g) {   // 16 keys: P (<= 2^8) in bf16 pairs, and what that leaves
+            float p[16];
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] *= alpha;
-              tmem_st_32x32b_x32(t_o + c * 32, o);
+            for (int c = 0; c < 16; c += 2) {
+              const float2 x = __ffma2_rn(make_float2(s[g * 16 + c], s[g * 16 + c + 1]), sl2x2, nm2);
+              const float2 y = make_float2(ex2_approx(x.x), ex2_approx(x.y));   // masked (-inf): 0
+              if (c & 2) lb = __fadd2_rn(lb, y);
+              else la = __fadd2_rn(la, y);
+              const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
+              const uint32_t hi = *reinterpret_cast<const uint32_t *>(&b);
+              const float2 d = __ffma2_rn(make_float2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), minus, y);
+              const __nv_bfloat162 rest = __floats2bfloat162_rn(d.x, d.y);
+              p[c / 2] = __uint_as_float(hi);
+              p[8 + c / 2] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&rest));
             }
+            // over the S columns they come from, which this thread has read
+            tmem_put_32x32b_x16(t_s + h * 32 + g * 16, p);
           }
-          // over the S columns they come from, which this thread has read
-          tmem_st_32x32b_x32(t_s + h * 64, hi);
-          tmem_st_32x32b_x32(t_s + h * 64 + 32, lo);
-          tc_fence_before();
-          __syncwarp();
-          if (elect_one()) mbar_arrive(&p_full[t][h]);
         }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&p_full[t][half]);
         const float2 lab = __fadd2_rn(la, lb);
         l_run += lab.x + lab.y;
       }
       if (!ok) break;
-      // the unit's partial result
+      // the unit's partial result, half the columns a warp
       const int64_t piece = 2 * ((int64_t)u.seg + blockIdx.x) + t;
       const bool store = live && in_bounds(piece, 2 * ((int64_t)a.Hkv * plan.blocks[a.n_prefixes] + gridDim.x), a.status,
                                            kSitePrefixPiece);
-      if (store) ws.tc_ml[piece * kTcRows + r] = make_float2(m_run, l_run);
-      float *dst = ws.tc_acc + tc_acc_at<D>(piece, r, 0);
+      float other;
+      ok = exchange(l_run, other);
+      if (!ok) break;
+      if (store && half == 0) ws.tc_ml[piece * kTcRows + r] = make_float2(m_run, l_run + other);
+      float *dst = ws.tc_acc + tc_acc_at<D>(piece, r, half * (D / 2));
       if (mine > 0) {
         ok = wwait(&pv_done[t], (uint32_t)(ns - 1) & 1u);
         if (!ok) break;
         tc_fence_after();
         if (any) {
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
+          for (int c = 0; c < D / 64; ++c) {
             float o[32];
-            tmem_ld_32x32b_x32(t_o + c * 32, o);
+            tmem_ld_32x32b_x32(t_o + half * (D / 2) + c * 32, o);
             if (store)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
@@ -485,15 +507,15 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         __syncwarp();
         if (elect_one()) mbar_arrive(&o_free[t]);
       } else if (store) {
-        for (int i = 0; i < D / 8; ++i) st_global_v8(dst + i * (kTcRows * 8), 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < D / 16; ++i) st_global_v8(dst + i * (kTcRows * 8), 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f);
       }
     }
     if (!ok) give_up();
-  } else {
-    // ---- 8-bit values to bf16 operands: a warp 32 keys, D / 8 lanes a key ----
+  } else if (warp >= kConvert) {
+    // ---- 8-bit values to bf16 operands: a warp 16 keys, D / 8 lanes a key ----
     if constexpr (BITS == 8) {
-      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
-      const int w = warp - 11, part = lane % kLanes;
+      constexpr int kKeys = kTcKeys / kConverters, kLanes = D / 8, kAtOnce = 32 / kLanes;
+      const int w = warp - kConvert, part = lane % kLanes;
       bool ok = true;
       int pos = 0;
       TcUnit u;
@@ -501,26 +523,35 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
           const int rem = u.len - j * kTcKeys;
           for (int kv = 0; kv < 2; ++kv) {
-            const int item = 2 * pos + kv, s = item % kRawStages, stages = kv ? VS : KS, to = pos % stages;
-            ok = wwait(&raw_full[s], (uint32_t)(item / kRawStages & 1)) &&
+            const int raws = kv ? kRawV : kRawK, s = kv * kRawK + pos % raws, stages = kv ? VS : KS, to = pos % stages;
+            ok = wwait(&raw_full[s], (uint32_t)(pos / raws & 1)) &&
                  wwait(kv ? &v_empty[to] : &k_empty[to], (uint32_t)(pos / stages & 1) ^ 1u);
             if (!ok) break;
             const uint8_t *raw = smem + L::kRawAt + s * L::kRaw, *scales = smem + L::kScales + s * 8 * 128;
             uint8_t *dst = smem + (kv ? L::kV : L::kK) + to * L::kTile + (part >> 3) * (kTcKeys * 128);
-#pragma unroll 4
-            for (int i = 0; i < 32; i += kAtOnce) {
-              const int key = w * 32 + i + lane / kLanes;
-              const uint2 v = *reinterpret_cast<const uint2 *>(raw + key * D + part * 8);
-              const float f = e8m0_value(scales[(key >> 4) * 128 + (key & 15)]);
+            // (all loads first: a warp alone on its scheduler waits for each otherwise)
+            uint2 v[kKeys / kAtOnce];
+            uint8_t code[kKeys / kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kKeys / kAtOnce; ++i) {
+              const int key = w * kKeys + i * kAtOnce + lane / kLanes;
+              v[i] = *reinterpret_cast<const uint2 *>(raw + key * D + part * 8);
+              code[i] = scales[(key >> 4) * 128 + (key & 15)];
+            }
+#pragma unroll
+            for (int i = 0; i < kKeys / kAtOnce; ++i) {
+              const int key = w * kKeys + i * kAtOnce + lane / kLanes;
+              const float f = e8m0_value(code[i]);
               const __nv_bfloat162 f2 = __floats2bfloat162_rn(f, f);   // exact
               uint32_t out[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const uint32_t h = f16x2_of_e4m3x2((e < 2 ? v.x : v.y) >> (e & 1) * 16);
+                const uint32_t h = f16x2_of_e4m3x2((e < 2 ? v[i].x : v[i].y) >> (e & 1) * 16);
                 const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h));
                 const __nv_bfloat162 b = __hmul2(__floats2bfloat162_rn(y.x, y.y), f2);
-                out[e] = key < rem ? *reinterpret_cast<const uint32_t *>(&b) : 0u;
+                out[e] = *reinterpret_cast<const uint32_t *>(&b);
               }
+              if (rem < kTcKeys && key >= rem) out[0] = out[1] = out[2] = out[3] = 0u;
               *reinterpret_cast<uint4 *>(dst + key * 128 + (((part & 7) ^ (key & 7)) << 4)) =
                   make_uint4(out[0], out[1], out[2], out[3]);
             }
@@ -548,7 +579,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
 template <int D, int BITS>
 bool launch(const CacheView &kv, const PagesArgs &a, const PagesWs &ws, cudaStream_t stream, int num_sms) {
   using L = TcSmem<D, BITS>;
-  static_assert(L::kMost + 1024 <= 232448, "shared memory of a CTA");
+  static_assert(L::kMost + 6144 <= 232448, "shared memory of a CTA");
   EncodeTiledFn enc = get_encode_tiled();
   if (!enc) return false;
   CUtensorMap q_map, kv_map, scale_map;
