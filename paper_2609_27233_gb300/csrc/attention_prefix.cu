@@ -26,8 +26,8 @@
 // the operands' place.  The last page is loaded from row n - 16 on where it holds n <
 // 16 entries: TMA reads rows before the first as zeros, so that nothing behind the
 // prefix's end is ever read; S is masked there.
-// 8-bit pages: e4m3 rows and scales into a ring, from which four warps make the bf16
-// operands, value * 2^e (exact), zeros behind the end.
+// 8-bit pages: e4m3 rows into rings of their own, from which eight warps (a page
+// each) make the bf16 operands, value * 2^e (exact), zeros behind the end.
 #include <cuda_fp16.h>
 
 #include "attention_pages.cuh"
@@ -49,15 +49,20 @@ struct TcSmem {
   static constexpr int kK = 2 * kTile;
   static constexpr int kV = kK + kKStages * kTile;
   static constexpr int kRawAt = kV + kVStages * kTile;
-  static constexpr int kScales = kRawAt + kRawStages * kRaw;              // [stage][8 pages][128 B], 16 used
-  static constexpr int kPlan = kScales + (BITS == 8 ? kRawStages * 8 * 128 : 0);
+  static constexpr int kPlan = kRawAt + kRawStages * kRaw;
   static constexpr int kMost = kPlan + 12 * (kSharedMaxPrefixes + 1) + 1024;
 };
-// warps 0 and 3 copies, 1-2 products, 4-19 softmax (two warps a slot and 32 rows: 64 keys each), 20-27 8-bit values
-constexpr int kSoftmax = 4, kConvert = 20, kConverters = 8;
+// warps 0 and 3 copies, 1-2 products, from 4 on softmax, then the 8-bit values
+constexpr int kSoftmax = 4, kConverters = 8;
+// Softmax warps of a slot's 32 rows: two, with half the keys each, take 1600 cycles a tile in
+// place of 2800.  8-bit pages: one, since the converters need registers too (with 28
+// warps the 72 registers a thread spill into a cache that the operands leave no room for).
 template <int BITS>
-constexpr int kTcThreads = 32 * (BITS == 8 ? kConvert + kConverters : kConvert);
-
+constexpr int kHalves = BITS == 8 ? 1 : 2;
+template <int BITS>
+constexpr int kConvert = kSoftmax + 8 * kHalves<BITS>;
+template <int BITS>
+constexpr int kTcThreads = 32 * (BITS == 8 ? kConvert<BITS> + kConverters : kConvert<BITS>);
 // one CTA's part of a segment
 struct TcUnit {
   int i, g, tile;     // prefix, KV head, first row tile
@@ -90,6 +95,18 @@ __device__ __forceinline__ bool unit_at(const PagesArgs &a, const PrefixPlan &p,
   return false;
 }
 
+// Loads that stay where they are written, ahead of their use: the compiler moves plain ones to it.
+__device__ __forceinline__ int ld_early(const int32_t *p) {
+  int v;
+  asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t ld_early_u8(const uint8_t *p) {
+  uint16_t v;
+  asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
+  return v;
+}
+
 // a tile's 32 columns from x on whose positions lie in [lo, hi)
 __device__ __forceinline__ uint32_t columns_in(int x, int lo, int hi) {
   lo = max(lo - x, 0), hi = min(hi - x, 32);
@@ -112,7 +129,7 @@ constexpr uint32_t kBMnMajor = 1u << 16;   // instruction descriptor: B is MN-ma
 template <int D, int BITS>
 __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     prefix_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap kv_map,
-                     const __grid_constant__ CUtensorMap scale_map, PagesArgs a, PagesWs ws) {
+                     const uint8_t *scales, PagesArgs a, PagesWs ws) {
   using L = TcSmem<D, BITS>;
   constexpr int DA = D / 64;
   constexpr int KS = L::kKStages, VS = L::kVStages;
@@ -139,7 +156,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       mbar_init(&p_full[s][0], 4);   // keys 0-63 of P ready (four softmax warps)
       mbar_init(&p_full[s][1], 4);   // keys 64-127
       mbar_init(&pv_done[s], 1);     // a tile's P V product has landed
-      mbar_init(&o_free[s], 8);      // a unit's epilogue has read O
+      mbar_init(&o_free[s], 4 * kHalves<BITS>);   // a unit's epilogue has read O
       for (int q = 0; q < 4; ++q) mbar_init(&met[s][q], 2);   // the two warps of 32 rows have left each other something
       mbar_init(&turn[s], 1);        // the other slot's products are issued
       mbar_init(&mma_done[s], 1);
@@ -151,7 +168,6 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     fence_mbar_init();
     prefetch_tensormap(&q_map);
     prefetch_tensormap(&kv_map);
-    if (BITS == 8) prefetch_tensormap(&scale_map);
   }
   if (warp == 1) {
     tmem_alloc(&tmem_base, kTcTmemCols);
@@ -190,14 +206,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   };
   // the whole warp waits, and goes on only if all of it saw the phase
   auto wwait = [&](uint64_t *m, uint32_t parity) {
-    return __all_sync(0xffffffffu, !aborted() && mbar_wait(m, parity)) != 0;
+    return __all_sync(0xffffffffu, mbar_try_wait(smem_u32(m), parity) || (!aborted() && mbar_wait(m, parity))) != 0;
   };
 
   if (warp == 0 || warp == 3) {
-    // ---- copies, K's (and Q's) by one warp and V's by the other: lanes 0-7 a page each (two
-    // boxes of it in lanes 0-15 for 16-bit pages of 128 columns), lanes 8-15 the scales of
-    // 8-bit pages.  A box takes about 90 cycles to issue, so one warp would be busy
-    // for as long as the products of a tile take ----
+    // ---- copies, K's (and Q's) by one warp and V's by the other, a lane a box: two of a page for
+    // 16-bit pages of 128 columns.  (A box takes about 90 cycles to issue: one warp would
+    // be busy for as long as the products of a tile take.) ----
     const int kv = warp == 0 ? 0 : 1;
     constexpr int kStagesK = BITS == 16 ? KS : kRawK, kStagesV = BITS == 16 ? VS : kRawV;
     const int stages = kv ? kStagesV : kStagesK;
@@ -222,14 +237,19 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       }
       ++nq;
       const int pg = lane & 7;
+      auto page_at = [&](int j) {   // read a tile ahead
+        const int at = j * 8 + pg;
+        return j < u.t1 && at < n_pages && in_bounds(at, a.max_prefix_pages, a.status, kSitePrefixTable) ? ld_early(table + at) : 0;
+      };
+      int page = page_at(u.t0);
       for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
         const int at = j * 8 + pg, s = pos % stages;
         int c = a.n_layers * a.n_pages;   // a coordinate past the tensor's last page: the copy reads zeros
-        if (at < n_pages && in_bounds(at, a.max_prefix_pages, a.status, kSitePrefixTable)) {
-          const int page = table[at];
+        if (at < n_pages) {
           if (page >= 0 && page < a.n_pages) c = a.layer * a.n_pages + page;
           else set_error(a.status, UMIM_ERR_INVALID_ARG);
         }
+        page = page_at(j + 1);
         ok = wwait(&empty[s], (uint32_t)(pos / stages & 1) ^ 1u);
         if (!ok) break;
         if constexpr (BITS == 16) {
@@ -240,12 +260,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                         (lane >> 3) * 64, at == n_pages - 1 && part ? part - kPageSize : 0, u.g, kv, c,
                         policy_evict_last());
         } else {
-          if (lane == 0) mbar_arrive_expect_tx(&full[s], L::kRaw + 8 * kPageSize);
+          if (lane == 0) mbar_arrive_expect_tx(&full[s], L::kRaw);
           __syncwarp();
           if (lane < 8)
             tma_load_5d(to + s * L::kRaw + pg * (kPageSize * D), &kv_map, &full[s], 0, 0, u.g, kv, c, policy_evict_last());
-          else if (lane < 16)
-            tma_load_4d(smem + L::kScales + ((kv * kRawK + s) * 8 + pg) * 128, &scale_map, &full[s], 0, u.g, kv, c);
         }
       }
     }
@@ -280,14 +298,14 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         const bool due = pend >= 0;
         const uint32_t pt = (uint32_t)(ns - 1) & 1u;
         if (due) {
-          if (aborted() || !mbar_wait(&v_full[pend & 1], (uint32_t)(pend >> 1 & 1)) || !mbar_wait(&p_full[t][0], pt) ||
+          if (aborted() || !mbar_wait(&v_full[pend % VS], (uint32_t)(pend / VS & 1)) || !mbar_wait(&p_full[t][0], pt) ||
               (pend_first && nu > 1 && !mbar_wait(&o_free[t], (uint32_t)nu & 1u)))
             return false;
         }
         if ((t == 1 || turns > 0) && (aborted() || !mbar_wait(&turn[t], (uint32_t)(turns + t + 1) & 1u))) return false;
         ++turns;
         if (due) {
-          const uint64_t v_desc = sw128_mnmajor_desc(smem_u32(smem + L::kV + (pend & 1) * L::kTile));
+          const uint64_t v_desc = sw128_mnmajor_desc(smem_u32(smem + L::kV + pend % VS * L::kTile));
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (h == 1 && !mbar_wait(&p_full[t][1], pt)) return false;
@@ -301,7 +319,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                           !pend_first || h || part || kk ? 1u : 0u);
           }
           tc_commit(&pv_done[t]);
-          commits(&v_empty[pend & 1], pend_two);
+          commits(&v_empty[pend % VS], pend_two);
           pend = -1;
           landing = true;
         }
@@ -356,19 +374,21 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       mbar_wait_for(&mma_done[t], 0, kWaitLimitNs);
     }
     __syncwarp();
-  } else if (warp >= kSoftmax && warp < kConvert) {
-    // ---- softmax and partial results of slot t: a thread a query row and 64 of the tile's keys
-    // (with all 128 a tile's softmax took longer than the other slot's products) ----
-    const int t = (warp - kSoftmax) >> 3, half = (warp - kSoftmax) >> 2 & 1;
+  } else if (warp >= kSoftmax && warp < kConvert<BITS>) {
+    // ---- softmax and partial results of slot t: a thread a query row, and all or half of the tile's keys ----
+    constexpr int H = kHalves<BITS>, kKeys = kTcKeys / H, kCols = D / H;
+    const int t = (warp - kSoftmax) >> (H == 2 ? 3 : 2), half = H == 2 ? (warp - kSoftmax) >> 2 & 1 : 0;
     const int quad = warp & 3;                 // tensor-memory lanes this warp may access
     const int r = quad * 32 + lane;            // row within the tile
-    const uint32_t t_s = tmem + ((uint32_t)(quad * 32) << 16) + t * kTcKeys + half * 64;
+    const uint32_t t_s = tmem + ((uint32_t)(quad * 32) << 16) + t * kTcKeys + half * kKeys;
     const uint32_t t_o = tmem + ((uint32_t)(quad * 32) << 16) + 256 + t * 128;
     const float sl2 = a.scale_log2;
     bool ok = true;
     int ns = 0, meets = 0;
     // what the other warp of these rows left: a value a row
-    auto exchange = [&](float mine, float &other) {
+    auto exchange = [&](float mine, float &other, float alone) {
+      other = alone;
+      if (H == 1) return true;
       float (&slot)[2][kTcRows] = s_row[meets & 1][t];
       slot[half][r] = mine;
       __syncwarp();
@@ -392,10 +412,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         if (!any) {
           tc_fence_before();
           __syncwarp();
-          if (elect_one()) mbar_arrive(&p_full[t][half]);
+          if (elect_one()) {
+            mbar_arrive(&p_full[t][half]);
+            if (H == 1) mbar_arrive(&p_full[t][1]);
+          }
           continue;
         }
-        const int rem = u.len - j * kTcKeys - half * 64;   // keys from this warp's first on
+        const int rem = u.len - j * kTcKeys - half * kKeys;   // keys from this warp's first on
         auto mask = [&](float (&s)[32], int x) {
           if (rem >= x + 32) return;
           // 16-bit pages: the last page's entries are its last rows
@@ -411,14 +434,14 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           for (int c = 4; c < 32; c += 2) m4[(c >> 1) & 3] = max3f(m4[(c >> 1) & 3], s[c], s[c + 1]);
           return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         };
-        float s[32];
-        tmem_ld_32x32b_x32(t_s + 32, s);
-        mask(s, 32);
-        float mx = largest(s), other;
-        tmem_ld_32x32b_x32(t_s, s);
-        mask(s, 0);
-        mx = fmaxf(mx, largest(s));
-        ok = exchange(mx, other);
+        float s[32], mx = -INFINITY, other;
+#pragma unroll (H == 2 ? 2 : 1)
+        for (int c = kKeys / 32 - 1; c >= 0; --c) {   // (the first 32 last: they are still there below)
+          tmem_ld_32x32b_x32(t_s + c * 32, s);
+          mask(s, c * 32);
+          mx = fmaxf(mx, largest(s));
+        }
+        ok = exchange(mx, other, mx);
         if (!ok) break;
         mx = fmaxf(mx, other) * sl2;
         // move the running max only when it grows by more than 2^8
@@ -444,11 +467,11 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         const float nm = (m_run == -INFINITY) ? 0.f : -m_run;
         const float2 sl2x2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm), minus = make_float2(-1.f, -1.f);
         float2 la = make_float2(0.f, 0.f), lb = la;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (h == 1) {
-            tmem_ld_32x32b_x32(t_s + 32, s);
-            mask(s, 32);
+#pragma unroll (H == 2 ? 2 : 1)   // (four chunks unrolled: their code is fetched over and over, and registers spill)
+        for (int h = 0; h < kKeys / 32; ++h) {
+          if (h > 0) {
+            tmem_ld_32x32b_x32(t_s + h * 32, s);
+            mask(s, h * 32);
           }
 #pragma unroll
           for (int g = 0; g < 2; ++g) {   // 16 keys: P (<= 2^8) in bf16 pairs, and what that leaves
@@ -469,11 +492,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             // over the S columns they come from, which this thread has read
             tmem_put_32x32b_x16(t_s + h * 32 + g * 16, p);
           }
+          if (h & 1) {   // 64 keys
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (elect_one()) mbar_arrive(&p_full[t][H == 2 ? half : h / 2]);
+          }
         }
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (elect_one()) mbar_arrive(&p_full[t][half]);
         const float2 lab = __fadd2_rn(la, lb);
         l_run += lab.x + lab.y;
       }
@@ -483,19 +508,19 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       const bool store = live && in_bounds(piece, 2 * ((int64_t)a.Hkv * plan.blocks[a.n_prefixes] + gridDim.x), a.status,
                                            kSitePrefixPiece);
       float other;
-      ok = exchange(l_run, other);
+      ok = exchange(l_run, other, 0.f);
       if (!ok) break;
       if (store && half == 0) ws.tc_ml[piece * kTcRows + r] = make_float2(m_run, l_run + other);
-      float *dst = ws.tc_acc + tc_acc_at<D>(piece, r, half * (D / 2));
+      float *dst = ws.tc_acc + tc_acc_at<D>(piece, r, half * kCols);
       if (mine > 0) {
         ok = wwait(&pv_done[t], (uint32_t)(ns - 1) & 1u);
         if (!ok) break;
         tc_fence_after();
         if (any) {
 #pragma unroll 1
-          for (int c = 0; c < D / 64; ++c) {
+          for (int c = 0; c < kCols / 32; ++c) {
             float o[32];
-            tmem_ld_32x32b_x32(t_o + half * (D / 2) + c * 32, o);
+            tmem_ld_32x32b_x32(t_o + half * kCols + c * 32, o);
             if (store)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
@@ -507,53 +532,68 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         __syncwarp();
         if (elect_one()) mbar_arrive(&o_free[t]);
       } else if (store) {
-        for (int i = 0; i < D / 16; ++i) st_global_v8(dst + i * (kTcRows * 8), 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < kCols / 8; ++i) st_global_v8(dst + i * (kTcRows * 8), 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f);
       }
     }
     if (!ok) give_up();
-  } else if (warp >= kConvert) {
-    // ---- 8-bit values to bf16 operands: a warp 16 keys, D / 8 lanes a key ----
+  } else if (warp >= kConvert<BITS>) {
+    // ---- 8-bit values to bf16 operands: a warp a page of the tile, D / 8 lanes a key ----
     if constexpr (BITS == 8) {
-      constexpr int kKeys = kTcKeys / kConverters, kLanes = D / 8, kAtOnce = 32 / kLanes;
-      const int w = warp - kConvert, part = lane % kLanes;
+      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kSteps = kPageSize / kAtOnce;
+      static_assert(kConverters * kPageSize == kTcKeys, "a warp a page");
+      const int w = warp - kConvert<BITS>, part = lane % kLanes;
       bool ok = true;
       int pos = 0;
       TcUnit u;
       for (int x = start; ok && unit_at(a, plan, x, end, u);) {
+        const int n_pages = ceil_div(u.len, kPageSize);
+        const int32_t *table = a.prefix_table + (int64_t)u.i * a.max_prefix_pages;
+        // this warp's page of a tile, read two tiles ahead, and this lane's of its 32 scales (K's, then
+        // V's), read one tile ahead (a page that is not there has been copied as zeros)
+        auto page_of = [&](int j) { return j < u.t1 && j * 8 + w < n_pages ? ld_early(table + j * 8 + w) : -1; };
+        auto code_of = [&](int page) {
+          if (page < 0 || page >= a.n_pages) return 127u;
+          return ld_early_u8(scales + ((((int64_t)a.layer * a.n_pages + page) * 2 + (lane >> 4)) * a.Hkv + u.g) * kPageSize + (lane & 15));
+        };
+        int page = page_of(u.t0 + 1);
+        uint32_t code = code_of(page_of(u.t0));
         for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
-          const int rem = u.len - j * kTcKeys;
+          const int rem = u.len - (j * 8 + w) * kPageSize;   // keys from the page's first on
+          const float scale = e8m0_value(code);
+          const __nv_bfloat162 scale2 = __floats2bfloat162_rn(scale, scale);   // exact
+          const uint32_t factor = *reinterpret_cast<const uint32_t *>(&scale2);
+          code = code_of(page);
+          page = page_of(j + 2);
+#pragma unroll 1   // (as small as it gets: the code of all roles competes for the instruction cache)
           for (int kv = 0; kv < 2; ++kv) {
             const int raws = kv ? kRawV : kRawK, s = kv * kRawK + pos % raws, stages = kv ? VS : KS, to = pos % stages;
-            ok = wwait(&raw_full[s], (uint32_t)(pos / raws & 1)) &&
-                 wwait(kv ? &v_empty[to] : &k_empty[to], (uint32_t)(pos / stages & 1) ^ 1u);
+            ok = wwait(&raw_full[s], (uint32_t)(pos / raws & 1));
             if (!ok) break;
-            const uint8_t *raw = smem + L::kRawAt + s * L::kRaw, *scales = smem + L::kScales + s * 8 * 128;
-            uint8_t *dst = smem + (kv ? L::kV : L::kK) + to * L::kTile + (part >> 3) * (kTcKeys * 128);
-            // (all loads first: a warp alone on its scheduler waits for each otherwise)
-            uint2 v[kKeys / kAtOnce];
-            uint8_t code[kKeys / kAtOnce];
+            const uint8_t *raw = smem + L::kRawAt + s * L::kRaw + w * (kPageSize * D) + part * 8;
+            ok = wwait(kv ? &v_empty[to] : &k_empty[to], (uint32_t)(pos / stages & 1) ^ 1u);
+            if (!ok) break;
+            uint8_t *dst = smem + (kv ? L::kV : L::kK) + to * L::kTile + (part >> 3) * (kTcKeys * 128) + w * (kPageSize * 128);
+#pragma unroll 1
+            for (int i0 = 0; i0 < kSteps; i0 += 4) {
+              uint2 v[4];   // (loads first: a warp nearly alone on its scheduler waits for each otherwise)
 #pragma unroll
-            for (int i = 0; i < kKeys / kAtOnce; ++i) {
-              const int key = w * kKeys + i * kAtOnce + lane / kLanes;
-              v[i] = *reinterpret_cast<const uint2 *>(raw + key * D + part * 8);
-              code[i] = scales[(key >> 4) * 128 + (key & 15)];
-            }
+              for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2 *>(raw + ((i0 + i) * kAtOnce + lane / kLanes) * D);
 #pragma unroll
-            for (int i = 0; i < kKeys / kAtOnce; ++i) {
-              const int key = w * kKeys + i * kAtOnce + lane / kLanes;
-              const float f = e8m0_value(code[i]);
-              const __nv_bfloat162 f2 = __floats2bfloat162_rn(f, f);   // exact
-              uint32_t out[4];
+              for (int i = 0; i < 4; ++i) {
+                const int key = (i0 + i) * kAtOnce + lane / kLanes;
+                const uint32_t f = __shfl_sync(0xffffffffu, factor, kv * 16 + key);
+                uint32_t out[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t h = f16x2_of_e4m3x2((e < 2 ? v[i].x : v[i].y) >> (e & 1) * 16);
-                const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-                const __nv_bfloat162 b = __hmul2(__floats2bfloat162_rn(y.x, y.y), f2);
-                out[e] = *reinterpret_cast<const uint32_t *>(&b);
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t h = f16x2_of_e4m3x2((e < 2 ? v[i].x : v[i].y) >> (e & 1) * 16);
+                  const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+                  const __nv_bfloat162 b = __hmul2(__floats2bfloat162_rn(y.x, y.y), *reinterpret_cast<const __nv_bfloat162 *>(&f));
+                  out[e] = *reinterpret_cast<const uint32_t *>(&b);
+                }
+                if (key >= rem) out[0] = out[1] = out[2] = out[3] = 0u;
+                *reinterpret_cast<uint4 *>(dst + key * 128 + (((part & 7) ^ (key & 7)) << 4)) =
+                    make_uint4(out[0], out[1], out[2], out[3]);
               }
-              if (rem < kTcKeys && key >= rem) out[0] = out[1] = out[2] = out[3] = 0u;
-              *reinterpret_cast<uint4 *>(dst + key * 128 + (((part & 7) ^ (key & 7)) << 4)) =
-                  make_uint4(out[0], out[1], out[2], out[3]);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -582,7 +622,7 @@ bool launch(const CacheView &kv, const PagesArgs &a, const PagesWs &ws, cudaStre
   static_assert(L::kMost + 6144 <= 232448, "shared memory of a CTA");
   EncodeTiledFn enc = get_encode_tiled();
   if (!enc) return false;
-  CUtensorMap q_map, kv_map, scale_map;
+  CUtensorMap q_map, kv_map;
   const cuuint32_t one[5] = {1, 1, 1, 1, 1};
   const cuuint64_t H = kv.n_kv_heads, N = (cuuint64_t)kv.n_layers * (cuuint64_t)kv.n_pages, row = D * BITS / 8, G = a.G;
   const cuuint64_t q_dims[4] = {(cuuint64_t)D, G, H, (cuuint64_t)a.B};
@@ -600,20 +640,11 @@ bool launch(const CacheView &kv, const PagesArgs &a, const PagesWs &ws, cudaStre
           BITS == 8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return false;
-  scale_map = kv_map;
-  if (BITS == 8) {
-    const cuuint64_t sdims[4] = {16, H, 2, N}, sstrides[3] = {16, 16 * H, 32 * H};
-    const cuuint32_t sbox[4] = {16, 1, 1, 1};
-    if (enc(&scale_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, kv.scales, sdims, sstrides, sbox, one,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return false;
-  }
   auto kern = prefix_tc_kernel<D, BITS>;
   if (!allow_smem(kern, L::kMost)) return false;
   const size_t smem = L::kPlan + 1024 + 12 * ((size_t)a.n_prefixes + 1);
   return launch_pdl(kern, dim3((unsigned)std::max(1, num_sms)), dim3(kTcThreads<BITS>), smem, stream, q_map, kv_map,
-                    scale_map, a, ws) == cudaSuccess;
+                    static_cast<const uint8_t *>(kv.scales), a, ws) == cudaSuccess;
 }
 
 }  // namespace
