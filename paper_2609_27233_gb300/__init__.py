@@ -151,21 +151,25 @@ class Kv8Pool:
     """An 8-bit paged cache: values torch.float8_e4m3fn [layers][pages][2][Hkv][16][D] and scales
     torch.float8_e8m0fnu [layers][pages][2][Hkv][16], an entry's value times its row's scale.  It holds the two
     tensors and copies nothing."""
-    __slots__ = ("values", "scales", "layers", "pages", "heads", "head_dim", "device", "_c")
+    __slots__ = ("values", "scales", "layers", "heads", "head_dim", "_c")
 
     def __init__(self, values, scales):
         shape = values.shape
-        if values.dtype != torch.float8_e4m3fn or len(shape) != 6 or shape[2] != 2 or not values.is_contiguous():
+        if values.dtype is not _E4M3 or len(shape) != 6 or shape[2] != 2 or not values.is_contiguous():
             raise ValueError("values must be contiguous float8_e4m3fn [layers][pages][2][Hkv][16][D]")
-        if scales.dtype != torch.float8_e8m0fnu or scales.shape != shape[:5] or not scales.is_contiguous():
+        if scales.dtype is not _E8M0 or scales.shape != shape[:5] or not scales.is_contiguous():
             raise ValueError("scales must be contiguous float8_e8m0fnu [layers][pages][2][Hkv][16]")
-        _on_gpu(values)
-        if scales.device != values.device:
-            raise ValueError("values and scales must be on one device")
-        self.values, self.scales, self.device = values, scales, values.device
-        self.layers, self.pages, _, self.heads, page_size, self.head_dim = shape
-        self._c = _pack_kv8(values.data_ptr(), scales.data_ptr(), self.layers, self.pages, self.heads, page_size,
+        where = values.get_device()
+        if where < 0 or scales.get_device() != where:
+            raise ValueError("expected CUDA tensors on one device")
+        self.values, self.scales = values, scales
+        self.layers, pages, _, self.heads, page_size, self.head_dim = shape
+        self._c = _pack_kv8(values.data_ptr(), scales.data_ptr(), self.layers, pages, self.heads, page_size,
                             self.head_dim)
+
+    @property
+    def device(self):
+        return self.values.device
 
     @classmethod
     def zeros(cls, layers, pages, heads, head_dim, device, stream=None):
@@ -184,6 +188,7 @@ def paged_kv(pool):
 # the layouts of umim_paged_kv, umim_paged_kv8 and umim_merge_weights (native alignment)
 _pack_kv = struct.Struct("@P5i4x").pack
 _pack_kv8 = struct.Struct("@2P5i4x").pack
+_I32, _BF16, _E4M3, _E8M0 = torch.int32, torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
 _pack_weights = struct.Struct("@9P2if4x").pack
 _WEIGHTS = ("w_kv", "b_kv", "ln_kv_gamma", "ln_kv_beta", "query", "w_o", "b_o", "ln_o_gamma", "ln_o_beta")
 
@@ -416,50 +421,57 @@ def umim_decode_attention_static(q, pool, layer, block_table, seq_lens, scale=0.
 # ---------------------------------------------------------------------------
 # the 8-bit cache, and decode attention over it and over shared prefixes
 # ---------------------------------------------------------------------------
-def _ints(t, shape, what):
-    """The address of a contiguous device int32 tensor of the given shape, or None."""
+# (a call's checks take about as long as its launch: few lookups, and shapes only where the count of elements says too little)
+def _ints(t, n, what):
+    """The address of a contiguous device int32 tensor of n elements, or None."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what} must be a contiguous CUDA int32 tensor of shape {tuple(shape)}")
+    if t.dtype is not _I32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous CUDA int32 tensor of {n}")
     return t.data_ptr()
 
 
 def _table(t, what):
     """(address, rows, columns) of a block table."""
-    if t.dim() != 2:
-        raise ValueError(f"{what} must be [rows][pages]")
-    rows, cols = t.shape
-    return _ints(t, (rows, cols), what), rows, cols
-
-
-def _kv_rows(t, n, heads, head_dim, what):
-    """(address, row stride) of bf16 rows [n][heads][head_dim], which may be strided."""
-    if t.dtype != torch.bfloat16 or t.shape != (n, heads, head_dim) or not t.is_cuda:
-        raise ValueError(f"{what} must be CUDA bf16 [{n}][{heads}][{head_dim}]")
-    st = t.stride()
-    if st[2] != 1 or (st[1] != head_dim and heads > 1):
-        raise ValueError(f"the heads of a row of {what} must be contiguous")
-    if n > 1 and st[0] < heads * head_dim:
-        raise ValueError(f"the rows of {what} overlap")
-    return t.data_ptr(), (st[0] if n > 1 else 0)
+    shape = t.shape
+    if len(shape) != 2 or t.dtype is not _I32 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous CUDA int32 tensor [rows][pages]")
+    return t.data_ptr(), shape[0], shape[1]
 
 
 def _whole(t, shape, what):
     """The address of a contiguous bf16 device tensor of the given shape, or None."""
     if t is None:
         return None
-    if t.dtype != torch.bfloat16 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not _BF16 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous CUDA bf16 tensor of shape {tuple(shape)}")
     return t.data_ptr()
+
+
+def _kv_rows(k, v, n, heads, head_dim):
+    """(address of k, of v, row stride) of bf16 rows [n][heads][head_dim], which may be strided, both alike."""
+    shape, st = (n, heads, head_dim), k.stride()
+    if k.dtype is not _BF16 or v.dtype is not _BF16 or k.shape != shape or v.shape != shape or not k.is_cuda or not v.is_cuda:
+        raise ValueError(f"k and v must be CUDA bf16 [{n}][{heads}][{head_dim}]")
+    if n < 2:   # (a single row's stride says nothing)
+        st = (0,) + st[1:]
+        if v.stride()[1:] != st[1:]:
+            raise ValueError("k and v must have the same strides")
+    elif v.stride() != st:
+        raise ValueError("k and v must have the same strides")
+    elif st[0] < heads * head_dim:
+        raise ValueError("rows of k and v overlap")
+    if st[2] != 1 or (st[1] != head_dim and heads > 1):
+        raise ValueError("the heads of a row of k and v must be contiguous")
+    return k.data_ptr(), v.data_ptr(), st[0]
 
 
 def _query(q, heads, head_dim):
     """(address, batch, query heads) of q [B][Hq][D]."""
     shape = q.shape
-    if len(shape) != 3 or shape[2] != head_dim:
-        raise ValueError(f"q must be [batch][query heads][{head_dim}]")
-    return _whole(q, shape, "q"), shape[0], shape[1]
+    if len(shape) != 3 or shape[2] != head_dim or q.dtype is not _BF16 or not q.is_cuda or not q.is_contiguous():
+        raise ValueError(f"q must be contiguous CUDA bf16 [batch][query heads][{head_dim}]")
+    return q.data_ptr(), shape[0], shape[1]
 
 
 def umim_kv8_write(pool, layer, block_table, start, k, v, cu_rows=None, dev_status=None, stream=None):
@@ -468,12 +480,9 @@ def umim_kv8_write(pool, layer, block_table, start, k, v, cu_rows=None, dev_stat
     sequence b."""
     table, B, cols = _table(block_table, "block_table")
     T = k.shape[0]
-    pk, stride = _kv_rows(k, T, pool.heads, pool.head_dim, "k")
-    pv, stride_v = _kv_rows(v, T, pool.heads, pool.head_dim, "v")
-    if stride != stride_v:
-        raise ValueError("k and v must have the same row stride")
-    code = lib().umim_kv8_write(pool._c, layer, table, cols, _ints(start, (B,), "start"),
-                                _ints(cu_rows, (B + 1,), "cu_rows"), B, pk, pv, stride, T, _p(dev_status),
+    pk, pv, stride = _kv_rows(k, v, T, pool.heads, pool.head_dim)
+    code = lib().umim_kv8_write(pool._c, layer, table, cols, _ints(start, B, "start"),
+                                _ints(cu_rows, B + 1, "cu_rows"), B, pk, pv, stride, T, _p(dev_status),
                                 _stream(stream))
     _check(code, "umim_kv8_write")
 
@@ -483,16 +492,13 @@ def umim_kv8_read(pool, layer, block_table, start, n_rows, cu_rows=None, out=Non
     such tensors (rows may be strided, both alike); rows of no sequence are left as they are."""
     table, B, cols = _table(block_table, "block_table")
     if out is None:
-        make = lambda: _made(stream, torch.empty, (n_rows, pool.heads, pool.head_dim), dtype=torch.bfloat16,
-                             device=pool.device)
-        out = make(), make()
-    k, v = out
-    pk, stride = _kv_rows(k, n_rows, pool.heads, pool.head_dim, "k")
-    pv, stride_v = _kv_rows(v, n_rows, pool.heads, pool.head_dim, "v")
-    if stride != stride_v:
-        raise ValueError("k and v must have the same row stride")
-    code = lib().umim_kv8_read(pool._c, layer, table, cols, _ints(start, (B,), "start"),
-                               _ints(cu_rows, (B + 1,), "cu_rows"), B, pk, pv, stride, n_rows, _p(dev_status),
+        k = _made(stream, torch.empty, (n_rows, pool.heads, pool.head_dim), dtype=_BF16, device=pool.values.device)
+        v = _made(stream, torch.empty_like, k)
+    else:
+        k, v = out
+    pk, pv, stride = _kv_rows(k, v, n_rows, pool.heads, pool.head_dim)
+    code = lib().umim_kv8_read(pool._c, layer, table, cols, _ints(start, B, "start"),
+                               _ints(cu_rows, B + 1, "cu_rows"), B, pk, pv, stride, n_rows, _p(dev_status),
                                _stream(stream))
     _check(code, "umim_kv8_read")
     return k, v
@@ -503,16 +509,19 @@ def umim_kv8_append_merge(pool, block_table, seq_lens, new_k, new_v, new_pages=N
     """umim_decode_append_merge for a Kv8Pool: the new (or surrogate) rows, bf16, quantised as they are
     written.  Returns released [B] int32."""
     table, B, cols = _table(block_table, "block_table")
-    row = (pool.layers, pool.heads, pool.head_dim)
+    lens = _ints(seq_lens, B, "seq_lens")
+    row = (B, pool.layers, pool.heads, pool.head_dim)
     if released is None:
-        released = _made(stream, torch.empty, B, dtype=torch.int32, device=pool.device)
-    n_rows = 0 if surrogate_k is None else surrogate_k.shape[0]
+        released = _made(stream, torch.empty_like, seq_lens)
+    n_rows, rows = 0, row
+    if surrogate_k is not None:
+        n_rows = surrogate_k.shape[0]
+        rows = (n_rows,) + row[1:]
     code = lib().umim_kv8_append_merge(
-        pool._c, table, cols, _ints(seq_lens, (B,), "seq_lens"), B, _whole(new_k, (B,) + row, "new_k"),
-        _whole(new_v, (B,) + row, "new_v"), _ints(new_pages, (B,), "new_pages"), _ints(merge_k, (B,), "merge_k"),
-        _ints(merge_row, (B,), "merge_row"), n_rows, _whole(surrogate_k, (n_rows,) + row, "surrogate_k"),
-        _whole(surrogate_v, (n_rows,) + row, "surrogate_v"), _ints(released, (B,), "released"), _p(dev_status),
-        _stream(stream))
+        pool._c, table, cols, lens, B, _whole(new_k, row, "new_k"), _whole(new_v, row, "new_v"),
+        _ints(new_pages, B, "new_pages"), _ints(merge_k, B, "merge_k"), _ints(merge_row, B, "merge_row"), n_rows,
+        _whole(surrogate_k, rows, "surrogate_k"), _whole(surrogate_v, rows, "surrogate_v"),
+        _ints(released, B, "released"), _p(dev_status), _stream(stream))
     _check(code, "umim_kv8_append_merge")
     return released
 
@@ -530,12 +539,15 @@ def umim_decode_attention_kv8(q, pool, layer, block_table, seq_lens, scale=0.0, 
         raise ValueError("block_table must have a row for every sequence")
     if out is None:
         out = _made(stream, torch.empty_like, q)
+        p_out = out.data_ptr()
+    else:
+        p_out = _whole(out, q.shape, "out")
     if workspace_buf is None:
         workspace_buf = workspace(umim_decode_attention_kv8_workspace_size(B, Hq, pool.heads, pool.head_dim), q.device,
                                   stream)
-    code = lib().umim_decode_attention_kv8(pq, Hq, pool._c, layer, table, cols, _ints(seq_lens, (B,), "seq_lens"), B,
-                                           float(scale), _whole(out, q.shape, "out"), workspace_buf.data_ptr(),
-                                           workspace_buf.numel(), _p(dev_status), _stream(stream))
+    code = lib().umim_decode_attention_kv8(pq, Hq, pool._c, layer, table, cols, _ints(seq_lens, B, "seq_lens"), B,
+                                           float(scale), p_out, workspace_buf.data_ptr(), workspace_buf.numel(),
+                                           _p(dev_status), _stream(stream))
     _check(code, "umim_decode_attention_kv8")
     return out
 
@@ -553,14 +565,16 @@ def _shared(call, q, cache, heads, head_dim, layer, prefix_table, prefix_lens, b
         raise ValueError("block_table must have a row for every sequence")
     if out is None:
         out = _made(stream, torch.empty_like, q)
+        p_out = out.data_ptr()
+    else:
+        p_out = _whole(out, q.shape, "out")
     if workspace_buf is None:
         workspace_buf = workspace(umim_decode_attention_shared_workspace_size(B, n, Hq, heads, head_dim), q.device,
                                   stream)
     code = getattr(lib(), call)(
-        pq, Hq, cache, layer, prefixes, prefix_cols, _ints(prefix_lens, (n,), "prefix_lens"),
-        _ints(prefix_offsets, (n + 1,), "prefix_offsets"), n, table, cols, _ints(seq_lens, (B,), "seq_lens"), B,
-        float(scale), _whole(out, q.shape, "out"), workspace_buf.data_ptr(), workspace_buf.numel(), _p(dev_status),
-        _stream(stream))
+        pq, Hq, cache, layer, prefixes, prefix_cols, _ints(prefix_lens, n, "prefix_lens"),
+        _ints(prefix_offsets, n + 1, "prefix_offsets"), n, table, cols, _ints(seq_lens, B, "seq_lens"), B,
+        float(scale), p_out, workspace_buf.data_ptr(), workspace_buf.numel(), _p(dev_status), _stream(stream))
     _check(code, call)
     return out
 
