@@ -87,7 +87,7 @@ size_t decode_attention_workspace_bytes(int B, int Hq, int Hkv, int D, int num_s
 umim_status decode_attention(const void *, int, const umim_paged_kv *, int, const int32_t *, int, const int32_t *,
                              int, float, void *, void *, int32_t *, cudaStream_t, int);
 umim_status kv8_rows(bool, const umim_paged_kv8 *, int, const int32_t *, int, const int32_t *, const int32_t *, int,
-                     void *, void *, int, int64_t, int32_t *, cudaStream_t, int);
+                     void *, void *, int, int64_t, int32_t *, cudaStream_t);
 umim_status kv8_append_merge(const umim_paged_kv8 *, int32_t *, int32_t, int32_t *, int32_t, const void *, const void *,
                              const int32_t *, const int32_t *, const int32_t *, int32_t, const void *, const void *,
                              int32_t *, int32_t *, cudaStream_t);
@@ -657,7 +657,7 @@ umim_status kv8_rows_checked(bool write, const umim_paged_kv8 *kv, int32_t layer
   if (!block_table || !start || !k || !v || !aligned(k, 16) || !aligned(v, 16)) return UMIM_ERR_INVALID_ARG;
   const DeviceScope scope(stream);
   return kv8_rows(write, kv, layer, block_table, max_pages, start, cu_rows, batch, k, v, n_rows, row_stride, dev_status,
-                  stream, scope.sms());
+                  stream);
 }
 
 umim_status shared_checked(const void *q, int32_t n_q_heads, void *values, void *scales, int32_t n_layers,

@@ -4,7 +4,7 @@
 // A row is one head's K or V of one entry, D bf16 values: largest magnitude,
 // scale code, D e4m3 codes (kv8.cuh has the rounding).  Bytes bound the calls on
 // many rows: 2 D read and D + 1 written a row.  D / 16 lanes hold a row, 16
-// values each (two 16-byte loads, one 16-byte store), so a warp takes 4 (D = 128)
+// values each (32 bytes and 16), so a warp takes 4 (D = 128)
 // or 8 rows at once; the largest magnitude is a maximum of the bf16 bit patterns,
 // which order as the magnitudes do, over packed pairs and then over the row's lanes.
 // Scaling by a power of two is exact in fp32, so a value is rounded once.
@@ -21,6 +21,9 @@ constexpr int kRowThreads = 256;
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 4;    // rows in flight a group of lanes
 constexpr int kMaxCluster = 8;    // CTAs per sequence (portable cluster size)
+// Heads of K and V that a warp takes of its rows.  Two: 32768 rows of 8 heads, D = 128, written in 36.9 us
+// (one 45, four 37, eight 39, sixteen 52), 65536 read in 63.6 (one 79, eight 64).
+constexpr int kRowHeads = 2;
 
 template <int D>
 constexpr int kRowLanes = D / 16;   // lanes of a row
@@ -39,10 +42,32 @@ __device__ __forceinline__ uint4 ld_row_v4(const void *p) {
   return v;
 }
 
+// A lane's 32 bytes in one access where rows start on 32-byte boundaries, else in two: rows a
+// multiple of 16 bytes apart are all that a call asks for.
+template <bool WIDE>
 __device__ __forceinline__ void load_row(const uint16_t *p, Row &r) {
+  if constexpr (WIDE) {
+    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r.x[0]), "=r"(r.x[1]), "=r"(r.x[2]), "=r"(r.x[3]), "=r"(r.x[4]), "=r"(r.x[5]), "=r"(r.x[6]),
+                   "=r"(r.x[7])
+                 : "l"(p));
+    return;
+  }
   const uint4 a = ld_row_v4(p), b = ld_row_v4(p + 8);
   r.x[0] = a.x, r.x[1] = a.y, r.x[2] = a.z, r.x[3] = a.w;
   r.x[4] = b.x, r.x[5] = b.y, r.x[6] = b.z, r.x[7] = b.w;
+}
+
+template <bool WIDE>
+__device__ __forceinline__ void store_row(uint16_t *p, const uint32_t (&x)[8]) {
+  if constexpr (WIDE) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]),
+                 "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4 *>(p)[0] = make_uint4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<uint4 *>(p)[1] = make_uint4(x[4], x[5], x[6], x[7]);
+  }
 }
 
 // The row's codes (16 of this lane) and its scale code.  Every lane of the warp takes part.
@@ -152,10 +177,11 @@ __device__ __forceinline__ void check_rows(const RowsArgs &a) {
   if (bad) set_error(a.status, UMIM_ERR_INVALID_ARG);
 }
 
-// One warp: kWarpRows consecutive rows (a row's page is looked up once) of U heads of K and V,
-// whose loads are in flight while the page is looked up.
-template <int D, int U>
+// One warp: kWarpRows consecutive rows of U heads of K and V, whose loads are in flight while the
+// rows' pages are looked up.
+template <int D, bool WIDE>
 __global__ void __launch_bounds__(kRowThreads) kv8_write_kernel(RowsArgs a) {
+  constexpr int U = kRowHeads;
   griddep_wait();
   if (blockIdx.x == 0) check_rows(a);
   const int lane = threadIdx.x & 31, heads = 2 * a.n_kv_heads, parts = ceil_div(heads, U);
@@ -168,7 +194,7 @@ __global__ void __launch_bounds__(kRowThreads) kv8_write_kernel(RowsArgs a) {
   for (int u = 0; u < U; ++u) {
     const int h = h0 + u;
     if (t < a.T && h < heads)
-      load_row((h < a.n_kv_heads ? a.k + h * D : a.v + (h - a.n_kv_heads) * D) + t * a.stride + col, r[u]);
+      load_row<WIDE>((h < a.n_kv_heads ? a.k + h * D : a.v + (h - a.n_kv_heads) * D) + t * a.stride + col, r[u]);
     else
       r[u] = Row{};
   }
@@ -186,8 +212,9 @@ __global__ void __launch_bounds__(kRowThreads) kv8_write_kernel(RowsArgs a) {
   }
 }
 
-template <int D, int U>
+template <int D, bool WIDE>
 __global__ void __launch_bounds__(kRowThreads) kv8_read_kernel(RowsArgs a) {
+  constexpr int U = kRowHeads;
   griddep_wait();
   if (blockIdx.x == 0) check_rows(a);
   const int lane = threadIdx.x & 31, heads = 2 * a.n_kv_heads, parts = ceil_div(heads, U);
@@ -226,8 +253,7 @@ __global__ void __launch_bounds__(kRowThreads) kv8_read_kernel(RowsArgs a) {
       out[i] = *reinterpret_cast<const uint32_t *>(&y);
     }
     uint16_t *p = (h < a.n_kv_heads ? a.k + h * D : a.v + (h - a.n_kv_heads) * D) + t * a.stride + col;
-    reinterpret_cast<uint4 *>(p)[0] = make_uint4(out[0], out[1], out[2], out[3]);
-    reinterpret_cast<uint4 *>(p)[1] = make_uint4(out[4], out[5], out[6], out[7]);
+    store_row<WIDE>(p, out);
   }
 }
 
@@ -271,7 +297,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(AppendArgs a
       r[u] = Row{};
       if (i < total) {
         const int layer = i / (2 * Hkv), kv = (i / Hkv) & 1, h = i % Hkv;
-        load_row((kv ? v : k) + (((int64_t)src * a.n_layers + layer) * Hkv + h) * D + col, r[u]);
+        load_row<false>((kv ? v : k) + (((int64_t)src * a.n_layers + layer) * Hkv + h) * D + col, r[u]);
       }
     }
   };
@@ -343,14 +369,11 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(AppendArgs a
 }
 
 template <int D, bool WRITE>
-umim_status launch_rows(const RowsArgs &a, cudaStream_t stream, int sms) {
-  // Few rows: two heads a warp, so that more of them share the work; eight once that
-  // makes more warps than the GPU holds.
-  const int heads = 2 * a.n_kv_heads, tiles = ceil_div(a.T, kWarpRows<D>);
-  const bool many = (int64_t)tiles * ceil_div(heads, 8) >= (int64_t)sms * 16;
-  auto kern = WRITE ? (many ? kv8_write_kernel<D, 8> : kv8_write_kernel<D, 2>)
-                    : (many ? kv8_read_kernel<D, 8> : kv8_read_kernel<D, 2>);
-  const int64_t warps = (int64_t)tiles * ceil_div(heads, many ? 8 : 2);
+umim_status launch_rows(const RowsArgs &a, cudaStream_t stream) {
+  const bool wide = reinterpret_cast<uintptr_t>(a.k) % 32 == 0 && reinterpret_cast<uintptr_t>(a.v) % 32 == 0 && a.stride % 16 == 0;
+  auto kern = WRITE ? (wide ? kv8_write_kernel<D, true> : kv8_write_kernel<D, false>)
+                    : (wide ? kv8_read_kernel<D, true> : kv8_read_kernel<D, false>);
+  const int64_t warps = (int64_t)ceil_div(a.T, kWarpRows<D>) * ceil_div(2 * a.n_kv_heads, kRowHeads);
   const int64_t blocks = (warps + kRowThreads / 32 - 1) / (kRowThreads / 32);
   trace_mark(stream, WRITE ? "kv8.write" : "kv8.read");
   const cudaError_t e = launch_pdl(kern, dim3((unsigned)blocks), dim3(kRowThreads), 0, stream, a);
@@ -362,7 +385,7 @@ umim_status launch_rows(const RowsArgs &a, cudaStream_t stream, int sms) {
 
 umim_status kv8_rows(bool write, const umim_paged_kv8 *kv, int layer, const int32_t *block_table, int max_pages,
                      const int32_t *start, const int32_t *cu_rows, int B, void *k, void *v, int T, int64_t stride,
-                     int32_t *status, cudaStream_t stream, int sms) {
+                     int32_t *status, cudaStream_t stream) {
   RowsArgs a{};
   a.values = static_cast<uint8_t *>(kv->values);
   a.scales = static_cast<uint8_t *>(kv->scales);
@@ -380,8 +403,8 @@ umim_status kv8_rows(bool write, const umim_paged_kv8 *kv, int layer, const int3
   a.v = static_cast<uint16_t *>(v);
   a.stride = stride;
   a.status = status;
-  if (kv->head_dim == 128) return write ? launch_rows<128, true>(a, stream, sms) : launch_rows<128, false>(a, stream, sms);
-  return write ? launch_rows<64, true>(a, stream, sms) : launch_rows<64, false>(a, stream, sms);
+  if (kv->head_dim == 128) return write ? launch_rows<128, true>(a, stream) : launch_rows<128, false>(a, stream);
+  return write ? launch_rows<64, true>(a, stream) : launch_rows<64, false>(a, stream);
 }
 
 umim_status kv8_append_merge(const umim_paged_kv8 *kv, int32_t *block_table, int32_t max_pages, int32_t *seq_lens,
