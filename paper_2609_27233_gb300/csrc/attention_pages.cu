@@ -119,8 +119,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   }
   __syncwarp();
   griddep_wait();
-  // the tensor cores' kernel, if that follows, starts as this one's CTAs leave; it reads nothing of this one's
-  if (SHARED) griddep_launch();
+  // The tensor cores' kernel, if that follows, is placed as this one's CTAs leave; it reads nothing of this one's.
+  // (The combine kernel placed that early cost a call of 34 us four.)
+  if (SHARED && a.most_rows != INT32_MAX) griddep_launch();
 
   const int G = a.G, Hkv = a.Hkv;
   const int32_t *pref = ws.at.pref;

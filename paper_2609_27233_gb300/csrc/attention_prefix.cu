@@ -26,8 +26,8 @@
 // the operands' place.  The last page is loaded from row n - 16 on where it holds n <
 // 16 entries: TMA reads rows before the first as zeros, so that nothing behind the
 // prefix's end is ever read; S is masked there.
-// 8-bit pages: e4m3 rows into rings of their own, from which eight warps (a page
-// each) make the bf16 operands, value * 2^e (exact), zeros behind the end.
+// 8-bit pages: e4m3 rows into rings of their own, from which eight warps (four for K,
+// four for V) make the bf16 operands, value * 2^e (exact), zeros behind the end.
 #include <cuda_fp16.h>
 
 #include "attention_pages.cuh"
@@ -146,9 +146,9 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&k_full[s], BITS == 8 ? kConverters : 1);
+      mbar_init(&k_full[s], BITS == 8 ? kConverters / 2 : 1);
       mbar_init(&k_empty[s], 2);   // read by both slots' products, or twice by one's
-      mbar_init(&v_full[s], BITS == 8 ? kConverters : 1);
+      mbar_init(&v_full[s], BITS == 8 ? kConverters / 2 : 1);
       mbar_init(&v_empty[s], 2);
       mbar_init(&q_full[s], 1);
       mbar_init(&q_empty[s], 1);     // a unit's S products have read the slot's Q
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     }
     for (int s = 0; s < kRawStages; ++s) {
       mbar_init(&raw_full[s], 1);
-      mbar_init(&raw_empty[s], kConverters);
+      mbar_init(&raw_empty[s], kConverters / 2);
     }
     fence_mbar_init();
     prefetch_tensormap(&q_map);
@@ -537,70 +537,74 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     }
     if (!ok) give_up();
   } else if (warp >= kConvert<BITS>) {
-    // ---- 8-bit values to bf16 operands: a warp a page of the tile, D / 8 lanes a key ----
+    // ---- 8-bit values to bf16 operands: half the warps for K and half for V (each has its own to wait
+    // for), a warp two pages of a tile, D / 8 lanes a key ----
     if constexpr (BITS == 8) {
-      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kSteps = kPageSize / kAtOnce;
-      static_assert(kConverters * kPageSize == kTcKeys, "a warp a page");
-      const int w = warp - kConvert<BITS>, part = lane % kLanes;
+      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kSteps = kPageSize / kAtOnce, kGroup = kConverters / 2;
+      static_assert(kGroup * 2 * kPageSize == kTcKeys, "a warp two pages");
+      const int kv = (warp - kConvert<BITS>) / kGroup, w = (warp - kConvert<BITS>) % kGroup, part = lane % kLanes;
+      const int raws = kv ? kRawV : kRawK, stages = kv ? VS : KS;
+      uint64_t *const raw_f = raw_full + kv * kRawK, *const raw_e = raw_empty + kv * kRawK;
+      uint64_t *const full = kv ? v_full : k_full, *const empty = kv ? v_empty : k_empty;
+      const uint8_t *const raw0 = smem + L::kRawAt + kv * kRawK * L::kRaw + 2 * w * (kPageSize * D) + lane / kLanes * D + part * 8;
+      uint8_t *const dst0 = smem + (kv ? L::kV : L::kK) + (part >> 3) * (kTcKeys * 128);
       bool ok = true;
       int pos = 0;
       TcUnit u;
       for (int x = start; ok && unit_at(a, plan, x, end, u);) {
         const int n_pages = ceil_div(u.len, kPageSize);
         const int32_t *table = a.prefix_table + (int64_t)u.i * a.max_prefix_pages;
-        // this warp's page of a tile, read two tiles ahead, and this lane's of its 32 scales (K's, then
-        // V's), read one tile ahead (a page that is not there has been copied as zeros)
-        auto page_of = [&](int j) { return j < u.t1 && j * 8 + w < n_pages ? ld_early(table + j * 8 + w) : -1; };
+        // this lane's key's page of a tile (16 lanes a page), read two tiles ahead, and the key's
+        // scale, read one tile ahead (a page that is not there has been copied as zeros)
+        auto page_of = [&](int j) {
+          const int at = j * 8 + 2 * w + (lane >> 4);
+          return j < u.t1 && at < n_pages ? ld_early(table + at) : -1;
+        };
         auto code_of = [&](int page) {
           if (page < 0 || page >= a.n_pages) return 127u;
-          return ld_early_u8(scales + ((((int64_t)a.layer * a.n_pages + page) * 2 + (lane >> 4)) * a.Hkv + u.g) * kPageSize + (lane & 15));
+          return ld_early_u8(scales + ((((int64_t)a.layer * a.n_pages + page) * 2 + kv) * a.Hkv + u.g) * kPageSize + (lane & 15));
         };
         int page = page_of(u.t0 + 1);
         uint32_t code = code_of(page_of(u.t0));
         for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
-          const int rem = u.len - (j * 8 + w) * kPageSize;   // keys from the page's first on
+          const int rem = u.len - (j * 8 + 2 * w) * kPageSize;   // keys from the warp's first on
           const float scale = e8m0_value(code);
           const __nv_bfloat162 scale2 = __floats2bfloat162_rn(scale, scale);   // exact
           const uint32_t factor = *reinterpret_cast<const uint32_t *>(&scale2);
           code = code_of(page);
           page = page_of(j + 2);
-#pragma unroll 1   // (as small as it gets: the code of all roles competes for the instruction cache)
-          for (int kv = 0; kv < 2; ++kv) {
-            const int raws = kv ? kRawV : kRawK, s = kv * kRawK + pos % raws, stages = kv ? VS : KS, to = pos % stages;
-            ok = wwait(&raw_full[s], (uint32_t)(pos / raws & 1));
-            if (!ok) break;
-            const uint8_t *raw = smem + L::kRawAt + s * L::kRaw + w * (kPageSize * D) + part * 8;
-            ok = wwait(kv ? &v_empty[to] : &k_empty[to], (uint32_t)(pos / stages & 1) ^ 1u);
-            if (!ok) break;
-            uint8_t *dst = smem + (kv ? L::kV : L::kK) + to * L::kTile + (part >> 3) * (kTcKeys * 128) + w * (kPageSize * 128);
-#pragma unroll 1
-            for (int i0 = 0; i0 < kSteps; i0 += 4) {
-              uint2 v[4];   // (loads first: a warp nearly alone on its scheduler waits for each otherwise)
+          const int s = pos % raws, to = pos % stages;
+          ok = wwait(&raw_f[s], (uint32_t)(pos / raws & 1)) && wwait(&empty[to], (uint32_t)(pos / stages & 1) ^ 1u);
+          if (!ok) break;
+          const uint8_t *raw = raw0 + s * L::kRaw;
+          uint8_t *dst = dst0 + to * L::kTile;
+#pragma unroll 1   // (not larger than it has to be: the code of all roles competes for the instruction cache)
+          for (int i0 = 0; i0 < 2 * kSteps; i0 += 4) {
+            uint2 v[4];   // (loads first: a warp nearly alone on its scheduler waits for each otherwise)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2 *>(raw + ((i0 + i) * kAtOnce + lane / kLanes) * D);
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2 *>(raw + (i0 + i) * kAtOnce * D);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int key = (i0 + i) * kAtOnce + lane / kLanes;
-                const uint32_t f = __shfl_sync(0xffffffffu, factor, kv * 16 + key);
-                uint32_t out[4];
+            for (int i = 0; i < 4; ++i) {
+              const int key = (i0 + i) * kAtOnce + lane / kLanes, row = 2 * w * kPageSize + key;
+              const uint32_t f = __shfl_sync(0xffffffffu, factor, key);
+              uint32_t out[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const uint32_t h = f16x2_of_e4m3x2((e < 2 ? v[i].x : v[i].y) >> (e & 1) * 16);
-                  const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-                  const __nv_bfloat162 b = __hmul2(__floats2bfloat162_rn(y.x, y.y), *reinterpret_cast<const __nv_bfloat162 *>(&f));
-                  out[e] = *reinterpret_cast<const uint32_t *>(&b);
-                }
-                if (key >= rem) out[0] = out[1] = out[2] = out[3] = 0u;
-                *reinterpret_cast<uint4 *>(dst + key * 128 + (((part & 7) ^ (key & 7)) << 4)) =
-                    make_uint4(out[0], out[1], out[2], out[3]);
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t h = f16x2_of_e4m3x2((e < 2 ? v[i].x : v[i].y) >> (e & 1) * 16);
+                const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+                const __nv_bfloat162 b = __hmul2(__floats2bfloat162_rn(y.x, y.y), *reinterpret_cast<const __nv_bfloat162 *>(&f));
+                out[e] = *reinterpret_cast<const uint32_t *>(&b);
               }
+              if (key >= rem) out[0] = out[1] = out[2] = out[3] = 0u;
+              *reinterpret_cast<uint4 *>(dst + row * 128 + (((part & 7) ^ (row & 7)) << 4)) =
+                  make_uint4(out[0], out[1], out[2], out[3]);
             }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (elect_one()) {
-              mbar_arrive(kv ? &v_full[to] : &k_full[to]);
-              mbar_arrive(&raw_empty[s]);
-            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (elect_one()) {
+            mbar_arrive(&full[to]);
+            mbar_arrive(&raw_e[s]);
           }
         }
       }
