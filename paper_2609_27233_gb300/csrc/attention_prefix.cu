@@ -26,8 +26,15 @@
 // the operands' place.  The last page is loaded from row n - 16 on where it holds n <
 // 16 entries: TMA reads rows before the first as zeros, so that nothing behind the
 // prefix's end is ever read; S is masked there.
-// 8-bit pages: e4m3 rows into rings of their own, from which eight warps (four for K,
-// four for V) make the bf16 operands, value * 2^e (exact), zeros behind the end.
+//
+// 8-bit pages: eight warps read e4m3 rows and make fp16 operands of them, code * 2^(e - E) with E the largest e of the page's 16
+// rows (a row's values are exact down to 2^-24 * 2^E, 2^-32 of the page's largest; converting
+// to value * 2^e in bf16 took twice the instructions, and they bound the kernel).  q
+// becomes fp16 in place, below 2^15 by a power of two a row.  With r the row's and the page's
+// powers of two times the scale, and F the page's largest exponent of V's rows,
+//     w = 2^(r s + F - n + 7),   O = sum w v',   l = sum 2^(-F - 7) w,   out = 2^-7 O / l,
+// n the running maximum of r s + F: the weights that multiply V are at most 2^15 and are one
+// fp16 number each (2^-12 of themselves), and l is exact in fp32, a page's sum at a time.
 #include <cuda_fp16.h>
 
 #include "attention_pages.cuh"
@@ -38,18 +45,15 @@ namespace umim {
 namespace {
 
 constexpr uint32_t kTcTmemCols = 512;   // S of the slots at 0 and 128, O at 256 and 384
-constexpr int kRawK = 2, kRawV = 1, kRawStages = kRawK + kRawV;   // 8-bit: K and V tiles as they come
+constexpr int kTcStages = 2;            // K and V rings
 
-// shared memory (bytes, every piece 1024-aligned but the scales)
-template <int D, int BITS>
+// shared memory (bytes, every piece but the plan 1024-aligned)
+template <int D>
 struct TcSmem {
   static constexpr int kTile = 128 * D * 2;               // Q of a slot, K, V: D / 64 atoms of [128 rows][128 B]
-  static constexpr int kKStages = BITS == 8 ? 1 : 2, kVStages = 2;
-  static constexpr int kRaw = BITS == 8 ? 128 * D : 0;
   static constexpr int kK = 2 * kTile;
-  static constexpr int kV = kK + kKStages * kTile;
-  static constexpr int kRawAt = kV + kVStages * kTile;
-  static constexpr int kPlan = kRawAt + kRawStages * kRaw;
+  static constexpr int kV = kK + kTcStages * kTile;
+  static constexpr int kPlan = kV + kTcStages * kTile;
   static constexpr int kMost = kPlan + 12 * (kSharedMaxPrefixes + 1) + 1024;
 };
 // warps 0 and 3 copies, 1-2 products, from 4 on softmax, then the 8-bit values
@@ -101,6 +105,11 @@ __device__ __forceinline__ int ld_early(const int32_t *p) {
   asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(p));
   return v;
 }
+__device__ __forceinline__ uint2 ld_early_v2(const uint8_t *p) {
+  uint2 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
 __device__ __forceinline__ uint32_t ld_early_u8(const uint8_t *p) {
   uint16_t v;
   asm volatile("ld.global.u8 %0, [%1];" : "=h"(v) : "l"(p));
@@ -129,14 +138,15 @@ constexpr uint32_t kBMnMajor = 1u << 16;   // instruction descriptor: B is MN-ma
 template <int D, int BITS>
 __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     prefix_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap kv_map,
-                     const uint8_t *scales, PagesArgs a, PagesWs ws) {
-  using L = TcSmem<D, BITS>;
+                     const uint8_t *values, const uint8_t *scales, PagesArgs a, PagesWs ws) {
+  using L = TcSmem<D>;
   constexpr int DA = D / 64;
-  constexpr int KS = L::kKStages, VS = L::kVStages;
+  constexpr int KS = kTcStages;
   extern __shared__ __align__(1024) uint8_t tc_raw[];
   __shared__ __align__(8) uint64_t q_full[2], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2],
-      p_full[2][2], pv_done[2], o_free[2], turn[2], mma_done[2], raw_full[kRawStages], raw_empty[kRawStages],
-      met[2][4];
+      p_full[2][2], pv_done[2], o_free[2], turn[2], mma_done[2],
+      met[2][4], q_ready[2], scales_full[4];
+  __shared__ float4 s_scales[4][kTcKeys / kPageSize];   // 8-bit: of the last four key tiles' pages, 2^E, F, 2^(-F - 7)
   __shared__ float s_row[2][2][2][kTcRows];   // [tile's parity][slot][half]: a row's maximum, or sum
   __shared__ uint32_t tmem_base;
   __shared__ int s_abort;
@@ -146,9 +156,9 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&k_full[s], BITS == 8 ? kConverters / 2 : 1);
+      mbar_init(&k_full[s], BITS == 8 ? kConverters : 1);
       mbar_init(&k_empty[s], 2);   // read by both slots' products, or twice by one's
-      mbar_init(&v_full[s], BITS == 8 ? kConverters / 2 : 1);
+      mbar_init(&v_full[s], BITS == 8 ? kConverters : 1);
       mbar_init(&v_empty[s], 2);
       mbar_init(&q_full[s], 1);
       mbar_init(&q_empty[s], 1);     // a unit's S products have read the slot's Q
@@ -157,17 +167,15 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       mbar_init(&p_full[s][1], 4);   // keys 64-127
       mbar_init(&pv_done[s], 1);     // a tile's P V product has landed
       mbar_init(&o_free[s], 4 * kHalves<BITS>);   // a unit's epilogue has read O
+      mbar_init(&q_ready[s], 4);     // 8-bit: Q turned into fp16 (four softmax warps)
       for (int q = 0; q < 4; ++q) mbar_init(&met[s][q], 2);   // the two warps of 32 rows have left each other something
       mbar_init(&turn[s], 1);        // the other slot's products are issued
       mbar_init(&mma_done[s], 1);
     }
-    for (int s = 0; s < kRawStages; ++s) {
-      mbar_init(&raw_full[s], 1);
-      mbar_init(&raw_empty[s], kConverters / 2);
-    }
+    for (int s = 0; s < 4; ++s) mbar_init(&scales_full[s], kConverters);
     fence_mbar_init();
     prefetch_tensormap(&q_map);
-    prefetch_tensormap(&kv_map);
+    if (BITS == 16) prefetch_tensormap(&kv_map);
   }
   if (warp == 1) {
     tmem_alloc(&tmem_base, kTcTmemCols);
@@ -210,21 +218,16 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   };
 
   if (warp == 0 || warp == 3) {
-    // ---- copies, K's (and Q's) by one warp and V's by the other, a lane a box: two of a page for
-    // 16-bit pages of 128 columns.  (A box takes about 90 cycles to issue: one warp would
-    // be busy for as long as the products of a tile take.) ----
+    // ---- copies: Q, and 16-bit pages, K's by one warp and V's by the other, a lane a box: two of a
+    // page of 128 columns.  (A box takes about 90 cycles to issue: one warp would be
+    // busy for as long as the products of a tile take.) ----
     const int kv = warp == 0 ? 0 : 1;
-    constexpr int kStagesK = BITS == 16 ? KS : kRawK, kStagesV = BITS == 16 ? VS : kRawV;
-    const int stages = kv ? kStagesV : kStagesK;
-    uint64_t *full = BITS == 16 ? (kv ? v_full : k_full) : kv ? raw_full + kRawK : raw_full;
-    uint64_t *empty = BITS == 16 ? (kv ? v_empty : k_empty) : kv ? raw_empty + kRawK : raw_empty;
-    uint8_t *to = smem + (BITS == 16 ? (kv ? L::kV : L::kK) : L::kRawAt + kv * kRawK * L::kRaw);
+    uint64_t *const full = kv ? v_full : k_full, *const empty = kv ? v_empty : k_empty;
+    uint8_t *const to = smem + (kv ? L::kV : L::kK);
     int nq = 0, pos = 0;   // units, and key tiles
     bool ok = true;
     TcUnit u;
     for (int x = start; ok && unit_at(a, plan, x, end, u);) {
-      const int n_pages = ceil_div(u.len, kPageSize), part = u.len % kPageSize;
-      const int32_t *table = a.prefix_table + (int64_t)u.i * a.max_prefix_pages;
       for (int t = 0; t < 2 && ok && kv == 0; ++t) {
         if (nq > 0) ok = wwait(&q_empty[t], (uint32_t)(nq - 1) & 1u);
         if (ok && lane == 0) {
@@ -236,43 +239,37 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         }
       }
       ++nq;
-      const int pg = lane & 7;
+      if (BITS == 8) continue;
+      const int n_pages = ceil_div(u.len, kPageSize), part = u.len % kPageSize, pg = lane & 7;
+      const int32_t *table = a.prefix_table + (int64_t)u.i * a.max_prefix_pages;
       auto page_at = [&](int j) {   // read a tile ahead
         const int at = j * 8 + pg;
         return j < u.t1 && at < n_pages && in_bounds(at, a.max_prefix_pages, a.status, kSitePrefixTable) ? ld_early(table + at) : 0;
       };
       int page = page_at(u.t0);
       for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
-        const int at = j * 8 + pg, s = pos % stages;
+        const int at = j * 8 + pg, s = pos % kTcStages;
         int c = a.n_layers * a.n_pages;   // a coordinate past the tensor's last page: the copy reads zeros
         if (at < n_pages) {
           if (page >= 0 && page < a.n_pages) c = a.layer * a.n_pages + page;
           else set_error(a.status, UMIM_ERR_INVALID_ARG);
         }
         page = page_at(j + 1);
-        ok = wwait(&empty[s], (uint32_t)(pos / stages & 1) ^ 1u);
+        ok = wwait(&empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
         if (!ok) break;
-        if constexpr (BITS == 16) {
-          if (lane == 0) mbar_arrive_expect_tx(&full[s], L::kTile);
-          __syncwarp();
-          if (lane < 8 * DA)
-            tma_load_5d(to + s * L::kTile + (lane >> 3) * (kTcKeys * 128) + pg * (kPageSize * 128), &kv_map, &full[s],
-                        (lane >> 3) * 64, at == n_pages - 1 && part ? part - kPageSize : 0, u.g, kv, c,
-                        policy_evict_last());
-        } else {
-          if (lane == 0) mbar_arrive_expect_tx(&full[s], L::kRaw);
-          __syncwarp();
-          if (lane < 8)
-            tma_load_5d(to + s * L::kRaw + pg * (kPageSize * D), &kv_map, &full[s], 0, 0, u.g, kv, c, policy_evict_last());
-        }
+        if (lane == 0) mbar_arrive_expect_tx(&full[s], L::kTile);
+        __syncwarp();
+        if (lane < 8 * DA)
+          tma_load_5d(to + s * L::kTile + (lane >> 3) * (kTcKeys * 128) + pg * (kPageSize * 128), &kv_map, &full[s],
+                      (lane >> 3) * 64, at == n_pages - 1 && part ? part - kPageSize : 0, u.g, kv, c, policy_evict_last());
       }
     }
     if (!ok) {
       give_up();
       // copies still in flight when a consumer gave up: wait for them (bounded; a phase that has
       // completed, or was never armed, costs no more than a millisecond)
-      for (int i = max(0, pos - stages); i <= pos; ++i)
-        mbar_wait_for(&full[i % stages], (uint32_t)(i / stages & 1), 1000000);
+      for (int i = max(0, pos - kTcStages); i <= pos && BITS == 16; ++i)
+        mbar_wait_for(&full[i % kTcStages], (uint32_t)(i / kTcStages & 1), 1000000);
       for (int t = 0; t < 2 && kv == 0; ++t)
         if (nq > 0) mbar_wait_for(&q_full[t], (uint32_t)(nq - 1) & 1u, 1000000);
     }
@@ -281,8 +278,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     // become ready, then S = Q K^T of its next tile once that has landed (P lies over S) ----
     const int t = warp - 1;
     if (elect_one()) {
-      constexpr uint32_t idesc_s = idesc_f32acc(kTcRows, kTcKeys, false);
-      constexpr uint32_t idesc_o = idesc_f32acc(kTcRows, D, false) | kBMnMajor;
+      constexpr bool kHalf = BITS == 8;   // fp16 operands, and one product for P V
+      constexpr uint32_t idesc_s = idesc_f32acc(kTcRows, kTcKeys, kHalf);
+      constexpr uint32_t idesc_o = idesc_f32acc(kTcRows, D, kHalf) | kBMnMajor;
+      uint64_t *const q_there = BITS == 8 ? q_ready : q_full;
       const uint32_t t_s = tmem + t * kTcKeys, t_o = tmem + 256 + t * 128;
       const uint64_t q_desc = sw128_kmajor_desc(smem_u32(smem) + t * L::kTile);
       int turns = 0, ns = 0, nu = 0;   // turns taken, S issued, units with a tile of this slot
@@ -298,28 +297,28 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         const bool due = pend >= 0;
         const uint32_t pt = (uint32_t)(ns - 1) & 1u;
         if (due) {
-          if (aborted() || !mbar_wait(&v_full[pend % VS], (uint32_t)(pend / VS & 1)) || !mbar_wait(&p_full[t][0], pt) ||
+          if (aborted() || !mbar_wait(&v_full[pend % KS], (uint32_t)(pend / KS & 1)) || !mbar_wait(&p_full[t][0], pt) ||
               (pend_first && nu > 1 && !mbar_wait(&o_free[t], (uint32_t)nu & 1u)))
             return false;
         }
         if ((t == 1 || turns > 0) && (aborted() || !mbar_wait(&turn[t], (uint32_t)(turns + t + 1) & 1u))) return false;
         ++turns;
         if (due) {
-          const uint64_t v_desc = sw128_mnmajor_desc(smem_u32(smem + L::kV + pend % VS * L::kTile));
+          const uint64_t v_desc = sw128_mnmajor_desc(smem_u32(smem + L::kV + pend % KS * L::kTile));
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (h == 1 && !mbar_wait(&p_full[t][1], pt)) return false;
             tc_fence_after();
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+            for (int part = 0; part < (BITS == 8 ? 1 : 2); ++part)
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk)   // 16 keys: a page
-                tc_mma_ts(t_o, t_s + (h * 4 + kk) * 16 + part * 8,
+                tc_mma_ts(t_o, t_s + (h * 4 + kk) * (BITS == 8 ? 8 : 16) + part * 8,
                           v_desc + (h * 4 + kk) * (kPageSize * 128 / 16), idesc_o,
                           !pend_first || h || part || kk ? 1u : 0u);
           }
           tc_commit(&pv_done[t]);
-          commits(&v_empty[pend % VS], pend_two);
+          commits(&v_empty[pend % KS], pend_two);
           pend = -1;
           landing = true;
         }
@@ -328,7 +327,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           return true;
         }
         if (aborted() || !mbar_wait(&k_full[rp % KS], (uint32_t)(rp / KS & 1)) ||
-            (first && !mbar_wait(&q_full[t], (uint32_t)nq & 1u)) || (landing && !mbar_wait(&pv_done[t], pt)))
+            (first && !mbar_wait(&q_there[t], (uint32_t)nq & 1u)) || (landing && !mbar_wait(&pv_done[t], pt)))
           return false;
         landing = false;
         const uint64_t k_desc = sw128_kmajor_desc(smem_u32(smem + L::kK + rp % KS * L::kTile));
@@ -358,7 +357,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         ok = take_turn(mine ? pos + at : -1, i == 0, at + step >= n, u.two, nq);
         if (!more) break;   // (that was the last P V)
         if (ok && i == 0 && !mine) {   // no tile of this slot's: its Q is in nobody's way
-          ok = mbar_wait(&q_full[t], (uint32_t)nq & 1u);
+          ok = mbar_wait(&q_there[t], (uint32_t)nq & 1u);
           if (ok) mbar_arrive(&q_empty[t]);
         }
         if (++i * step >= n) {
@@ -382,9 +381,8 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     const int r = quad * 32 + lane;            // row within the tile
     const uint32_t t_s = tmem + ((uint32_t)(quad * 32) << 16) + t * kTcKeys + half * kKeys;
     const uint32_t t_o = tmem + ((uint32_t)(quad * 32) << 16) + 256 + t * 128;
-    const float sl2 = a.scale_log2;
     bool ok = true;
-    int ns = 0, meets = 0;
+    int ns = 0, meets = 0, nq = 0, pos = 0;   // tiles of the slot, exchanges, units, ring position of the unit's first tile
     // what the other warp of these rows left: a value a row
     auto exchange = [&](float mine, float &other, float alone) {
       other = alone;
@@ -405,6 +403,38 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       const bool any = __any_sync(0xffffffffu, live);   // (warps without rows only keep the others going)
       float m_run = -INFINITY, l_run = 0.f;             // running max (log2 units, moved in steps > 8) and row sum
       int mine = 0;                                     // tiles
+      float sl2 = a.scale_log2;
+      if constexpr (BITS == 8) {
+        // the row of Q to fp16, its largest magnitude in [2^14, 2^15); rows of zeros (or below 2^-86)
+        // and ones that hold no number by a fixed power
+        ok = wwait(&q_full[t], (uint32_t)nq & 1u);
+        if (!ok) break;
+        uint8_t *row = smem + t * L::kTile + r * 128;
+        uint32_t m = 0;
+#pragma unroll 1
+        for (int c = 0; c < D / 8; ++c) {
+          const uint4 v = *reinterpret_cast<const uint4 *>(row + (c >> 3) * (kTcRows * 128) + (((c & 7) ^ (r & 7)) << 4));
+          m = __vmaxu2(m, __vmaxu2(__vmaxu2(v.x & 0x7fff7fff, v.y & 0x7fff7fff), __vmaxu2(v.z & 0x7fff7fff, v.w & 0x7fff7fff)));
+        }
+        m = max(m & 0xffff, m >> 16) >> 7;
+        const uint32_t e = m == 255 ? 127u : max(m, 41u);
+        const float inv = __uint_as_float((268u - e) << 23);   // 2^(14 - (e - 127))
+        sl2 *= __uint_as_float((e - 14) << 23);
+#pragma unroll 1
+        for (int c = 0; c < D / 8; ++c) {
+          uint4 *at = reinterpret_cast<uint4 *>(row + (c >> 3) * (kTcRows * 128) + (((c & 7) ^ (r & 7)) << 4));
+          auto half2_of = [&](uint32_t v) {
+            const __half2 h = __floats2half2_rn(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv);
+            return *reinterpret_cast<const uint32_t *>(&h);
+          };
+          const uint4 v = *at;
+          *at = make_uint4(half2_of(v.x), half2_of(v.y), half2_of(v.z), half2_of(v.w));
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&q_ready[t]);
+        ++nq;
+      }
       for (int j = u.t0 + (u.two ? 0 : t); j < u.t1; j += u.two ? 1 : 2, ++mine, ++ns) {
         ok = wwait(&s_full[t], (uint32_t)ns & 1u);
         if (!ok) break;
@@ -434,16 +464,36 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           for (int c = 4; c < 32; c += 2) m4[(c >> 1) & 3] = max3f(m4[(c >> 1) & 3], s[c], s[c + 1]);
           return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         };
+        // 8-bit: of each page, the powers of two of K's and V's rows
+        const float4 *scale = s_scales[(pos + j - u.t0) & 3];
+        if constexpr (BITS == 8) {
+          ok = wwait(&scales_full[(pos + j - u.t0) & 3], (uint32_t)((pos + j - u.t0) >> 2) & 1u);
+          if (!ok) break;
+        }
+        auto factor = [&](int page) { return fmaxf(sl2 * scale[page].x, 1e-37f); };   // (never 0: -inf stays -inf)
         float s[32], mx = -INFINITY, other;
-#pragma unroll (H == 2 ? 2 : 1)
+#pragma unroll 1
         for (int c = kKeys / 32 - 1; c >= 0; --c) {   // (the first 32 last: they are still there below)
           tmem_ld_32x32b_x32(t_s + c * 32, s);
           mask(s, c * 32);
-          mx = fmaxf(mx, largest(s));
+          if constexpr (BITS == 8) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              float m2[2] = {s[16 * g], s[16 * g + 1]};
+#pragma unroll
+              for (int x = 2; x < 16; x += 4) {
+                m2[0] = max3f(m2[0], s[16 * g + x], s[16 * g + x + 1]);
+                if (x + 2 < 16) m2[1] = max3f(m2[1], s[16 * g + x + 2], s[16 * g + x + 3]);
+              }
+              mx = fmaxf(mx, fmaf(fmaxf(m2[0], m2[1]), factor(2 * c + g), scale[2 * c + g].y));
+            }
+          } else {
+            mx = fmaxf(mx, largest(s));
+          }
         }
         ok = exchange(mx, other, mx);
         if (!ok) break;
-        mx = fmaxf(mx, other) * sl2;
+        mx = BITS == 8 ? mx : fmaxf(mx, other) * sl2;
         // move the running max only when it grows by more than 2^8
         const bool grow = mx > m_run + 8.f;
         float alpha = 1.f;
@@ -465,32 +515,56 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           tmem_wait_st();
         }
         const float nm = (m_run == -INFINITY) ? 0.f : -m_run;
-        const float2 sl2x2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm), minus = make_float2(-1.f, -1.f);
-        float2 la = make_float2(0.f, 0.f), lb = la;
+        const float2 minus = make_float2(-1.f, -1.f);
+        float2 sl2x2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm), la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll (H == 2 ? 2 : 1)   // (four chunks unrolled: their code is fetched over and over, and registers spill)
         for (int h = 0; h < kKeys / 32; ++h) {
           if (h > 0) {
             tmem_ld_32x32b_x32(t_s + h * 32, s);
             mask(s, h * 32);
           }
+          if constexpr (BITS == 8) {
+            float p[16];   // the weights of 32 keys in fp16 pairs
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {   // 16 keys: P (<= 2^8) in bf16 pairs, and what that leaves
-            float p[16];
+            for (int g = 0; g < 2; ++g) {   // a page
+              const float4 z = scale[2 * h + g];
+              const float k = factor(2 * h + g), off = z.y + nm + 7.f;
+              sl2x2 = make_float2(k, k), nm2 = make_float2(off, off);
+              la = lb = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int c = 0; c < 16; c += 2) {
-              const float2 x = __ffma2_rn(make_float2(s[g * 16 + c], s[g * 16 + c + 1]), sl2x2, nm2);
-              const float2 y = make_float2(ex2_approx(x.x), ex2_approx(x.y));   // masked (-inf): 0
-              if (c & 2) lb = __fadd2_rn(lb, y);
-              else la = __fadd2_rn(la, y);
-              const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
-              const uint32_t hi = *reinterpret_cast<const uint32_t *>(&b);
-              const float2 d = __ffma2_rn(make_float2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), minus, y);
-              const __nv_bfloat162 rest = __floats2bfloat162_rn(d.x, d.y);
-              p[c / 2] = __uint_as_float(hi);
-              p[8 + c / 2] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&rest));
+              for (int c = 0; c < 16; c += 2) {
+                const float2 x = __ffma2_rn(make_float2(s[g * 16 + c], s[g * 16 + c + 1]), sl2x2, nm2);
+                const float2 y = make_float2(ex2_approx(x.x), ex2_approx(x.y));   // masked (-inf): 0
+                if (c & 2) lb = __fadd2_rn(lb, y);
+                else la = __fadd2_rn(la, y);
+                const __half2 b = __floats2half2_rn(y.x, y.y);
+                p[g * 8 + c / 2] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&b));
+              }
+              const float2 lab = __fadd2_rn(la, lb);
+              l_run = fmaf(lab.x + lab.y, z.z, l_run);
             }
-            // over the S columns they come from, which this thread has read
-            tmem_put_32x32b_x16(t_s + h * 32 + g * 16, p);
+            // over S columns that have been read: 16 for each 32
+            tmem_put_32x32b_x16(t_s + h * 16, p);
+          } else {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {   // 16 keys: P (<= 2^8) in bf16 pairs, and what that leaves
+              float p[16];
+  #pragma unroll
+              for (int c = 0; c < 16; c += 2) {
+                const float2 x = __ffma2_rn(make_float2(s[g * 16 + c], s[g * 16 + c + 1]), sl2x2, nm2);
+                const float2 y = make_float2(ex2_approx(x.x), ex2_approx(x.y));   // masked (-inf): 0
+                if (c & 2) lb = __fadd2_rn(lb, y);
+                else la = __fadd2_rn(la, y);
+                const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
+                const uint32_t hi = *reinterpret_cast<const uint32_t *>(&b);
+                const float2 d = __ffma2_rn(make_float2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), minus, y);
+                const __nv_bfloat162 rest = __floats2bfloat162_rn(d.x, d.y);
+                p[c / 2] = __uint_as_float(hi);
+                p[8 + c / 2] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&rest));
+              }
+              // over the S columns they come from, which this thread has read
+              tmem_put_32x32b_x16(t_s + h * 32 + g * 16, p);
+            }
           }
           if (h & 1) {   // 64 keys
             tmem_wait_st();
@@ -499,9 +573,12 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             if (elect_one()) mbar_arrive(&p_full[t][H == 2 ? half : h / 2]);
           }
         }
-        const float2 lab = __fadd2_rn(la, lb);
-        l_run += lab.x + lab.y;
+        if constexpr (BITS == 16) {
+          const float2 lab = __fadd2_rn(la, lb);
+          l_run += lab.x + lab.y;
+        }
       }
+      pos += u.t1 - u.t0;
       if (!ok) break;
       // the unit's partial result, half the columns a warp
       const int64_t piece = 2 * ((int64_t)u.seg + blockIdx.x) + t;
@@ -521,6 +598,9 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           for (int c = 0; c < kCols / 32; ++c) {
             float o[32];
             tmem_ld_32x32b_x32(t_o + half * kCols + c * 32, o);
+            if constexpr (BITS == 8)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] *= 0x1p-7f;
             if (store)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
@@ -537,75 +617,98 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     }
     if (!ok) give_up();
   } else if (warp >= kConvert<BITS>) {
-    // ---- 8-bit values to bf16 operands: half the warps for K and half for V (each has its own to wait
-    // for), a warp two pages of a tile, D / 8 lanes a key ----
+    // ---- 8-bit values to fp16 operands: a warp a page of the tile, D / 8 lanes a key.  A tile's
+    // values come straight from the pages into registers, a tile ahead: through shared
+    // memory they left room for one stage of K, whose products then waited for its
+    // conversion, and that for the products before ----
     if constexpr (BITS == 8) {
-      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kSteps = kPageSize / kAtOnce, kGroup = kConverters / 2;
-      static_assert(kGroup * 2 * kPageSize == kTcKeys, "a warp two pages");
-      const int kv = (warp - kConvert<BITS>) / kGroup, w = (warp - kConvert<BITS>) % kGroup, part = lane % kLanes;
-      const int raws = kv ? kRawV : kRawK, stages = kv ? VS : KS;
-      uint64_t *const raw_f = raw_full + kv * kRawK, *const raw_e = raw_empty + kv * kRawK;
-      uint64_t *const full = kv ? v_full : k_full, *const empty = kv ? v_empty : k_empty;
-      const uint8_t *const raw0 = smem + L::kRawAt + kv * kRawK * L::kRaw + 2 * w * (kPageSize * D) + lane / kLanes * D + part * 8;
-      uint8_t *const dst0 = smem + (kv ? L::kV : L::kK) + (part >> 3) * (kTcKeys * 128);
+      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kSteps = kPageSize / kAtOnce;
+      static_assert(kConverters * kPageSize == kTcKeys, "a warp a page");
+      const int w = warp - kConvert<BITS>, part = lane % kLanes;
+      const int own = lane / kLanes * D + part * 8;   // this lane's place in a step's keys
       bool ok = true;
       int pos = 0;
       TcUnit u;
       for (int x = start; ok && unit_at(a, plan, x, end, u);) {
         const int n_pages = ceil_div(u.len, kPageSize);
         const int32_t *table = a.prefix_table + (int64_t)u.i * a.max_prefix_pages;
-        // this lane's key's page of a tile (16 lanes a page), read two tiles ahead, and the key's
-        // scale, read one tile ahead (a page that is not there has been copied as zeros)
+        // this warp's page of a tile, read two tiles ahead; -1 for none, which reads as zeros
         auto page_of = [&](int j) {
-          const int at = j * 8 + 2 * w + (lane >> 4);
-          return j < u.t1 && at < n_pages ? ld_early(table + at) : -1;
+          const int at = j * 8 + w;
+          if (j >= u.t1 || at >= n_pages || !in_bounds(at, a.max_prefix_pages, a.status, kSitePrefixTable)) return -1;
+          return ld_early(table + at);
         };
-        auto code_of = [&](int page) {
-          if (page < 0 || page >= a.n_pages) return 127u;
-          return ld_early_u8(scales + ((((int64_t)a.layer * a.n_pages + page) * 2 + kv) * a.Hkv + u.g) * kPageSize + (lane & 15));
+        auto checked = [&](int page, int j) {
+          if (page >= 0 && page < a.n_pages) return page;
+          if (j < u.t1 && j * 8 + w < n_pages) set_error(a.status, UMIM_ERR_INVALID_ARG);
+          return -1;
         };
-        int page = page_of(u.t0 + 1);
-        uint32_t code = code_of(page_of(u.t0));
+        auto row_at = [&](int page, int kv) {   // the page's first row of K or V
+          return ((((int64_t)a.layer * a.n_pages + page) * 2 + kv) * a.Hkv + u.g) * kPageSize;
+        };
+        auto load = [&](uint2 (&v)[kSteps], int page, int kv) {
+          const uint8_t *p = values + row_at(page, kv) * D + own;
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i) v[i] = page >= 0 ? ld_early_v2(p + i * kAtOnce * D) : make_uint2(0, 0);
+        };
+        auto code_of = [&](int page) {   // a key's: lanes 0-15 K's, 16-31 V's
+          return page >= 0 ? ld_early_u8(scales + row_at(page, lane >> 4) + (lane & 15)) : 127u;
+        };
+        uint2 k[kSteps], v[kSteps];
+        int page = checked(page_of(u.t0), u.t0);
+        uint32_t code = code_of(page);
+        load(k, page, 0);
+        load(v, page, 1);
+        page = page_of(u.t0 + 1);
         for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
-          const int rem = u.len - (j * 8 + 2 * w) * kPageSize;   // keys from the warp's first on
-          const float scale = e8m0_value(code);
-          const __nv_bfloat162 scale2 = __floats2bfloat162_rn(scale, scale);   // exact
-          const uint32_t factor = *reinterpret_cast<const uint32_t *>(&scale2);
-          code = code_of(page);
+          const int rem = u.len - (j * 8 + w) * kPageSize;   // keys from the page's first on
+          const int s = pos % kTcStages, next = checked(page, j + 1);
           page = page_of(j + 2);
-          const int s = pos % raws, to = pos % stages;
-          ok = wwait(&raw_f[s], (uint32_t)(pos / raws & 1)) && wwait(&empty[to], (uint32_t)(pos / stages & 1) ^ 1u);
-          if (!ok) break;
-          const uint8_t *raw = raw0 + s * L::kRaw;
-          uint8_t *dst = dst0 + to * L::kTile;
-#pragma unroll 1   // (not larger than it has to be: the code of all roles competes for the instruction cache)
-          for (int i0 = 0; i0 < 2 * kSteps; i0 += 4) {
-            uint2 v[4];   // (loads first: a warp nearly alone on its scheduler waits for each otherwise)
+          // the largest code of the page's rows, those that are NaN or behind the end apart
+          uint32_t most = (lane & 15) < rem && code != 255 ? code : 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint2 *>(raw + (i0 + i) * kAtOnce * D);
+          for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+          const uint32_t most_v = __shfl_sync(0xffffffffu, most, 16);
+          const int down = (int)code - (int)most;   // 0 or less
+          const float scale = code == 255 ? NAN : down < -126 ? 0.f : __uint_as_float((uint32_t)(127 + down) << 23);
+          const __half2 scale2 = __floats2half2_rn(scale, scale);
+          const uint32_t factor = *reinterpret_cast<const uint32_t *>(&scale2);
+          code = code_of(next);
+          auto convert = [&](const uint2 (&in)[kSteps], uint8_t *dst, int first) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int key = (i0 + i) * kAtOnce + lane / kLanes, row = 2 * w * kPageSize + key;
-              const uint32_t f = __shfl_sync(0xffffffffu, factor, key);
+            for (int i = 0; i < kSteps; ++i) {
+              const int key = i * kAtOnce + lane / kLanes;
+              const uint32_t f = __shfl_sync(0xffffffffu, factor, first + key);
               uint32_t out[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const uint32_t h = f16x2_of_e4m3x2((e < 2 ? v[i].x : v[i].y) >> (e & 1) * 16);
-                const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-                const __nv_bfloat162 b = __hmul2(__floats2bfloat162_rn(y.x, y.y), *reinterpret_cast<const __nv_bfloat162 *>(&f));
+                const uint32_t h = f16x2_of_e4m3x2((e < 2 ? in[i].x : in[i].y) >> (e & 1) * 16);
+                const __half2 b = __hmul2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&f));
                 out[e] = *reinterpret_cast<const uint32_t *>(&b);
               }
               if (key >= rem) out[0] = out[1] = out[2] = out[3] = 0u;
-              *reinterpret_cast<uint4 *>(dst + row * 128 + (((part & 7) ^ (row & 7)) << 4)) =
-                  make_uint4(out[0], out[1], out[2], out[3]);
+              *reinterpret_cast<uint4 *>(dst + (part >> 3) * (kTcKeys * 128) + (w * kPageSize + key) * 128 +
+                                         (((part & 7) ^ (key & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
             }
+          };
+          ok = wwait(&k_empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
+          if (!ok) break;
+          if (lane == 0) {   // (four tiles' scales: S of the tile two before is done, so the softmax of the one four before is)
+            s_scales[pos & 3][w] = make_float4(e8m0_value(most), (float)((int)most_v - 127), ldexpf(1.f, 120 - (int)most_v), 0.f);
+            mbar_arrive(&scales_full[pos & 3]);
           }
+          convert(k, smem + L::kK + s * L::kTile, 0);
           fence_proxy_async_smem();
           __syncwarp();
-          if (elect_one()) {
-            mbar_arrive(&full[to]);
-            mbar_arrive(&raw_e[s]);
-          }
+          if (elect_one()) mbar_arrive(&k_full[s]);
+          load(k, next, 0);
+          ok = wwait(&v_empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
+          if (!ok) break;
+          convert(v, smem + L::kV + s * L::kTile, 16);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (elect_one()) mbar_arrive(&v_full[s]);
+          load(v, next, 1);
         }
       }
       if (!ok) give_up();
@@ -622,13 +725,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
 
 template <int D, int BITS>
 bool launch(const CacheView &kv, const PagesArgs &a, const PagesWs &ws, cudaStream_t stream, int num_sms) {
-  using L = TcSmem<D, BITS>;
+  using L = TcSmem<D>;
   static_assert(L::kMost + 6144 <= 232448, "shared memory of a CTA");
   EncodeTiledFn enc = get_encode_tiled();
   if (!enc) return false;
   CUtensorMap q_map, kv_map;
   const cuuint32_t one[5] = {1, 1, 1, 1, 1};
-  const cuuint64_t H = kv.n_kv_heads, N = (cuuint64_t)kv.n_layers * (cuuint64_t)kv.n_pages, row = D * BITS / 8, G = a.G;
+  const cuuint64_t H = kv.n_kv_heads, N = (cuuint64_t)kv.n_layers * (cuuint64_t)kv.n_pages, G = a.G;
   const cuuint64_t q_dims[4] = {(cuuint64_t)D, G, H, (cuuint64_t)a.B};
   const cuuint64_t q_strides[3] = {D * 2, G * D * 2, H * G * D * 2};
   const cuuint32_t q_box[4] = {64, (cuuint32_t)G, 1, (cuuint32_t)tile_sequences(a.G)};
@@ -636,19 +739,21 @@ bool launch(const CacheView &kv, const PagesArgs &a, const PagesWs &ws, cudaStre
           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return false;
-  const cuuint64_t dims[5] = {(cuuint64_t)D, 16, H, 2, N};
-  const cuuint64_t strides[4] = {row, 16 * row, H * 16 * row, 2 * H * 16 * row};
-  const cuuint32_t box[5] = {BITS == 8 ? (cuuint32_t)D : 64, 16, 1, 1, 1};
-  if (enc(&kv_map, BITS == 8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, kv.values, dims,
-          strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-          BITS == 8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return false;
+  kv_map = q_map;
+  if (BITS == 16) {
+    const cuuint64_t row = D * 2, dims[5] = {(cuuint64_t)D, 16, H, 2, N};
+    const cuuint64_t strides[4] = {row, 16 * row, H * 16 * row, 2 * H * 16 * row};
+    const cuuint32_t box[5] = {64, 16, 1, 1, 1};
+    if (enc(&kv_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, kv.values, dims, strides, box, one,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return false;
+  }
   auto kern = prefix_tc_kernel<D, BITS>;
   if (!allow_smem(kern, L::kMost)) return false;
   const size_t smem = L::kPlan + 1024 + 12 * ((size_t)a.n_prefixes + 1);
   return launch_pdl(kern, dim3((unsigned)std::max(1, num_sms)), dim3(kTcThreads<BITS>), smem, stream, q_map, kv_map,
-                    static_cast<const uint8_t *>(kv.scales), a, ws) == cudaSuccess;
+                    static_cast<const uint8_t *>(kv.values), static_cast<const uint8_t *>(kv.scales), a, ws) == cudaSuccess;
 }
 
 }  // namespace

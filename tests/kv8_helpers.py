@@ -48,7 +48,7 @@ def i32(x, d):
     return torch.from_numpy(np.ascontiguousarray(np.asarray(x, dtype=np.int32))).to(d)
 
 
-def attention_bound(want, size, most, finest):
+def attention_bound(want, size, most, finest, half):
     """How far an output may be from its value in 64 bits.
 
     The output is rounded once, 2^-8 of itself.  A score is an fp32 sum of at most 128 products in the tensor core,
@@ -62,18 +62,23 @@ def attention_bound(want, size, most, finest):
     Over the 8-bit cache a weight times its row's scale is an fp16 number and an fp16 remainder in units of 2^-15 of
     the largest of them (or of a piece's largest, which is smaller): the remainder is a multiple of 2^-24 of such a
     unit, so however small the weight, 2^-25 * 2^-15 = 2^-40 of the largest one may be missing, of every row's
-    |V| / scale.  That is 2^-40 * finest; it shows where the rows of the large weights hold zeros in a column."""
-    eps = 4 * (2.0 ** -16 + 2.0 ** -17 * most[..., None])
-    return 2.0 ** -8 * np.abs(want) + eps * size + 2.0 ** -40 * finest + 1e-30
+    |V| / scale.  That is 2^-40 * finest; it shows where the rows of the large weights hold zeros in a column.
+
+    half: over a prefix of many rows in the 8-bit cache a weight is one fp16 number, off by 2^-12 of itself (the row
+    sum is made of the weights before that), in units of 2^-7 of the running maximum, which some weight reached: 2^-25
+    * 2^-7 = 2^-32 of the largest may be missing of every row's |V| / scale.  (Rows are exact there while
+    their scales lie within 2^15 of their page's largest, as all of these do.)"""
+    eps = 4 * (2.0 ** -16 + 2.0 ** -17 * most[..., None]) + (2.0 ** -12 if half else 0)
+    return 2.0 ** -8 * np.abs(want) + eps * size + 2.0 ** (-32 if half else -40) * finest + 1e-30
 
 
-def check_attention(got, want, size, most, finest):
+def check_attention(got, want, size, most, finest, half=False):
     got = got.double().cpu().numpy()
     assert got.shape == want.shape
     np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
     ok = ~np.isnan(want)
     err = np.abs(got - want)
-    bound = attention_bound(want, size, most, finest)
+    bound = attention_bound(want, size, most, finest, half)
     bad = ok & (err > bound)
     assert not bad.any(), (np.argwhere(bad)[:5], err[bad][:5], bound[bad][:5])
 

@@ -180,11 +180,11 @@ def test_shared(prefix_lens, groups, lens, hq, hkv, d, bits):
     c = SharedCase(len(lens) + hq, prefix_lens, groups, lens, hq, hkv, d, layers=2)
     status = m.new_status(dv)
     for layer in (0, 1):
-        check_attention(shared(m, bits)(layer=layer, dev_status=status, **c.args(m, bits, dv)), *c.want(bits, layer))
+        check_attention(shared(m, bits)(layer=layer, dev_status=status, **c.args(m, bits, dv)), *c.want(bits, layer), half=bits == 8)
     if len(groups) == 1:
         a = c.args(m, bits, dv)
         del a["prefix_offsets"]
-        check_attention(shared(m, bits)(layer=1, dev_status=status, scale=0.3, **a), *c.want(bits, 1, 0.3))
+        check_attention(shared(m, bits)(layer=1, dev_status=status, scale=0.3, **a), *c.want(bits, 1, 0.3), half=bits == 8)
     assert int(status.item()) == 0
 
 
@@ -192,7 +192,7 @@ def test_shared(prefix_lens, groups, lens, hq, hkv, d, bits):
 def test_sequences_of_no_prefix(bits):
     m, dv = umim(), dev()
     c = SharedCase(40, [50, 20], None, [5, 0, 30, 7, 0, 12], 8, 2, 64, offsets=[1, 3, 4])
-    check_attention(shared(m, bits)(layer=0, **c.args(m, bits, dv)), *c.want(bits))
+    check_attention(shared(m, bits)(layer=0, **c.args(m, bits, dv)), *c.want(bits), half=bits == 8)
 
 
 @pytest.mark.parametrize("bits", [16, 8])
@@ -206,7 +206,7 @@ def test_garbage_past_the_ends(bits, many):
             c.bits[:, table[t // 16], :, :, t % 16] = 0x7fc0 if t % 2 else 0xff80
             c.codes[:, table[t // 16], :, :, t % 16] = 0x7f
             c.scales[:, table[t // 16], :, :, t % 16] = 255
-    check_attention(shared(m, bits)(layer=0, **c.args(m, bits, dv)), *c.want(bits))
+    check_attention(shared(m, bits)(layer=0, **c.args(m, bits, dv)), *c.want(bits), half=bits == 8)
 
 
 @pytest.mark.parametrize("bits", [16, 8])
@@ -229,23 +229,23 @@ def test_bad_arguments_on_the_device(bits, many):
     for bad in (-1, 16 * cols + 1):
         got = run(prefix_lens=[bad, 40])
         c.prefix_lens[0] = 0
-        check_attention(got, *c.want(bits))
+        check_attention(got, *c.want(bits), half=bits == 8)
         c.prefix_lens[0] = 50
     got = run(prefix_offsets=[0, B - 2, B + 1])          # the second prefix has nobody
     keep = c.offsets
     c.offsets = np.array([0, B - 2, B - 2])
-    check_attention(got, *c.want(bits))
+    check_attention(got, *c.want(bits), half=bits == 8)
     c.offsets = keep
     got = run(prefix_offsets=[B - 2, 3, B])              # (B - 2, B - 2, B)
     c.offsets = np.array([B - 2, B - 2, B])
-    check_attention(got, *c.want(bits))
+    check_attention(got, *c.want(bits), half=bits == 8)
     c.offsets = keep
     bt = c.prefix_bt.copy()
     bt[0, 1] = c.pages
     got = run(prefix_table=bt)
     z = c.prefix_bt[0, 1]
     c.bits[:, z], c.codes[:, z] = 0, 0
-    check_attention(got, *c.want(bits))
+    check_attention(got, *c.want(bits), half=bits == 8)
     assert not np.array_equal(full[0], c.want(bits)[0])
 
 
@@ -258,7 +258,7 @@ def test_nan_in_a_prefix(bits, many):
     c.bits[0, c.prefix_bt[0, 1], 0, 1, 2, 5], c.codes[0, c.prefix_bt[0, 1], 0, 1, 2, 5] = 0x7fc0, 0x7f
     got = shared(m, bits)(layer=0, **c.args(m, bits, dv)).float().cpu().numpy()
     assert np.isnan(got[:B - 2, 4:]).all() and np.isfinite(got[:, :4]).all() and np.isfinite(got[B - 2:]).all()
-    check_attention(torch.from_numpy(got[:, :4].copy()), *(x[:, :4] for x in c.want(bits)))
+    check_attention(torch.from_numpy(got[:, :4].copy()), *(x[:, :4] for x in c.want(bits)), half=bits == 8)
 
 
 @pytest.mark.parametrize("bits", [16, 8])
@@ -269,7 +269,7 @@ def test_many_prefixes(bits):
     groups = r.integers(0, 4, n)
     B = int(groups.sum())
     c = SharedCase(44, r.integers(0, 60, n).tolist(), groups, r.integers(0, 20, B).tolist(), 4, 2, 64)
-    check_attention(shared(m, bits)(layer=0, **c.args(m, bits, dv)), *c.want(bits))
+    check_attention(shared(m, bits)(layer=0, **c.args(m, bits, dv)), *c.want(bits), half=bits == 8)
 
 
 @pytest.mark.parametrize("bits", [16, 8])
@@ -294,7 +294,7 @@ def test_graphs_share_a_workspace(bits, B):
             graphs[i].replay()
             shared(m, bits)(layer=0, workspace_buf=ws, **args[1 - i])
             assert torch.equal(outs[i], eager[i])
-    check_attention(outs[0], *cases[0].want(bits))
+    check_attention(outs[0], *cases[0].want(bits), half=bits == 8)
 
 
 def test_calls_at_once_on_two_streams():
