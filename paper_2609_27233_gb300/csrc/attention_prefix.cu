@@ -46,6 +46,10 @@ namespace {
 
 constexpr uint32_t kTcTmemCols = 512;   // S of the slots at 0 and 128, O at 256 and 384
 constexpr int kTcStages = 2;            // K and V rings
+#ifndef KAHEAD
+#define KAHEAD 3
+#endif
+constexpr int kAhead = KAHEAD;               // 8-bit: key tiles on their way into L2 ahead of their loads
 
 // shared memory (bytes, every piece but the plan 1024-aligned)
 template <int D>
@@ -156,7 +160,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&k_full[s], BITS == 8 ? kConverters : 1);
+      mbar_init(&k_full[s], BITS == 8 ? kConverters + 1 : 1);
       mbar_init(&k_empty[s], 2);   // read by both slots' products, or twice by one's
       mbar_init(&v_full[s], BITS == 8 ? kConverters : 1);
       mbar_init(&v_empty[s], 2);
@@ -239,9 +243,32 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         }
       }
       ++nq;
-      if (BITS == 8) continue;
       const int n_pages = ceil_div(u.len, kPageSize), part = u.len % kPageSize, pg = lane & 7;
       const int32_t *table = a.prefix_table + (int64_t)u.i * a.max_prefix_pages;
+      if constexpr (BITS == 8) {
+        // the pages that the converters will load, on their way into L2: from HBM a tile
+        // takes longer than the products of the one before.  A lane an operand's page.
+        if (kv == 0) continue;
+        auto prefetch = [&](int j) {
+          const int at = j * 8 + pg;
+          if (lane >= 16 || j >= u.t1 || at >= n_pages) return;
+          const int page = table[at];
+          if (page < 0 || page >= a.n_pages) return;
+          const int64_t row = ((((int64_t)a.layer * a.n_pages + page) * 2 + (lane >> 3)) * a.Hkv + u.g) * kPageSize;
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(values + row * D), "r"(kPageSize * D) : "memory");
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(scales + row));
+        };
+        for (int i = 0; i < kAhead; ++i) prefetch(u.t0 + i);
+        for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
+          ok = wwait(&k_empty[pos % kTcStages], (uint32_t)(pos / kTcStages & 1) ^ 1u);
+          if (!ok) break;
+          prefetch(j + kAhead);
+          __syncwarp();
+          // (part of the tile's arrivals, though it has written nothing: no phase passes this warp unseen)
+          if (elect_one()) mbar_arrive(&k_full[pos % kTcStages]);
+        }
+        continue;
+      }
       auto page_at = [&](int j) {   // read a tile ahead
         const int at = j * 8 + pg;
         return j < u.t1 && at < n_pages && in_bounds(at, a.max_prefix_pages, a.status, kSitePrefixTable) ? ld_early(table + at) : 0;
@@ -654,27 +681,34 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         auto code_of = [&](int page) {   // a key's: lanes 0-15 K's, 16-31 V's
           return page >= 0 ? ld_early_u8(scales + row_at(page, lane >> 4) + (lane & 15)) : 127u;
         };
+        // of a tile's scales: the largest codes of the page's rows (those that are NaN or behind the end
+        // apart), and this lane's key's factor in the page's units, packed twice
+        uint32_t most, most_v, factor;
+        auto scales_of = [&](uint32_t code, int rem) {
+          most = (lane & 15) < rem && code != 255 ? code : 0;
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+          const int down = (int)code - (int)most;   // 0 or less
+          const float scale = code == 255 ? NAN : down < -126 ? 0.f : __uint_as_float((uint32_t)(127 + down) << 23);
+          const __half2 scale2 = __floats2half2_rn(scale, scale);
+          factor = *reinterpret_cast<const uint32_t *>(&scale2);
+          most_v = __shfl_sync(0xffffffffu, most, 16);
+        };
+        // The order below: a wait for one load is a wait for all loads before it, so what the short ones
+        // bring is used before the next long ones are issued.
         uint2 k[kSteps], v[kSteps];
         int page = checked(page_of(u.t0), u.t0);
         uint32_t code = code_of(page);
         load(k, page, 0);
         load(v, page, 1);
-        page = page_of(u.t0 + 1);
+        scales_of(code, u.len - (u.t0 * 8 + w) * kPageSize);
+        int next = checked(page_of(u.t0 + 1), u.t0 + 1);
         for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
           const int rem = u.len - (j * 8 + w) * kPageSize;   // keys from the page's first on
-          const int s = pos % kTcStages, next = checked(page, j + 1);
-          page = page_of(j + 2);
-          // the largest code of the page's rows, those that are NaN or behind the end apart
-          uint32_t most = (lane & 15) < rem && code != 255 ? code : 0;
-#pragma unroll
-          for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-          const uint32_t most_v = __shfl_sync(0xffffffffu, most, 16);
-          const int down = (int)code - (int)most;   // 0 or less
-          const float scale = code == 255 ? NAN : down < -126 ? 0.f : __uint_as_float((uint32_t)(127 + down) << 23);
-          const __half2 scale2 = __floats2half2_rn(scale, scale);
-          const uint32_t factor = *reinterpret_cast<const uint32_t *>(&scale2);
+          const int s = pos % kTcStages;
           code = code_of(next);
-          auto convert = [&](const uint2 (&in)[kSteps], uint8_t *dst, int first) {
+          page = page_of(j + 2);
+          auto convert = [&](const uint2 (&in)[kSteps], uint8_t *dst, uint32_t factor, int first) {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
               const int key = i * kAtOnce + lane / kLanes;
@@ -697,18 +731,22 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             s_scales[pos & 3][w] = make_float4(e8m0_value(most), (float)((int)most_v - 127), ldexpf(1.f, 120 - (int)most_v), 0.f);
             mbar_arrive(&scales_full[pos & 3]);
           }
-          convert(k, smem + L::kK + s * L::kTile, 0);
+          convert(k, smem + L::kK + s * L::kTile, factor, 0);
           fence_proxy_async_smem();
           __syncwarp();
           if (elect_one()) mbar_arrive(&k_full[s]);
+          const uint32_t factor_v = factor;
+          scales_of(code, rem - kTcKeys);   // the next tile's
+          page = checked(page, j + 2);
           load(k, next, 0);
           ok = wwait(&v_empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
           if (!ok) break;
-          convert(v, smem + L::kV + s * L::kTile, 16);
+          convert(v, smem + L::kV + s * L::kTile, factor_v, 16);
           fence_proxy_async_smem();
           __syncwarp();
           if (elect_one()) mbar_arrive(&v_full[s]);
           load(v, next, 1);
+          next = page;
         }
       }
       if (!ok) give_up();
