@@ -678,7 +678,7 @@ umim_status run_pages(const CacheView &kv, PagesArgs a, void *out, void *workspa
   const int total_warps = std::max(1, num_sms) * kAttnWarps;
   PagesWs ws;
   pages_carve(workspace, &ws, a.B, SHARED ? a.n_prefixes : 0, a.G, a.Hkv, D, num_sms);
-  const bool tc = SHARED && a.B * a.G > kTcMinRows;
+  const bool tc = SHARED && tc_pays(a.B, a.n_prefixes, a.G, a.Hkv, D, BITS == 8, a.max_prefix_pages);
   a.most_rows = tc ? kTcMinRows : INT32_MAX;
   a.smem_plan = a.B <= kSmemPlanBatch ? 1 : 0;
   if (!a.smem_plan) {   // (never with prefixes: their batch is limited)

@@ -39,10 +39,21 @@ struct PrefixPlan {
 // prefixes with many rows, on the tensor cores
 // ---------------------------------------------------------------------------
 constexpr int kTcRows = 128, kTcKeys = 128;
-// More rows than this go there: a tile of 128 rows costs the same with fewer rows in it.
-constexpr int kTcMinRows = 32;
+// Where that kernel runs, prefixes of more rows than this are its: a tile of 128 rows and 128 entries costs
+// 16 to 23 ns of the GPU however many of the rows are there, eight pages 8 to 12 ns for every 16 rows here.
+constexpr int kTcMinRows = 16;
 
 __host__ __device__ inline int tile_sequences(int G) { return kTcRows / G; }   // whole sequences a tile of rows
+
+// Whether it runs at all: it takes 4 us of its own, so when a batch of equal groups, their prefixes as long as the
+// table is wide, would save as much (in ns: 1 a page and 16 rows, 1.5 for 8-bit pages, half for D = 64, against twice
+// that a page and 128 rows).  16-bit, 8 heads, D = 128: 16 sequences of 4 query heads a KV head behind 3000 entries take 17.5 us
+// either way, 24 take 19.0 with it and 21.5 without, 64 behind 500 entries 19.7 and 18.4, 64 behind 12000 38 and 110.
+inline bool tc_pays(int B, int n, int G, int Hkv, int D, bool narrow, int max_prefix_pages) {
+  if ((int64_t)B * G <= kTcMinRows) return false;
+  const int64_t rows = ((int64_t)B * G + n - 1) / n, saved = (rows + 15) / 16 - 2 * ((rows + kTcRows - 1) / kTcRows);
+  return (int64_t)Hkv * max_prefix_pages * n * saved * (narrow ? 3 : 2) * D > 2 * 4000 * 128;
+}
 
 // segments at most (of one KV head): pairs of row tiles, and a single one a prefix
 inline int64_t tc_max_segments(int B, int n, int G) {

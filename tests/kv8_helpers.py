@@ -86,13 +86,17 @@ def check_attention(got, want, size, most, finest, half=False):
 class SharedCase:
     """Groups of sequences over prefixes, in a 16- and an 8-bit cache of the same values."""
 
-    def __init__(self, seed, prefix_lens, groups, lens, Hq, Hkv, D, layers=1, offsets=None):
+    def __init__(self, seed, prefix_lens, groups, lens, Hq, Hkv, D, layers=1, offsets=None, wide=False):
         r = W.rng(seed)
         self.prefix_lens, self.lens, self.Hkv = list(prefix_lens), list(lens), Hkv
         B = len(lens)
         self.offsets = np.concatenate([[0], np.cumsum(groups)]) if offsets is None else np.asarray(offsets)
         bt, self.pages = tables(r, list(lens) + list(prefix_lens), spare=3)
         self.bt, self.prefix_bt = bt[:B], bt[B:]
+        if wide:   # a table wide enough that prefixes of many rows go to the tensor cores' kernel, however short
+            full = np.full((len(prefix_lens), 6000), -1, np.int32)
+            full[:, :self.prefix_bt.shape[1]] = self.prefix_bt
+            self.prefix_bt = full
         self.bits = pool_bits(r, layers, self.pages, Hkv, D)
         self.codes, self.scales = oracle.kv8.quantise(self.bits)
         self.q = key_like(r, (B, Hq, D))

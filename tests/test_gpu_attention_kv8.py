@@ -173,11 +173,12 @@ SHARED = [
 ]
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("prefix_lens,groups,lens,hq,hkv,d", SHARED)
-def test_shared(prefix_lens, groups, lens, hq, hkv, d, bits):
+def test_shared(prefix_lens, groups, lens, hq, hkv, d, bits, wide):
     m, dv = umim(), dev()
-    c = SharedCase(len(lens) + hq, prefix_lens, groups, lens, hq, hkv, d, layers=2)
+    c = SharedCase(len(lens) + hq, prefix_lens, groups, lens, hq, hkv, d, layers=2, wide=wide)
     status = m.new_status(dv)
     for layer in (0, 1):
         check_attention(shared(m, bits)(layer=layer, dev_status=status, **c.args(m, bits, dv)), *c.want(bits, layer), half=bits == 8)
@@ -200,7 +201,7 @@ def test_sequences_of_no_prefix(bits):
 def test_garbage_past_the_ends(bits, many):
     m, dv = umim(), dev()
     B = 64 if many else 3
-    c = SharedCase(41, [37], [B], [(7 * b) % 19 for b in range(B)], 16, 2, 128)
+    c = SharedCase(41, [37], [B], [(7 * b) % 19 for b in range(B)], 16, 2, 128, wide=many)
     for table, n in [(c.prefix_bt[0], 37)] + list(zip(c.bt, c.lens)):
         for t in range(n, -(-n // 16) * 16):
             c.bits[:, table[t // 16], :, :, t % 16] = 0x7fc0 if t % 2 else 0xff80
@@ -215,7 +216,7 @@ def test_bad_arguments_on_the_device(bits, many):
     """Lengths, offsets and pages that are not there: reported, and what the header says instead."""
     m, dv = umim(), dev()
     B = 64 if many else 6
-    c = SharedCase(42, [50, 40], [B - 2, 2], [5] * B, 8, 2, 64)
+    c = SharedCase(42, [50, 40], [B - 2, 2], [5] * B, 8, 2, 64, wide=many)
 
     def run(**change):
         a = c.args(m, bits, dv)
@@ -254,7 +255,7 @@ def test_bad_arguments_on_the_device(bits, many):
 def test_nan_in_a_prefix(bits, many):
     m, dv = umim(), dev()
     B = 66 if many else 4
-    c = SharedCase(43, [50, 40], [B - 2, 2], [5] * B, 8, 2, 64)
+    c = SharedCase(43, [50, 40], [B - 2, 2], [5] * B, 8, 2, 64, wide=many)
     c.bits[0, c.prefix_bt[0, 1], 0, 1, 2, 5], c.codes[0, c.prefix_bt[0, 1], 0, 1, 2, 5] = 0x7fc0, 0x7f
     got = shared(m, bits)(layer=0, **c.args(m, bits, dv)).float().cpu().numpy()
     assert np.isnan(got[:B - 2, 4:]).all() and np.isfinite(got[:, :4]).all() and np.isfinite(got[B - 2:]).all()
@@ -262,13 +263,15 @@ def test_nan_in_a_prefix(bits, many):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
-def test_many_prefixes(bits):
+@pytest.mark.parametrize("wide", [False, True])
+def test_many_prefixes(bits, wide):
     m, dv = umim(), dev()
-    n = 200
+    n = 40 if wide else 200
     r = W.rng(44)
-    groups = r.integers(0, 4, n)
+    groups = r.integers(0, 40 if wide else 4, n)
     B = int(groups.sum())
-    c = SharedCase(44, r.integers(0, 60, n).tolist(), groups, r.integers(0, 20, B).tolist(), 4, 2, 64)
+    c = SharedCase(44, r.integers(0, 200 if wide else 60, n).tolist(), groups, r.integers(0, 20, B).tolist(), 4, 2, 64,
+                   wide=wide)
     check_attention(shared(m, bits)(layer=0, **c.args(m, bits, dv)), *c.want(bits), half=bits == 8)
 
 
@@ -277,7 +280,8 @@ def test_many_prefixes(bits):
 def test_graphs_share_a_workspace(bits, B):
     """Two captured calls on one workspace, replayed in turn, with an eager call between: each its own answer."""
     m, dv = umim(), dev()
-    cases = [SharedCase(50 + i, [200 + 90 * i], [B], [(3 + i) * b % 20 for b in range(B)], 8, 2, 128) for i in range(2)]
+    cases = [SharedCase(50 + i, [200 + 90 * i], [B], [(3 + i) * b % 20 for b in range(B)], 8, 2, 128, wide=B > 3)
+             for i in range(2)]
     ws = m.workspace(m.umim_decode_attention_shared_workspace_size(B, 1, 8, 2, 128), dv)
     args = [c.args(m, bits, dv) for c in cases]
     outs = [torch.empty_like(a["q"]) for a in args]
@@ -315,7 +319,7 @@ def test_calls_at_once_on_two_streams():
 @pytest.mark.parametrize("B", [3, 70])
 def test_results_do_not_change_between_calls(bits, B):
     m, dv = umim(), dev()
-    c = SharedCase(62, [3000], [B], [b % 30 for b in range(B)], 16, 2, 128)
+    c = SharedCase(62, [3000], [B], [b % 30 for b in range(B)], 16, 2, 128, wide=B > 3)
     a = c.args(m, bits, dv)
     first = shared(m, bits)(layer=0, **a)
     for _ in range(10):
