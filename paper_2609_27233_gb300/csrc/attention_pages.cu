@@ -35,6 +35,7 @@
 #include "attention_pages.cuh"
 #include "kv8.cuh"
 #include "mma.cuh"
+#include "tmem.cuh"
 
 namespace umim {
 namespace {
@@ -70,9 +71,9 @@ __device__ __forceinline__ uint2 lds_v2(uint32_t a) {
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
   return v;
 }
-__device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
+__device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
   uint16_t v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  asm volatile("ld.shared.u8 %0, [%1];" : "=h"(v) : "r"(a));
   return v;
 }
 
@@ -423,22 +424,33 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
     }
     // to log2 units; keys past the end masked.  This lane's keys are nt * 8 + 2 qc + {0, 1}.
     float w[2][4];   // weights' exponents (8-bit), then the weights
+    float own = 0.f;   // 8-bit: a lane turns one of the 32 scales into 2^e (lanes 0-15, K's) or e (V's)
+    if constexpr (BITS == 8) {
+      const uint32_t code = lds_u8(sc + lane);
+      own = lane < 16 ? e8m0_value(code) : code == 255 ? NAN : (float)((int)code - 127);
+    }
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
       float ke[2] = {1.f, 1.f}, ve[2] = {0.f, 0.f};
       if constexpr (BITS == 8) {
-        const uint32_t kc = lds_u16(sc + nt * 8 + 2 * qc), vc = lds_u16(sc + 16 + nt * 8 + 2 * qc);
-        ke[0] = e8m0_value(kc & 0xff), ke[1] = e8m0_value(kc >> 8);
-        const uint32_t v0 = vc & 0xff, v1 = vc >> 8;
-        ve[0] = v0 == 255 ? NAN : (float)((int)v0 - 127), ve[1] = v1 == 255 ? NAN : (float)((int)v1 - 127);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          ke[e] = __shfl_sync(0xffffffffu, own, nt * 8 + 2 * qc + e);
+          ve[e] = __shfl_sync(0xffffffffu, own, 16 + nt * 8 + 2 * qc + e);
+        }
       }
 #pragma unroll
       for (int e = 0; e < 2 * NR; ++e) {
-        const bool live = nt * 8 + 2 * qc + (e & 1) < nvalid;
-        const float x = (s[nt][e] + s2[nt][e]) * q_scale[e >> 1] * ke[e & 1];
-        s[nt][e] = live ? x : -INFINITY;
-        w[nt][e] = live ? x + ve[e & 1] : -INFINITY;
+        s[nt][e] = (s[nt][e] + s2[nt][e]) * q_scale[e >> 1] * ke[e & 1];
+        w[nt][e] = s[nt][e] + ve[e & 1];
       }
+    }
+    if (nvalid < 16) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2 * NR; ++e)
+          if (nt * 8 + 2 * qc + (e & 1) >= nvalid) s[nt][e] = w[nt][e] = -INFINITY;
     }
     bool moved = false;
     float c[NR];
@@ -454,18 +466,18 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
       n[j] = BITS == 8 ? fmaxf(n[j], row_max(w)) : m[j];
       // no finite score so far: weights from 0, so that a score of -inf weighs 0 and NaN stays NaN
       const float m0 = m[j] == -INFINITY ? 0.f : m[j], n0 = n[j] == -INFINITY ? 0.f : n[j];
-      c[j] = exp2f(n_was - n0);
+      c[j] = ex2_approx(n_was - n0);
       moved = moved || c[j] != 1.f;
       float sum = 0.f;
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
         for (int e = 2 * j; e < 2 * j + 2; ++e) {
-          const float p = exp2f(s[nt][e] - m0);
+          const float p = ex2_approx(s[nt][e] - m0);
           sum += p;
-          w[nt][e] = BITS == 8 ? exp2f(w[nt][e] - n0 + 15.f) : p;
+          w[nt][e] = BITS == 8 ? ex2_approx(w[nt][e] - n0 + 15.f) : p;
         }
-      l[j] = l[j] * exp2f(m_was - m0) + sum;
+      l[j] = l[j] * ex2_approx(m_was - m0) + sum;
     }
     if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
