@@ -110,7 +110,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   __shared__ uint64_t bars[kAttnWarps][P::kStages];
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
-  const int gw = blockIdx.x * kAttnWarps + warp, total_warps = gridDim.x * kAttnWarps;
+  const int gw = blockIdx.x * kAttnWarps + warp;
+  __shared__ int s_tc;
   uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t *wbuf = base + warp * P::kWarp;
   uint8_t *wscales = base + kAttnWarps * P::kWarp + warp * P::kStages * P::kScales;
@@ -137,11 +138,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   if (SHARED) {
     pre = plan_at(plan, a.n_prefixes);
     plan += 3 * (a.n_prefixes + 1);
-    if (warp == 0)
-      plan_prefixes(a, pre, blockIdx.x == 0, [&](int sequences, int len) {
-        const int rows = sequences * G, nb = rows > a.most_rows ? 0 : ceil_div(rows, 16);
-        return make_int2(nb, nb * ceil_div(len, kPageSize));
-      });
+    if (warp == 0) {
+      const int tc = plan_prefixes(a, pre, blockIdx.x == 0, [&](int b, int len) { return pages_work(a, b, len); },
+                                   [&](int b, int len) { return tc_work(a, b, len); });
+      if (lane == 0) s_tc = tc;
+    }
   }
   if (SHARED || a.smem_plan) {
     own = plan_prefix<kAttnWarps * 32>(a.seq_lens, a.B, a.max_pages, plan, blockIdx.x == 0, a.status);
@@ -159,6 +160,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
     own = pref[a.B];
   }
   const int total = Hkv * (own + (SHARED ? pre.pages[a.n_prefixes] : 0));
+  // (s_tc: the barriers of plan_prefix have passed)
+  const int ctas = SHARED ? pages_ctas((int)gridDim.x, total, (int64_t)Hkv * s_tc, BITS == 8) : (int)gridDim.x;
+  if (SHARED && (int)blockIdx.x >= ctas) return;
+  const int total_warps = ctas * kAttnWarps;
   const int W = max(1, ceil_div(total, total_warps));
   if (blockIdx.x == 0 && threadIdx.x == 0) ws.at.plan->W = W;
   const int start = (int)min((int64_t)gw * W, (int64_t)total);

@@ -60,6 +60,29 @@ inline int64_t tc_max_segments(int B, int n, int G) {
   return B / (2 * tile_sequences(G)) + std::min<int64_t>(n, (int64_t)B * G / (kTcMinRows + 1)) + 1;
 }
 
+// CTAs of the pages' kernel, `ctas` for all.  Both kernels run at once where each has a fair part of the
+// work, the CTAs that this one leaves unused making room for the other's: 64 sequences behind 16000
+// entries, 16384 of their own, 32/8 heads, D = 128: 52.9 -> 44.4 us, 96 behind 4 x 4000 with 4000, 37.9 -> 34.3.  Below an
+// eighth they run one after the other on the whole GPU: few CTAs take their time over many
+// short sequences (64 of one page each beside 16384 entries: 41 -> 52 us).  A key tile of a row tile takes an SM
+// about as long as 12 (16 bits) or 15 pages of 16 rows.
+__device__ __forceinline__ int pages_ctas(int ctas, int64_t pages, int64_t tiles, bool narrow) {
+  const int64_t all = pages + tiles * (narrow ? 15 : 12);
+  if (pages * 8 < all || pages * 10 > all * 9) return ctas;
+  return (int)((ctas * pages + all / 2) / all);
+}
+
+// the key tiles of a prefix for its row tiles, 0 where its rows are too few for the tensor cores' kernel
+__device__ __forceinline__ int2 tc_work(const PagesArgs &a, int sequences, int len) {
+  const int tiles = sequences * a.G > a.most_rows ? ceil_div(sequences, tile_sequences(a.G)) : 0;
+  return make_int2((tiles + 1) / 2, tiles * ceil_div(len, kTcKeys));
+}
+// the page visits of the rest
+__device__ __forceinline__ int2 pages_work(const PagesArgs &a, int sequences, int len) {
+  const int rows = sequences * a.G, nb = rows > a.most_rows ? 0 : ceil_div(rows, 16);
+  return make_int2(nb, nb * ceil_div(len, kPageSize));
+}
+
 struct PagesWs {
   AttnWs at;
   PrefixPlan pre, tc;
@@ -121,11 +144,11 @@ inline size_t pages_carve(void *base, PagesWs *ws, int B, int n, int G, int Hkv,
 // The plan of the prefixes, by a CTA's first warp (a barrier follows at the
 // caller's).  Offsets that decrease or leave [0, B] count as the largest before
 // them, a length outside the table as 0; both are recorded when `report` is set.
-// work(rows' sequences, entries): (blocks, page visits).
-template <typename Work>
-__device__ __forceinline__ void plan_prefixes(const PagesArgs &a, const PrefixPlan &p, bool report, Work work) {
+// work(rows' sequences, entries): (blocks, page visits); the result is the sum of other's second.
+template <typename Work, typename Other>
+__device__ __forceinline__ int plan_prefixes(const PagesArgs &a, const PrefixPlan &p, bool report, Work work, Other other) {
   const int lane = threadIdx.x & 31, n = a.n_prefixes;
-  int most = 0, pages = 0, blocks = 0;
+  int most = 0, pages = 0, blocks = 0, rest = 0;
   for (int i0 = 0; i0 <= n; i0 += 32) {
     const int i = i0 + lane;
     int o = i <= n ? (a.prefix_offsets ? a.prefix_offsets[i] : i * a.B) : 0;   // (no offsets: one prefix for all)
@@ -151,6 +174,7 @@ __device__ __forceinline__ void plan_prefixes(const PagesArgs &a, const PrefixPl
         if (report) set_error(a.status, UMIM_ERR_INVALID_ARG);
       } else if (L > 0) {
         w = work(p.first[i + 1] - p.first[i], L);
+        rest += other(p.first[i + 1] - p.first[i], L).y;
       }
     }
     int xb = w.x, xp = w.y;
@@ -166,6 +190,7 @@ __device__ __forceinline__ void plan_prefixes(const PagesArgs &a, const PrefixPl
     blocks += __shfl_sync(0xffffffffu, xb, 31);
     pages += __shfl_sync(0xffffffffu, xp, 31);
   }
+  return __reduce_add_sync(0xffffffffu, rest);
 }
 
 // the last i in [0, n) with at[i] * times <= x

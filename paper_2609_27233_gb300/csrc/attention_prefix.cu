@@ -156,12 +156,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   __shared__ float4 s_scales[4][kTcKeys / kPageSize];   // 8-bit: of the last four key tiles' pages, 2^E, F, 2^(-F - 7)
   __shared__ float s_row[2][2][2][kTcRows];   // [tile's parity][slot][half]: a row's maximum, or sum
   __shared__ uint32_t tmem_base;
-  __shared__ int s_abort;
+  __shared__ int s_abort, s_pages;
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(tc_raw) + 1023) & ~uintptr_t(1023));
   const int warp = warp_index(), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     s_abort = 0;
+    s_pages = 0;
     for (int s = 0; s < 2; ++s) {
       mbar_init(&k_full[s], BITS == 8 ? kConverters + 1 : 1);
       mbar_init(&k_empty[s], 2);   // read by both slots' products, or twice by one's
@@ -193,17 +194,28 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   // Nothing here waits for the kernel before: this one's inputs and workspace were
   // free when that one let it start (its own wait was over), and it waits at its end
   // for that one, for the combine kernel behind both.
-  if (warp == 2)
-    plan_prefixes(a, plan, false, [&](int sequences, int len) {   // (the kernel before reports)
-      const int tiles = sequences * a.G > a.most_rows ? ceil_div(sequences, spt) : 0;
-      return make_int2((tiles + 1) / 2, tiles * ceil_div(len, kTcKeys));
-    });
+  __syncthreads();   // (s_pages is 0)
+  if (warp == 2) {   // (the kernel before reports)
+    const int rest = plan_prefixes(a, plan, false, [&](int b, int len) { return tc_work(a, b, len); },
+                                   [&](int b, int len) { return pages_work(a, b, len); });
+    if (lane == 0) atomicAdd(&s_pages, rest);
+  } else if (warp > 2) {   // the sequences' own pages, as the kernel before counts them
+    int own = 0;
+    for (int b = threadIdx.x - 96; b < a.B; b += kTcThreads<BITS> - 96) {
+      const int len = a.seq_lens[b];
+      if (len > 0 && (int64_t)len <= (int64_t)a.max_pages * kPageSize) own += ceil_div(len, kPageSize);
+    }
+    own = __reduce_add_sync(0xffffffffu, own);
+    if (lane == 0 && own > 0) atomicAdd(&s_pages, own);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base;
   const int total = a.Hkv * plan.pages[a.n_prefixes];
-  const int W = max(2, ceil_div(total, (int)gridDim.x));   // (2: every CTA between a segment's first and last has a tile of it)
+  const int others = pages_ctas((int)gridDim.x, (int64_t)a.Hkv * s_pages, total, BITS == 8);
+  const int ctas = others == (int)gridDim.x ? others : (int)gridDim.x - others;   // (one after the other, or at once)
+  const int W = max(2, ceil_div(total, ctas));   // (2: every CTA between a segment's first and last has a tile of it)
   const int start = (int)min((int64_t)blockIdx.x * W, (int64_t)total), end = min(start + W, total);
   if (blockIdx.x == 0) {   // for the combine kernel
     for (int i = threadIdx.x; i <= a.n_prefixes; i += kTcThreads<BITS>) {
