@@ -21,7 +21,8 @@ constexpr int kSmemPlanBatch = 4096;   // sequences whose prefix sum a decode CT
 
 struct AttnPlan {
   int32_t W;          // pages per warp
-  int32_t pad[63];
+  int32_t total;      // (segment, page) pairs (attention_pages.cu)
+  int32_t pad[62];
 };
 
 struct AttnWs {

@@ -6,8 +6,9 @@
 //
 // The split is attention.cu's: (segment, page) pairs of the whole batch,
 // flattened, an equal contiguous range for every warp of a persistent grid, one
-// partial result (m, l, acc) a piece of a range that lies in one segment, merged by
-// a small kernel.  A segment is a list of pages with up to 16 query rows that
+// partial result (m, l, acc) a piece of a range that lies in one segment (without
+// prefixes, the last ones of a CTA's warps are joined where they are of one segment),
+// merged by a small kernel.  A segment is a list of pages with up to 16 query rows that
 // attend to all of it: the query heads of one KV head over a sequence's own
 // entries, or 16 of the rows (sequence, query head) of a group over the group's
 // prefix, so that a page of a prefix is read once for 16 rows.
@@ -112,6 +113,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int gw = blockIdx.x * kAttnWarps + warp;
   __shared__ int s_tc;
+  __shared__ int s_last[kAttnWarps];   // the segment of a warp's last piece, -1 for none
   uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t *wbuf = base + warp * P::kWarp;
   uint8_t *wscales = base + kAttnWarps * P::kWarp + warp * P::kStages * P::kScales;
@@ -165,10 +167,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   if (SHARED && (int)blockIdx.x >= ctas) return;
   const int total_warps = ctas * kAttnWarps;
   const int W = max(1, ceil_div(total, total_warps));
-  if (blockIdx.x == 0 && threadIdx.x == 0) ws.at.plan->W = W;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    ws.at.plan->W = W;
+    ws.at.plan->total = total;
+  }
   const int start = (int)min((int64_t)gw * W, (int64_t)total);
   const int end = min(total, start + W);
-  if (start >= end) return;
+  bool whole = start < end;   // this warp has a last piece to hand in
+  if (SHARED && !whole) return;   // (without prefixes there are barriers to come)
 
   const uint64_t pol = policy_evict_first();
 
@@ -245,15 +251,16 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   // ---- compute cursor and loader cursor (every lane keeps both; one issues the copies) ----
   Segment cs, ls;
   int cpi, lpi;
-  locate(start, cs, cpi);
+  int ld_pos = start;
+  if (SHARED || whole) locate(start, cs, cpi);
   ls = cs;
   lpi = cpi;
-  int ld_pos = start;
   auto page_of = [&]() {
     const int cols = SHARED && ls.prefix ? a.max_prefix_pages : a.max_pages;
     return in_bounds(lpi, cols, a.status, kSitePagesTable) ? ls.table[lpi] : -1;
   };
-  int next_page = page_of();   // looked up a copy ahead: the copy does not wait for the table
+  // looked up a copy ahead: the copy does not wait for the table
+  int next_page = SHARED || whole ? page_of() : -1;
   auto issue = [&](int stage) {
     int c = a.layer * a.n_pages + next_page;
     if (next_page < 0 || next_page >= a.n_pages) {
@@ -328,7 +335,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
       }
     }
   };
-  load_q();
+  if (SHARED || whole) load_q();
   float acc[NT][4];
   // a row's largest score and weight (log2), and sum of exp2(score - m)
   float m[NR], n[NR], l[NR];
@@ -340,23 +347,19 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
   };
   reset();
 
-  auto flush = [&]() {
+  // the segment's rows to [16] (m, l) and [16] rows of D columns, `stride` apart
+  auto hand_in = [&](float2 *ml, float *columns, int stride) {
     // complete the row sums across the 4 threads of each row
 #pragma unroll
     for (int j = 0; j < NR; ++j) {
       l[j] += __shfl_xor_sync(0xffffffffu, l[j], 1);
       l[j] += __shfl_xor_sync(0xffffffffu, l[j], 2);
     }
-    const int64_t piece = number(cs) + gw;
-    if (!in_bounds(piece, (int64_t)Hkv * (a.B + (SHARED ? pre.blocks[a.n_prefixes] : 0)) + total_warps, a.status,
-                   kSitePagesPiece))
-      return;
 #pragma unroll
     for (int j = 0; j < NR; ++j) {
       if (rows[j] < 0) continue;
-      const int64_t at = piece * 16 + qr + 8 * j;
-      if (qc == 0) ws.at.part_ml[at] = make_float2(m[j], l[j]);
-      float *dst = ws.at.part_acc + at * D;
+      if (qc == 0) ml[qr + 8 * j] = make_float2(m[j], l[j]);
+      float *dst = columns + (qr + 8 * j) * stride;
       if constexpr (BITS == 16) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -377,6 +380,15 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
       }
     }
   };
+  // a piece's place in the workspace, -1 for none (debug build)
+  auto place = [&](int64_t piece) {
+    const int64_t n = (int64_t)Hkv * (a.B + (SHARED ? pre.blocks[a.n_prefixes] : 0)) + total_warps;
+    return in_bounds(piece, n, a.status, kSitePagesPiece) ? piece : int64_t(-1);
+  };
+  auto flush = [&]() {
+    const int64_t at = place((int64_t)number(cs) + gw);
+    if (at >= 0) hand_in(ws.at.part_ml + at * 16, ws.at.part_acc + at * 16 * D, D);
+  };
 
   int it = 0;
   for (int pos = start; pos < end; ++pos, ++it) {
@@ -394,7 +406,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
       // let the copies still in flight land (each wait bounded) before leaving
       for (int k = 1; k < P::kStages && pos + k < ld_pos; ++k)
         mbar_wait(&bars[warp][(it + k) % P::kStages], ((it + k) / P::kStages) & 1);
-      return;
+      if (SHARED) return;
+      whole = false;
+      break;
     }
     const uint32_t ks = smem_u32(wbuf + stage * P::kStage), vs = ks + 16 * P::kRow;
     const uint32_t sc = smem_u32(wscales + stage * P::kScales);
@@ -572,16 +586,70 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
     // refill this stage
     if (ld_pos < end) issue(stage);
   }
-  flush();
+
+  // (With prefixes the same took 3 to 8 % longer: 16 rows a piece to join, in place of 4 or 7.)
+  if constexpr (SHARED) {
+    flush();
+    return;
+  }
+  // The warps' last pieces: those of one segment meet in shared memory, where the rings were, and become one
+  // piece of the first of its warps: with four sequences of 32768 entries a row had 114 pieces, one a
+  // warp, and a call took 33.0 us in place of 29.4.
+  constexpr int kStride = D + 4;   // of a row there: eight rows of a store meet no bank twice
+  static_assert(16 * kStride * 4 + 128 <= P::kWarp, "a piece where a warp's ring was");
+  if (lane == 0) s_last[warp] = whole ? number(cs) : -1;
+  __syncthreads();
+  const int last = lane < kAttnWarps ? s_last[lane] : -1;
+  const int before = __shfl_up_sync(0xffffffffu, last, 1), behind = __shfl_down_sync(0xffffffffu, last, 1);
+  const bool first_of = last >= 0 && (lane == 0 || before != last);
+  const bool alone = first_of && (lane == kAttnWarps - 1 || behind != last);
+  const uint32_t firsts = __ballot_sync(0xffffffffu, first_of), alones = __ballot_sync(0xffffffffu, alone);
+  if (whole) {
+    if (alones >> warp & 1) flush();
+    else hand_in(reinterpret_cast<float2 *>(wbuf + 16 * kStride * 4), reinterpret_cast<float *>(wbuf), kStride);
+  }
+  __syncthreads();
+  for (uint32_t runs = firsts & ~alones; runs; runs &= runs - 1) {
+    constexpr int E = D / 32;
+    const int w0 = __ffs(runs) - 1, seg = __shfl_sync(0xffffffffu, last, w0);
+    const int n = __popc(__ballot_sync(0xffffffffu, last == seg && lane >= w0));
+    for (int row = warp; row < G; row += kAttnWarps) {
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < n) ml = reinterpret_cast<const float2 *>(base + (w0 + lane) * P::kWarp + 16 * kStride * 4)[row];
+      float M = ml.x;
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+      M = __shfl_sync(0xffffffffu, M, 0);
+      const float c = exp2f(ml.x - (M == -INFINITY ? 0.f : M));   // (no finite score: weighted, not skipped)
+      float L = ml.y * c, o[E];
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 4
+      for (int w = 0; w < n; ++w) {
+        const float cw = __shfl_sync(0xffffffffu, c, w);
+        const float *src = reinterpret_cast<const float *>(base + (w0 + w) * P::kWarp) + row * kStride + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(src[e], cw, o[e]);
+      }
+      const int64_t at = place((int64_t)seg + blockIdx.x * kAttnWarps + w0);
+      if (at < 0) continue;
+      if (lane == 0) ws.at.part_ml[at * 16 + row] = make_float2(M, L);
+      float *dst = ws.at.part_acc + (at * 16 + row) * D + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) dst[e] = o[e];
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
-// combine for shared prefixes: WPR warps per (b, query head) row, over the pieces
-// of its own entries' segment and then of its prefix's block
+// combine: WPR warps per (b, query head) row, over the pieces of its own entries'
+// segment and then of its prefix's block
 // ---------------------------------------------------------------------------
-template <int D, int WPR>
+template <int D, bool SHARED, int WPR>
 __global__ void __launch_bounds__(kCombineThreads)
-    shared_combine_kernel(PagesWs ws, bool tc, int B, int n_prefixes, int Hq, int Hkv, int G, __nv_bfloat16 *out) {
+    pages_combine_kernel(PagesWs ws, bool tc, int B, int n_prefixes, int Hq, int Hkv, int G, __nv_bfloat16 *out) {
   constexpr int E = D / 32;
   constexpr int kWarps = kCombineThreads / 32, RPB = kWarps / WPR;   // rows per CTA
   __shared__ float s_m[kWarps], s_l[kWarps];
@@ -595,18 +663,28 @@ __global__ void __launch_bounds__(kCombineThreads)
   for (int e = 0; e < E; ++e) o[e] = 0.f;
   bool any = false;
   if (live) {
-    const int b = row_g / Hq, h = row_g % Hq, g = h / G, W = ws.at.plan->W;
-    // pieces of the segment that takes n positions from `at` on: seg + w for the warps w that meet them
+    const int b = row_g / Hq, h = row_g % Hq, g = h / G, W = ws.at.plan->W, total = ws.at.plan->total;
+    // Pieces of the segment that takes n positions from `at` on: seg + w for the warps w that meet them.
+    // Without prefixes they are joined: the first of those warps has one, the first of every further CTA,
+    // and the last warp where the segment ends inside its range (handed in by itself).
     auto merge = [&](int seg, int at, int n, int row) {
       if (n <= 0) return;
       any = true;
-      const int w0 = at / W, w1 = (at + n - 1) / W;
-      merge_rows<E>(ws.at, (int64_t)(seg + w0) * 16 + row, w1 - w0 + 1, sub, WPR, M, l, o);
+      const int w0 = at / W, w1 = (at + n - 1) / W, c0 = w0 / kAttnWarps, c1 = w1 / kAttnWarps;
+      const bool inside = w1 > w0 && w1 % kAttnWarps != 0 && at + n < min((w1 + 1) * (int64_t)W, (int64_t)total);
+      auto row_of = [&](int k) {
+        const int w = SHARED || k == 0 ? w0 + k : k <= c1 - c0 ? (c0 + k) * kAttnWarps : w1;
+        return (int64_t)(seg + w) * 16 + row;
+      };
+      merge_pieces<E>(
+          SHARED ? w1 - w0 + 1 : 1 + c1 - c0 + (inside ? 1 : 0), sub, WPR, M, l, o,
+          [&](int k) { return ws.at.part_ml + row_of(k); },
+          [&](int k) { return ws.at.part_acc + row_of(k) * D + lane * E; });
     };
     const int first = ws.at.pref[b], n = ws.at.pref[b + 1] - first;
     merge(b * Hkv + g, Hkv * first + g * n, n, h % G);
-    const int i = last_at_most(ws.pre.first, n_prefixes, 1, b);
-    if (b >= ws.pre.first[i] && b < ws.pre.first[i + 1]) {
+    const int i = SHARED ? last_at_most(ws.pre.first, n_prefixes, 1, b) : 0;
+    if (SHARED && b >= ws.pre.first[i] && b < ws.pre.first[i + 1]) {
       const int nb = ws.pre.blocks[i + 1] - ws.pre.blocks[i], bi = b - ws.pre.first[i];
       const int ns = tc ? ws.tc.blocks[i + 1] - ws.tc.blocks[i] : 0;
       if (nb > 0) {
@@ -727,26 +805,16 @@ umim_status run_pages(const CacheView &kv, PagesArgs a, void *out, void *workspa
   }
   trace_mark(stream, "attention.combine");
   __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(out);
-  if constexpr (SHARED) {
-    // a row merges the pieces of two segments
-    const int wpr = combine_warps(2 + total_warps / std::max(1, (a.n_prefixes + a.B) * a.Hkv) * 2);
-    const int rows = kCombineThreads / 32 / wpr;
-    auto comb = wpr == 8 ? shared_combine_kernel<D, 8>
-                : wpr == 4 ? shared_combine_kernel<D, 4>
-                : wpr == 2 ? shared_combine_kernel<D, 2> : shared_combine_kernel<D, 1>;
-    if (launch_pdl(comb, dim3((unsigned)((a.B * a.Hq + rows - 1) / rows)), dim3(kCombineThreads), 0, stream, ws, tc,
-                   a.B, a.n_prefixes, a.Hq, a.Hkv, a.G, o) != cudaSuccess)
-      return UMIM_ERR_CUDA;
-  } else {
-    const int wpr = combine_warps(1 + total_warps / std::max(1, a.B * a.Hkv));
-    const int rows = kCombineThreads / 32 / wpr;
-    auto comb = wpr == 8 ? attn_combine_kernel<D, 8>
-                : wpr == 4 ? attn_combine_kernel<D, 4>
-                : wpr == 2 ? attn_combine_kernel<D, 2> : attn_combine_kernel<D, 1>;
-    if (launch_pdl(comb, dim3((unsigned)((a.B * a.Hq + rows - 1) / rows)), dim3(kCombineThreads), 0, stream, ws.at, a.B,
-                   a.Hq, a.Hkv, a.G, o) != cudaSuccess)
-      return UMIM_ERR_CUDA;
-  }
+  // about as many pieces as a row has: one or two a CTA that has some of its entries, or, of two segments, one a warp
+  const int n = SHARED ? a.n_prefixes : 0, segments = std::max(1, (n + a.B) * a.Hkv);
+  const int wpr = combine_warps(SHARED ? 2 + total_warps / segments * 2 : 2 + 2 * (total_warps / kAttnWarps) / segments);
+  const int rows = kCombineThreads / 32 / wpr;
+  auto comb = wpr == 8 ? pages_combine_kernel<D, SHARED, 8>
+              : wpr == 4 ? pages_combine_kernel<D, SHARED, 4>
+              : wpr == 2 ? pages_combine_kernel<D, SHARED, 2> : pages_combine_kernel<D, SHARED, 1>;
+  if (launch_pdl(comb, dim3((unsigned)((a.B * a.Hq + rows - 1) / rows)), dim3(kCombineThreads), 0, stream, ws, tc, a.B, n,
+                 a.Hq, a.Hkv, a.G, o) != cudaSuccess)
+    return UMIM_ERR_CUDA;
   trace_mark(stream, nullptr);
   return cudaGetLastError() == cudaSuccess ? UMIM_OK : UMIM_ERR_CUDA;
 }

@@ -6,11 +6,12 @@
 // over a range of the prefix's entries is one partial result (m, l, O) a row,
 // which the combine kernel (attention_pages.cu) joins with the row's others.
 //
-// What bounds it: not the tensor cores (10 us of 25 in the case below) and not HBM, but what a slot's
+// What bounds it: not the tensor cores (10 us of 25 in the case below, alone on the GPU) and not HBM, but what a slot's
 // tile goes through one step after the other: S, its way to the softmax warps, the
 // softmax, P V, and the next S, some 4000 cycles in 16 bits, with two slots in turn to
 // cover it.  64 sequences x 4 query heads a KV head behind 16384 entries, 8 KV heads, D = 128,
-// 16 bits: 25 us of a call of 54; five 8-bit prefixes of 12000, 120 sequences: 65 of 86.
+// 16 bits: a call of 48 us, 54 where the own entries' kernel does not run beside this one but
+// before it; five 8-bit prefixes of 12000, 120 sequences: 65 us of 86.
 //
 // Work: a row tile is 128 rows (whole sequences), a key tile 128 entries (8 pages).  A
 // segment is a pair of row tiles, or a single one, of a prefix and KV head;
