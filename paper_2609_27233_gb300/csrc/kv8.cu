@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kRowThreads) kv8_write_kernel(RowsArgs a) {
   griddep_wait();
   if (blockIdx.x == 0) check_rows(a);
   const int lane = threadIdx.x & 31, heads = 2 * a.n_kv_heads, parts = ceil_div(heads, U);
-  const int task = (blockIdx.x * kRowThreads + threadIdx.x) >> 5;
+  const int task = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
   const int t0 = task / parts * kWarpRows<D>, h0 = task % parts * U;
   if (t0 >= a.T) return;
   const int t = t0 + lane / kRowLanes<D>, col = lane % kRowLanes<D> * 16;
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kRowThreads) kv8_read_kernel(RowsArgs a) {
   griddep_wait();
   if (blockIdx.x == 0) check_rows(a);
   const int lane = threadIdx.x & 31, heads = 2 * a.n_kv_heads, parts = ceil_div(heads, U);
-  const int task = (blockIdx.x * kRowThreads + threadIdx.x) >> 5;
+  const int task = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
   const int t0 = task / parts * kWarpRows<D>, h0 = task % parts * U;
   if (t0 >= a.T) return;
   const int t = t0 + lane / kRowLanes<D>, col = lane % kRowLanes<D> * 16;
