@@ -500,7 +500,8 @@ umim_status umim_decode_attention_kv8(const void *q, int32_t n_q_heads, const um
  * prefix_offsets  device int32 [n_prefixes + 1], nondecreasing in [0, batch],
  *                 or NULL with n_prefixes == 1: every sequence
  * block_table     device int32 [batch][max_pages]: own entries (entry t of a
- *                 sequence, t = 0 behind the prefix, in page t / 16)
+ *                 sequence, t = 0 behind the prefix, in page t / 16).  Either
+ *                 table may have no columns, and may be NULL then
  * seq_lens        device int32 [batch]: own entries
  * out             device bf16 [batch][n_q_heads][head_dim]
  * workspace       device, umim_decode_attention_shared_workspace_size() bytes
@@ -509,8 +510,12 @@ umim_status umim_decode_attention_kv8(const void *q, int32_t n_q_heads, const um
  * UMIM_ERR_UNSUPPORTED: batch > 4096, n_prefixes > 512, page visits
  * n_kv_heads * (batch * max_pages + (n_prefixes + batch * n_q_heads /
  * n_kv_heads / 16) * max_prefix_pages) above 2^30, and the shapes that
- * umim_decode_attention does not support.  Device-side errors:
- * UMIM_ERR_INVALID_ARG for a length outside its table (it counts as 0), an
+ * umim_decode_attention does not support.
+ * Over the 8-bit cache, with a prefix of more than 16 rows (sequence, query
+ * head of one KV head), the entries of a page of K or of V may be rounded to
+ * 2^-31 of the largest of them, and weights to 2^-12 of themselves or 2^-32 of
+ * the largest (weights times the largest scale of their page of V).
+ * Device-side errors: UMIM_ERR_INVALID_ARG for a length outside its table (it counts as 0), an
  * offset that decreases (it counts as the largest before it) or leaves
  * [0, batch] (as 0), and a used page outside [0, n_pages) (it reads as
  * zeros); UMIM_ERR_TIMEOUT for a stalled copy.

@@ -675,7 +675,9 @@ umim_status shared_checked(const void *q, int32_t n_q_heads, void *values, void 
       n_kv_heads * ((int64_t)batch * max_pages + blocks * max_prefix_pages) > kMaxPageVisits)
     return UMIM_ERR_UNSUPPORTED;
   if (batch == 0) return UMIM_OK;
-  if (!q || !prefix_table || !prefix_lens || !block_table || !seq_lens || !out) return UMIM_ERR_INVALID_ARG;
+  // (a table without columns may have no address)
+  if (!q || (!prefix_table && max_prefix_pages > 0) || !prefix_lens || (!block_table && max_pages > 0) || !seq_lens || !out)
+    return UMIM_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(out, 2)) return UMIM_ERR_INVALID_ARG;
   const DeviceScope scope(stream);
   const int sms = scope.sms();

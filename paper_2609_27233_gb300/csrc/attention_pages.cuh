@@ -68,7 +68,7 @@ inline int64_t tc_max_segments(int B, int n, int G) {
 // about as long as 12 (16 bits) or 15 pages of 16 rows.
 __device__ __forceinline__ int pages_ctas(int ctas, int64_t pages, int64_t tiles, bool narrow) {
   const int64_t all = pages + tiles * (narrow ? 15 : 12);
-  if (pages * 8 < all || pages * 10 > all * 9) return ctas;
+  if (pages * 8 <= all || pages * 10 >= all * 9) return ctas;   // (no work at all too)
   return (int)((ctas * pages + all / 2) / all);
 }
 

@@ -34,12 +34,13 @@
 // 16 entries: TMA reads rows before the first as zeros, so that nothing behind the
 // prefix's end is ever read; S is masked there.
 //
-// 8-bit pages: eight warps read e4m3 rows and make fp16 operands of them, code * 2^(e - E) with E the largest e of the page's 16
-// rows (a row's values are exact down to 2^-24 * 2^E, 2^-32 of the page's largest; converting
-// to value * 2^e in bf16 took twice the instructions, and they bound the kernel).  q
+// 8-bit pages: eight warps read e4m3 rows and make fp16 operands of them, code * 2^(e - E + 7) with E the largest e of the
+// page's 16 rows: 57344 at most, and multiples of 2^-24, so off by 2^-40 of the page's largest
+// at most; rows with e below E - 31 become zeros, which is 2^-31 of it at most.  (Converting
+// to value * 2^e in bf16 took twice the instructions, and they bound the kernel.)  q
 // becomes fp16 in place, below 2^15 by a power of two a row.  With r the row's and the page's
 // powers of two times the scale, and F the page's largest exponent of V's rows,
-//     w = 2^(r s + F - n + 7),   O = sum w v',   l = sum 2^(-F - 7) w,   out = 2^-7 O / l,
+//     w = 2^(r s + F - n + 7),   O = sum w v',   l = sum 2^(-F - 7) w,   out = 2^-14 O / l,
 // n the running maximum of r s + F: the weights that multiply V are at most 2^15 and are one
 // fp16 number each (2^-12 of themselves), and l is exact in fp32, a page's sum at a time.
 #include <cuda_fp16.h>
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   __shared__ __align__(8) uint64_t q_full[2], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2],
       p_full[2][2], pv_done[2], o_free[2], turn[2], mma_done[2],
       met[2][4], q_ready[2], scales_full[4];
-  __shared__ float4 s_scales[4][kTcKeys / kPageSize];   // 8-bit: of the last four key tiles' pages, 2^E, F, 2^(-F - 7)
+  __shared__ float4 s_scales[4][kTcKeys / kPageSize];   // 8-bit: of the last four key tiles' pages, 2^(E - 7), F, 2^(-F - 7)
   __shared__ float s_row[2][2][2][kTcRows];   // [tile's parity][slot][half]: a row's maximum, or sum
   __shared__ uint32_t tmem_base;
   __shared__ int s_abort, s_pages;
@@ -592,7 +593,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
 #pragma unroll
             for (int g = 0; g < 2; ++g) {   // 16 keys: P (<= 2^8) in bf16 pairs, and what that leaves
               float p[16];
-  #pragma unroll
+#pragma unroll
               for (int c = 0; c < 16; c += 2) {
                 const float2 x = __ffma2_rn(make_float2(s[g * 16 + c], s[g * 16 + c + 1]), sl2x2, nm2);
                 const float2 y = make_float2(ex2_approx(x.x), ex2_approx(x.y));   // masked (-inf): 0
@@ -643,7 +644,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             tmem_ld_32x32b_x32(t_o + half * kCols + c * 32, o);
             if constexpr (BITS == 8)
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] *= 0x1p-7f;
+              for (int i = 0; i < 32; ++i) o[i] *= 0x1p-14f;
             if (store)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
@@ -705,7 +706,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
 #pragma unroll
           for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
           const int down = (int)code - (int)most;   // 0 or less
-          const float scale = code == 255 ? NAN : down < -126 ? 0.f : __uint_as_float((uint32_t)(127 + down) << 23);
+          const float scale = code == 255 ? NAN : down < -126 ? 0.f : __uint_as_float((uint32_t)(134 + down) << 23);
           const __half2 scale2 = __floats2half2_rn(scale, scale);
           factor = *reinterpret_cast<const uint32_t *>(&scale2);
           most_v = __shfl_sync(0xffffffffu, most, 16);
@@ -744,7 +745,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           ok = wwait(&k_empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
           if (!ok) break;
           if (lane == 0) {   // (four tiles' scales: S of the tile two before is done, so the softmax of the one four before is)
-            s_scales[pos & 3][w] = make_float4(e8m0_value(most), (float)((int)most_v - 127), ldexpf(1.f, 120 - (int)most_v), 0.f);
+            s_scales[pos & 3][w] = make_float4(e8m0_value(most) * 0x1p-7f, (float)((int)most_v - 127), ldexpf(1.f, 120 - (int)most_v), 0.f);
             mbar_arrive(&scales_full[pos & 3]);
           }
           convert(k, smem + L::kK + s * L::kTile, factor, 0);

@@ -65,9 +65,11 @@ def attention_bound(want, size, most, finest, half):
     |V| / scale.  That is 2^-40 * finest; it shows where the rows of the large weights hold zeros in a column.
 
     half: over a prefix of many rows in the 8-bit cache a weight is one fp16 number, off by 2^-12 of itself (the row
-    sum is made of the weights before that), in units of 2^-7 of the running maximum, which some weight reached: 2^-25
-    * 2^-7 = 2^-32 of the largest may be missing of every row's |V| / scale.  (Rows are exact there while
-    their scales lie within 2^15 of their page's largest, as all of these do.)"""
+    sum is made of the weights before that).  Operands there are in units of their page's largest scale F, so it is
+    weight * F whose largest is (after the running maximum) 2^7 or more units and that is a multiple of 2^-24 of one:
+    2^-25 * 2^-7 = 2^-32 of the largest weight * F may be missing of every row's |V| / F, a row's own scale of which
+    is F at most.  SharedCase's `finest` is that sum, and 2^-8 of the rows' (2^-32 * 2^-8 = 2^-40).  (Rows are exact there while
+    their scales lie within 2^22 of their page's largest: test_values_far_apart_on_the_tensor_cores has others.)"""
     eps = 4 * (2.0 ** -16 + 2.0 ** -17 * most[..., None]) + (2.0 ** -12 if half else 0)
     return 2.0 ** -8 * np.abs(want) + eps * size + 2.0 ** (-32 if half else -40) * finest + 1e-30
 
@@ -113,8 +115,15 @@ class SharedCase:
                 if self.offsets[i] <= b < self.offsets[i + 1]:
                     at[b].insert(0, self.prefix_bt[i])
                     ns[b].insert(0, self.prefix_lens[i])
-        return oracle.kv8.attend(self.q, pool, layer, at, ns, scale,
-                                 row_scales=oracle.kv8.scales(self.scales) if bits == 8 else None)
+        if bits == 16:
+            return oracle.kv8.attend(self.q, pool, layer, at, ns, scale)
+        own = oracle.kv8.scales(self.scales)
+        most_of = own.copy()   # V's scales: the largest of a prefix's page, over the entries that it has
+        for table, n in zip(self.prefix_bt, self.prefix_lens):
+            for p in range(-(-n // PAGE)):
+                most_of[:, table[p], 1] = own[:, table[p], 1, :, :min(PAGE, n - PAGE * p)].max(-1)[..., None]
+        want, size, most, finest = oracle.kv8.attend(self.q, pool, layer, at, ns, scale, row_scales=own)
+        return want, size, most, oracle.kv8.attend(self.q, pool, layer, at, ns, scale, row_scales=most_of)[3] + finest / 256
 
     def args(self, m, bits, d):
         pool = to_bf16(self.bits, d) if bits == 16 else to_pool8(m, self.codes, self.scales, d)

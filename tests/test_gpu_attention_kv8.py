@@ -7,7 +7,7 @@ import torch
 import oracle
 import workloads as W
 from helpers import dev, umim
-from kv8_helpers import SharedCase, check_attention, i32, key_like, shared, tables, to_bf16, to_pool8
+from kv8_helpers import SharedCase, attention_bound, check_attention, i32, key_like, shared, tables, to_bf16, to_pool8
 
 pytestmark = pytest.mark.gpu
 
@@ -260,6 +260,41 @@ def test_nan_in_a_prefix(bits, many):
     got = shared(m, bits)(layer=0, **c.args(m, bits, dv)).float().cpu().numpy()
     assert np.isnan(got[:B - 2, 4:]).all() and np.isfinite(got[:, :4]).all() and np.isfinite(got[B - 2:]).all()
     check_attention(torch.from_numpy(got[:, :4].copy()), *(x[:, :4] for x in c.want(bits)), half=bits == 8)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_far_apart_on_the_tensor_cores(d):
+    """Rows of V in one page with scales up to 2^30 apart.  The operands are multiples of 2^-24 in units of 2^-7 of the
+    page's largest scale: a value is off by 2^-32 of that at most, and so is their mean by weights that sum up to 1."""
+    m, dv = umim(), dev()
+    c = SharedCase(45, [333], [40], [(5 * b) % 20 for b in range(40)], 8, 2, d, wide=True)
+    f = oracle.bf16.to_f64(c.bits)
+    f[:, :, 1] *= np.exp2(W.rng(46).integers(-11, 12, f[:, :, 1].shape[:-1]))[..., None]
+    c.codes, c.scales = oracle.kv8.quantise(oracle.bf16.from_f32(f.astype(np.float32)))
+    s = c.scales[:, :, 1].astype(int)
+    assert (s.max(-1) - s.min(-1)).max() <= 31
+    want, size, most, finest = c.want(8)
+    got = shared(m, 8)(layer=0, **c.args(m, 8, dv))
+    err = np.abs(got.double().cpu().numpy() - want)
+    top = 2.0 ** (s.max() - 127)
+    assert (err <= attention_bound(want, size, most, finest, True) + 2.0 ** -32 * top).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("B", [3, 70])
+def test_no_entries_at_all(bits, B):
+    """Tables without columns, or lengths of zero: zeros, and nothing is reported; a prefix alone needs no own table."""
+    m, dv = umim(), dev()
+    c = SharedCase(47, [90], [B], [0] * B, 8, 2, 128, wide=B > 3)
+    a, status = c.args(m, bits, dv), m.new_status(dv)
+    none = torch.zeros((B, 0), dtype=torch.int32, device=dv)
+    check_attention(shared(m, bits)(layer=0, dev_status=status, **{**a, "block_table": none}), *c.want(bits), half=bits == 8)
+    zero = i32([0], dv)
+    for change in ({}, {"block_table": none}, {"prefix_table": none[:1]}, {"block_table": none, "prefix_table": none[:1]}):
+        out = torch.ones_like(a["q"])
+        shared(m, bits)(layer=0, dev_status=status, out=out, **{**a, "prefix_lens": zero, **change})
+        assert (out == 0).all()
+    assert int(status.item()) == 0
 
 
 @pytest.mark.parametrize("bits", [16, 8])
