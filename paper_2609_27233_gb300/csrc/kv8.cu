@@ -21,8 +21,8 @@ constexpr int kRowThreads = 256;
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 4;    // rows in flight a group of lanes
 constexpr int kMaxCluster = 8;    // CTAs per sequence (portable cluster size)
-// Heads of K and V that a warp takes of its rows.  Two: 32768 rows of 8 heads, D = 128, written in 36.9 us
-// (one 45, four 37, eight 39, sixteen 52), 65536 read in 63.6 (one 79, eight 64).
+// Heads of K and V that a warp takes of its rows.  Two: 32768 rows of 8 heads, D = 128, written in 32.2 us
+// (6.3 TB/s; one 38.8, four 33.1), 65536 read in 62.9 (6.4 TB/s; one 77, four 62.6).
 constexpr int kRowHeads = 2;
 
 template <int D>
