@@ -21,7 +21,7 @@ constexpr int kRowThreads = 256;
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 4;    // rows in flight a group of lanes
 constexpr int kMaxCluster = 8;    // CTAs per sequence (portable cluster size)
-// Heads of K and V that a warp takes of its rows.  Two: 32768 rows of 8 heads, D = 128, written in 32.2 us
+// Heads of K and V that a warp takes of its rows.  Two: 32768 rows of 8 heads, D = 128, written in 31.8 us
 // (6.3 TB/s; one 38.8, four 33.1), 65536 read in 62.9 (6.4 TB/s; one 77, four 62.6).
 constexpr int kRowHeads = 2;
 
@@ -130,6 +130,7 @@ struct RowsArgs {
   int32_t B, T;
   uint16_t *k, *v;           // read by a write, written by a read
   int64_t stride;            // elements from one row's heads to the next row's
+  uint64_t per_part;         // 2^34 / parts, rounded up: a division by the parts of a row is a product
   int32_t *status;
 };
 
@@ -151,15 +152,16 @@ __device__ __forceinline__ int2 place_of(const RowsArgs &a, int t0, int t) {
     b = lo;
     while (b + 1 < a.B && a.cu_rows[b + 1] <= t) ++b;
     const int first = a.cu_rows[b];
-    if (t < first || t >= a.cu_rows[b + 1]) return make_int2(-1, 0);
+    if (first < 0 || t < first || t >= a.cu_rows[b + 1]) return make_int2(-1, 0);
     in = t - first;
   }
   if (t >= a.T) return make_int2(-1, 0);
-  const int64_t entry = (int64_t)a.start[b] + in;
+  // (in 32 bits: a table has less than 2^27 pages, and there are 2^24 rows at most)
+  const int start = a.start[b];
+  const uint32_t entry = (uint32_t)start + in;
   int page = -1;
-  if (entry >= 0 && entry < (int64_t)a.max_pages * kPageSize && a.start[b] >= 0)
-    page = a.block_table[(int64_t)b * a.max_pages + entry / kPageSize];
-  if (page < 0 || page >= a.n_pages) {
+  if (start >= 0 && entry < (uint32_t)a.max_pages * kPageSize) page = a.block_table[(uint32_t)b * a.max_pages + entry / kPageSize];
+  if ((uint32_t)page >= (uint32_t)a.n_pages) {
     set_error(a.status, UMIM_ERR_INVALID_ARG);
     page = -1;
   }
@@ -183,7 +185,8 @@ __global__ void __launch_bounds__(kRowThreads) kv8_write_kernel(RowsArgs a) {
   if (blockIdx.x == 0) check_rows(a);
   const int lane = threadIdx.x & 31, heads = 2 * a.n_kv_heads, parts = ceil_div(heads, U);
   const int task = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
-  const int t0 = task / parts * kWarpRows<D>, h0 = task % parts * U;
+  const int block = (int)(task * a.per_part >> 34);   // task / parts: task < 2^22 * parts, so that its error stays below 1 / parts
+  const int t0 = block * kWarpRows<D>, h0 = (task - block * parts) * U;
   if (t0 >= a.T) return;
   const int t = t0 + lane / kRowLanes<D>, col = lane % kRowLanes<D> * 16;
   Row r[U];
@@ -216,7 +219,8 @@ __global__ void __launch_bounds__(kRowThreads) kv8_read_kernel(RowsArgs a) {
   if (blockIdx.x == 0) check_rows(a);
   const int lane = threadIdx.x & 31, heads = 2 * a.n_kv_heads, parts = ceil_div(heads, U);
   const int task = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
-  const int t0 = task / parts * kWarpRows<D>, h0 = task % parts * U;
+  const int block = (int)(task * a.per_part >> 34);   // task / parts: task < 2^22 * parts, so that its error stays below 1 / parts
+  const int t0 = block * kWarpRows<D>, h0 = (task - block * parts) * U;
   if (t0 >= a.T) return;
   const int t = t0 + lane / kRowLanes<D>, col = lane % kRowLanes<D> * 16;
   const int2 at = place_of(a, t0, t);
@@ -366,11 +370,13 @@ __global__ void __launch_bounds__(kAppendThreads) kv8_append_kernel(AppendArgs a
 }
 
 template <int D, bool WRITE>
-umim_status launch_rows(const RowsArgs &a, cudaStream_t stream) {
+umim_status launch_rows(RowsArgs a, cudaStream_t stream) {
   const bool wide = reinterpret_cast<uintptr_t>(a.k) % 32 == 0 && reinterpret_cast<uintptr_t>(a.v) % 32 == 0 && a.stride % 16 == 0;
   auto kern = WRITE ? (wide ? kv8_write_kernel<D, true> : kv8_write_kernel<D, false>)
                     : (wide ? kv8_read_kernel<D, true> : kv8_read_kernel<D, false>);
-  const int64_t warps = (int64_t)ceil_div(a.T, kWarpRows<D>) * ceil_div(2 * a.n_kv_heads, kRowHeads);
+  const int parts = ceil_div(2 * a.n_kv_heads, kRowHeads);   // of a row: warps that share it, 64 at most
+  a.per_part = ((uint64_t(1) << 34) + parts - 1) / parts;
+  const int64_t warps = (int64_t)ceil_div(a.T, kWarpRows<D>) * parts;
   const int64_t blocks = (warps + kRowThreads / 32 - 1) / (kRowThreads / 32);
   trace_mark(stream, WRITE ? "kv8.write" : "kv8.read");
   const cudaError_t e = launch_pdl(kern, dim3((unsigned)blocks), dim3(kRowThreads), 0, stream, a);
