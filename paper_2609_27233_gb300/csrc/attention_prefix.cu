@@ -11,7 +11,7 @@
 // softmax, P V, and the next S, some 4000 cycles in 16 bits, with two slots in turn to
 // cover it.  64 sequences x 4 query heads a KV head behind 16384 entries, 8 KV heads, D = 128,
 // 16 bits: a call of 48 us, 54 where the own entries' kernel does not run beside this one but
-// before it; five 8-bit prefixes of 12000, 120 sequences: 65 us of 86.
+// before it; five 8-bit prefixes of 12000, 120 sequences: 63 us of 83.
 //
 // Work: a row tile is 128 rows (whole sequences), a key tile 128 entries (8 pages).  A
 // segment is a pair of row tiles, or a single one, of a prefix and KV head;
@@ -699,14 +699,15 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           return page >= 0 ? ld_early_u8(scales + row_at(page, lane >> 4) + (lane & 15)) : 127u;
         };
         // of a tile's scales: the largest codes of the page's rows (those that are NaN or behind the end
-        // apart), and this lane's key's factor in the page's units, packed twice
+        // apart), and this lane's key's factor in the page's units, packed twice (0 behind the end)
         uint32_t most, most_v, factor;
         auto scales_of = [&](uint32_t code, int rem) {
-          most = (lane & 15) < rem && code != 255 ? code : 0;
+          const bool there = (lane & 15) < rem;
+          most = there && code != 255 ? code : 0;
 #pragma unroll
           for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
           const int down = (int)code - (int)most;   // 0 or less
-          const float scale = code == 255 ? NAN : down < -126 ? 0.f : __uint_as_float((uint32_t)(134 + down) << 23);
+          const float scale = !there || down < -126 ? 0.f : code == 255 ? NAN : __uint_as_float((uint32_t)(134 + down) << 23);
           const __half2 scale2 = __floats2half2_rn(scale, scale);
           factor = *reinterpret_cast<const uint32_t *>(&scale2);
           most_v = __shfl_sync(0xffffffffu, most, 16);
@@ -725,19 +726,20 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           const int s = pos % kTcStages;
           code = code_of(next);
           page = page_of(j + 2);
-          auto convert = [&](const uint2 (&in)[kSteps], uint8_t *dst, uint32_t factor, int first) {
+          // rows from `rem` on as zeros: V's, so that 0 * garbage makes no NaN (K's scores are masked)
+          auto convert = [&](const uint2 (&in)[kSteps], uint8_t *dst, uint32_t factor, int first, int rem) {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
               const int key = i * kAtOnce + lane / kLanes;
               const uint32_t f = __shfl_sync(0xffffffffu, factor, first + key);
+              const uint32_t x[2] = {key < rem ? in[i].x : 0u, key < rem ? in[i].y : 0u};
               uint32_t out[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const uint32_t h = f16x2_of_e4m3x2((e < 2 ? in[i].x : in[i].y) >> (e & 1) * 16);
+                const uint32_t h = f16x2_of_e4m3x2(x[e / 2] >> (e & 1) * 16);
                 const __half2 b = __hmul2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&f));
                 out[e] = *reinterpret_cast<const uint32_t *>(&b);
               }
-              if (key >= rem) out[0] = out[1] = out[2] = out[3] = 0u;
               *reinterpret_cast<uint4 *>(dst + (part >> 3) * (kTcKeys * 128) + (w * kPageSize + key) * 128 +
                                          (((part & 7) ^ (key & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
             }
@@ -748,7 +750,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             s_scales[pos & 3][w] = make_float4(e8m0_value(most) * 0x1p-7f, (float)((int)most_v - 127), ldexpf(1.f, 120 - (int)most_v), 0.f);
             mbar_arrive(&scales_full[pos & 3]);
           }
-          convert(k, smem + L::kK + s * L::kTile, factor, 0);
+          convert(k, smem + L::kK + s * L::kTile, factor, 0, kPageSize);
           fence_proxy_async_smem();
           __syncwarp();
           if (elect_one()) mbar_arrive(&k_full[s]);
@@ -758,7 +760,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           load(k, next, 0);
           ok = wwait(&v_empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
           if (!ok) break;
-          convert(v, smem + L::kV + s * L::kTile, factor_v, 16);
+          convert(v, smem + L::kV + s * L::kTile, factor_v, 16, rem);
           fence_proxy_async_smem();
           __syncwarp();
           if (elect_one()) mbar_arrive(&v_full[s]);
