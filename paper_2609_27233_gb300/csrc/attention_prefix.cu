@@ -40,9 +40,12 @@
 // to value * 2^e in bf16 took twice the instructions, and they bound the kernel.)  q
 // becomes fp16 in place, below 2^15 by a power of two a row.  With r the row's and the page's
 // powers of two times the scale, and F the page's largest exponent of V's rows,
-//     w = 2^(r s + F - n + 7),   O = sum w v',   l = sum 2^(-F - 7) w,   out = 2^-14 O / l,
-// n the running maximum of r s + F: the weights that multiply V are at most 2^15 and are one
-// fp16 number each (2^-12 of themselves), and l is exact in fp32, a page's sum at a time.
+//     w = 2^(r s + F - n + 7),   O = sum w v',   l = sum 2^(r s - m),   out = 2^(n - m - 14) O / l,
+// n the running maximum of r s + F and m that of r s: the weights that multiply V are at most 2^15 and are one
+// fp16 number each (2^-12 of themselves).  l has a maximum of its own, since a page may hold most of the weight and
+// hardly any of the output: V's scales lie up to 2^220 apart.  A page's part of l is the sum of its w times 2^-(m + F - n + 7);
+// in a tile with a page whose w of a weight of 1 would be below 2^-26 (so that its fp16 weights are all 0), the
+// exponentials are taken once more against m.
 #include <cuda_fp16.h>
 
 #include "attention_pages.cuh"
@@ -155,7 +158,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   __shared__ __align__(8) uint64_t q_full[2], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2],
       p_full[2][2], pv_done[2], o_free[2], turn[2], mma_done[2],
       met[2][4], q_ready[2], scales_full[4];
-  __shared__ float4 s_scales[4][kTcKeys / kPageSize];   // 8-bit: of the last four key tiles' pages, 2^(E - 7), F, 2^(-F - 7)
+  __shared__ float2 s_scales[4][kTcKeys / kPageSize];   // 8-bit: of the last four key tiles' pages, 2^(E - 7), F
   __shared__ float s_row[2][2][2][kTcRows];   // [tile's parity][slot][half]: a row's maximum, or sum
   __shared__ uint32_t tmem_base;
   __shared__ int s_abort, s_pages;
@@ -446,6 +449,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       const bool live = r < spt * a.G && seq < plan.first[u.i + 1];
       const bool any = __any_sync(0xffffffffu, live);   // (warps without rows only keep the others going)
       float m_run = -INFINITY, l_run = 0.f;             // running max (log2 units, moved in steps > 8) and row sum
+      float top = -INFINITY;                            // 8-bit: the largest score, which the row sum is relative to
       int mine = 0;                                     // tiles
       float sl2 = a.scale_log2;
       if constexpr (BITS == 8) {
@@ -509,13 +513,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         };
         // 8-bit: of each page, the powers of two of K's and V's rows
-        const float4 *scale = s_scales[(pos + j - u.t0) & 3];
+        const float2 *scale = s_scales[(pos + j - u.t0) & 3];
         if constexpr (BITS == 8) {
           ok = wwait(&scales_full[(pos + j - u.t0) & 3], (uint32_t)((pos + j - u.t0) >> 2) & 1u);
           if (!ok) break;
         }
         auto factor = [&](int page) { return fmaxf(sl2 * scale[page].x, 1e-37f); };   // (never 0: -inf stays -inf)
-        float s[32], mx = -INFINITY, other;
+        float s[32], mx = -INFINITY, most = -INFINITY, low = INFINITY, other;
 #pragma unroll 1
         for (int c = kKeys / 32 - 1; c >= 0; --c) {   // (the first 32 last: they are still there below)
           tmem_ld_32x32b_x32(t_s + c * 32, s);
@@ -529,7 +533,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                 m2[0] = max3f(m2[0], s[16 * g + x], s[16 * g + x + 1]);
                 if (x + 2 < 16) m2[1] = max3f(m2[1], s[16 * g + x + 2], s[16 * g + x + 3]);
               }
-              mx = fmaxf(mx, fmaf(fmaxf(m2[0], m2[1]), factor(2 * c + g), scale[2 * c + g].y));
+              const float y = fmaxf(m2[0], m2[1]) * factor(2 * c + g);
+              most = fmaxf(most, y);
+              low = fminf(low, scale[2 * c + g].y);
+              mx = fmaxf(mx, y + scale[2 * c + g].y);
             }
           } else {
             mx = fmaxf(mx, largest(s));
@@ -544,7 +551,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         if (grow) {
           alpha = (m_run == -INFINITY) ? 0.f : ex2_approx(m_run - mx);
           m_run = mx;
-          l_run *= alpha;
+          if (BITS == 16) l_run *= alpha;
         }
         // O is rescaled before the tile's first product, of half 0 (the tile before's has landed: S followed it)
         if (half == 0 && mine > 0 && __any_sync(0xffffffffu, grow)) {
@@ -559,6 +566,34 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           tmem_wait_st();
         }
         const float nm = (m_run == -INFINITY) ? 0.f : -m_run;
+        float top0 = 0.f, from = 0.f;   // 8-bit: a page's w times 2^(from - F) are its part of the row sum
+        if constexpr (BITS == 8) {
+          const float was = top;
+          top = fmaxf(top, most);
+          top0 = top == -INFINITY ? 0.f : top;   // (no finite score so far: a sum of NaN stays NaN)
+          l_run *= ex2_approx(was - top0);
+          from = m_run == -INFINITY ? INFINITY : m_run - top0 - 7.f;
+          if (__any_sync(0xffffffffu, live && !(from - low < 26.f))) {   // the row sum by itself, the whole warp's (seldom)
+            const float2 m2 = make_float2(-top0, -top0);
+#pragma unroll 1
+            for (int c = kKeys / 32 - 1; c >= 0; --c) {
+              tmem_ld_32x32b_x32(t_s + c * 32, s);
+              mask(s, c * 32);
+#pragma unroll
+              for (int g = 0; g < 2; ++g) {
+                const float k = factor(2 * c + g);
+                float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int x = 0; x < 16; x += 2) {
+                  const float2 y = __ffma2_rn(make_float2(s[g * 16 + x], s[g * 16 + x + 1]), make_float2(k, k), m2);
+                  sum = __fadd2_rn(sum, make_float2(ex2_approx(y.x), ex2_approx(y.y)));
+                }
+                l_run += sum.x + sum.y;
+              }
+            }
+            from = -INFINITY;
+          }
+        }
         const float2 minus = make_float2(-1.f, -1.f);
         float2 sl2x2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm), la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll (H == 2 ? 2 : 1)   // (four chunks unrolled: their code is fetched over and over, and registers spill)
@@ -571,8 +606,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             float p[16];   // the weights of 32 keys in fp16 pairs
 #pragma unroll
             for (int g = 0; g < 2; ++g) {   // a page
-              const float4 z = scale[2 * h + g];
-              const float k = factor(2 * h + g), off = z.y + nm + 7.f;
+              const float f = scale[2 * h + g].y, k = factor(2 * h + g), off = f + nm + 7.f;
               sl2x2 = make_float2(k, k), nm2 = make_float2(off, off);
               la = lb = make_float2(0.f, 0.f);
 #pragma unroll
@@ -585,7 +619,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                 p[g * 8 + c / 2] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&b));
               }
               const float2 lab = __fadd2_rn(la, lb);
-              l_run = fmaf(lab.x + lab.y, z.z, l_run);
+              l_run = fmaf(lab.x + lab.y, ex2_approx(from - f), l_run);
             }
             // over S columns that have been read: 16 for each 32
             tmem_put_32x32b_x16(t_s + h * 16, p);
@@ -631,20 +665,22 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
       float other;
       ok = exchange(l_run, other, 0.f);
       if (!ok) break;
-      if (store && half == 0) ws.tc_ml[piece * kTcRows + r] = make_float2(m_run, l_run + other);
+      if (store && half == 0) ws.tc_ml[piece * kTcRows + r] = make_float2(BITS == 8 ? top : m_run, l_run + other);
       float *dst = ws.tc_acc + tc_acc_at<D>(piece, r, half * kCols);
       if (mine > 0) {
         ok = wwait(&pv_done[t], (uint32_t)(ns - 1) & 1u);
         if (!ok) break;
         tc_fence_after();
         if (any) {
+          // 8-bit: from O's units to the row sum's (n - m is at most a cache row's exponent)
+          const float up = m_run == -INFINITY ? 1.f : exp2f(m_run - top);
 #pragma unroll 1
           for (int c = 0; c < kCols / 32; ++c) {
             float o[32];
             tmem_ld_32x32b_x32(t_o + half * kCols + c * 32, o);
             if constexpr (BITS == 8)
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] *= 0x1p-14f;
+              for (int i = 0; i < 32; ++i) o[i] = o[i] * 0x1p-14f * up;
             if (store)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
@@ -747,7 +783,8 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           ok = wwait(&k_empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
           if (!ok) break;
           if (lane == 0) {   // (four tiles' scales: S of the tile two before is done, so the softmax of the one four before is)
-            s_scales[pos & 3][w] = make_float4(e8m0_value(most) * 0x1p-7f, (float)((int)most_v - 127), ldexpf(1.f, 120 - (int)most_v), 0.f);
+            // (a page behind the end: F beyond any other's, so that it takes no part in the tile's least)
+            s_scales[pos & 3][w] = make_float2(e8m0_value(most) * 0x1p-7f, rem > 0 ? (float)((int)most_v - 127) : 1e30f);
             mbar_arrive(&scales_full[pos & 3]);
           }
           convert(k, smem + L::kK + s * L::kTile, factor, 0, kPageSize);
