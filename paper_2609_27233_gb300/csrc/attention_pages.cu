@@ -22,6 +22,8 @@
 // their own largest: with t_j = s_j + f_j (log2) and n = max t_j, w_j = 2^(t_j - n + 15)
 // is at most 2^15 and is taken as two fp16 numbers, high part and remainder
 // (22 significant bits down to 2^-18 of the largest weight, 2^-40 of it below).
+// n leaves out the rows of V that hold nothing but zeros, whatever scale they are stored with:
+// beside values of 2^-30 a single one, stored with 1, would be the unit of all weights.
 // Up to eight query heads the two parts are rows 0-7 and 8-15 of one product.
 //
 // A lane's operands come as 16-byte pieces of rows: the head dimension that
@@ -75,6 +77,11 @@ __device__ __forceinline__ uint4 lds_v4(uint32_t a) {
 __device__ __forceinline__ uint2 lds_v2(uint32_t a) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
 __device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
@@ -366,7 +373,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
           *reinterpret_cast<float2 *>(dst + t * 8 + 2 * qc) = make_float2(acc[t][2 * j], acc[t][2 * j + 1]);
       } else {
         // from units of 2^(n - 15) to those of the row sum (n - m is a cache row's exponent at most)
-        const float up = exp2f((n[j] == -INFINITY ? 0.f : n[j]) - (m[j] == -INFINITY ? 0.f : m[j]));
+        const float up = n[j] == -INFINITY ? 1.f : exp2f(n[j] - m[j]);   // (no value so far: acc is 0, or NaN)
         auto out = [&](int t, int c) {
           const float x = R8 ? acc[t][c] + acc[t][2 + c] : acc[t][2 * j + c];
           return x * 0x1p-15f * up;
@@ -476,18 +483,45 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1)
         for (int e = 0; e < 2 * NR; ++e)
           if (nt * 8 + 2 * qc + (e & 1) >= nvalid) s[nt][e] = w[nt][e] = -INFINITY;
     }
+    auto row_max = [&](const float (&x)[2][4], int j) {
+      float y = fmaxf(fmaxf(x[0][2 * j], x[0][2 * j + 1]), fmaxf(x[1][2 * j], x[1][2 * j + 1]));
+      y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
+      return fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
+    };
+    float top[NR];   // the page's largest weights
+    if constexpr (BITS == 8) {
+      // Rows of zeros are looked for by two lanes a row: 4 bytes each, and all of the row where that leaves a doubt.
+      // (64 sequences of 1200 entries, three batches in turn: 37.8 -> 38.6 us.  Only where a largest weight would
+      // move, but whole rows: 39.4.)
+      auto rows_of = [&](uint32_t x) {   // bit 2 r: row r holds something
+        const uint32_t held = __ballot_sync(0xffffffffu, (x & 0x7f7f7f7f) != 0);
+        return (held | held >> 1) & 0x55555555;
+      };
+      uint32_t held = rows_of(lds_u32(vs + P::at(lane >> 1, lane & 1)));
+      if (held != 0x55555555) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const uint4 x = lds_v4(vs + P::at(lane >> 1, (lane & 1) * (D / 32) + i));
+          any |= x.x | x.y | x.z | x.w;
+        }
+        held = rows_of(any);
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2 * NR; ++e)   // (NaN, of a scale, stays)
+            if (!(held >> 2 * (nt * 8 + 2 * qc + (e & 1)) & 1)) w[nt][e] -= INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < NR; ++j) top[j] = row_max(w, j);
+    }
     bool moved = false;
     float c[NR];
 #pragma unroll
     for (int j = 0; j < NR; ++j) {
-      auto row_max = [&](const float (&x)[2][4]) {
-        float y = fmaxf(fmaxf(x[0][2 * j], x[0][2 * j + 1]), fmaxf(x[1][2 * j], x[1][2 * j + 1]));
-        y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
-        return fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
-      };
       const float m_was = m[j], n_was = n[j];
-      m[j] = fmaxf(m[j], row_max(s));
-      n[j] = BITS == 8 ? fmaxf(n[j], row_max(w)) : m[j];
+      m[j] = fmaxf(m[j], row_max(s, j));
+      n[j] = BITS == 8 ? fmaxf(n[j], top[j]) : m[j];
       // no finite score so far: weights from 0, so that a score of -inf weighs 0 and NaN stays NaN
       const float m0 = m[j] == -INFINITY ? 0.f : m[j], n0 = n[j] == -INFINITY ? 0.f : n[j];
       c[j] = ex2_approx(n_was - n0);

@@ -1,5 +1,6 @@
 """Attention over the 8-bit cache where its rows' scales say little about what the rows are worth: scales far apart
-between pages.  The sum of the weights has to have a measure of its own."""
+between pages, rows of zeros (which are stored with scale 1), pages that are not there.  What a weight times its row's
+scale is measured by has to come from rows that hold something, and the sum of the weights from none of that."""
 import numpy as np
 import pytest
 import torch
@@ -82,6 +83,7 @@ class Entries:
 # (kernel, sequences, query heads): "decode" is umim_decode_attention_kv8 with up to eight and with more query heads a KV
 # head; "pages" and "tensor cores" are the shared call's kernels
 FORMS = [("decode", 2, 4), ("decode", 2, 12), ("pages", 3, 4), ("tensor cores", 40, 4), ("tensor cores", 33, 1)]
+PAGES = FORMS[:3]
 
 
 def plain(seed, n, B, hq, D=64, heads=1, size=1.0):
@@ -117,3 +119,87 @@ def test_small_values_with_most_of_the_weight(kernel, B, hq, more):
     V *= 2.0 ** np.where(small, -80, 80)[:, None, None]
     K[small, :, 0] = more * np.log(2)
     Entries(4, K, V, q).check(umim(), dev(), kernel)
+
+
+@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("size", [1.0, 0.05, 1e-12])
+@pytest.mark.parametrize("share", [0, 7, 10, 13])
+def test_a_sink_without_a_value(kernel, B, hq, size, share):
+    """An entry with a V row of zeros and 2^share times the others' weight: the others are all of the output."""
+    n = 1027
+    K, V, q = plain(5, n, B, hq, size=size)
+    K[3], V[3] = 0, 0
+    K[3, :, 0] = np.log(2.0 ** share * n)
+    Entries(6, K, V, q).check(umim(), dev(), kernel)
+
+
+@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", [0, -20, -40, -60])
+def test_rows_of_zeros(kernel, B, hq, D, power):
+    """K and V of 2^power with rows of zeros in places: first and last of a page, a whole page, the last entry."""
+    n = 333
+    K, V, q = plain(7, n, B, hq, D, heads=2, size=2.0 ** power)
+    K *= 2.0 ** power
+    for t in (0, 15, 16, 40, n - 1):
+        V[t] = 0
+    V[64:80, 1] = 0
+    for t in (5, 16, 70):
+        K[t] = 0
+    K[96:112, 0] = 0
+    q *= 2.0 ** min(-power, 30)
+    Entries(8, K, V, q).check(umim(), dev(), kernel, scale=2.0 ** max(0, -power - 30))
+
+
+@pytest.mark.parametrize("kernel,B,hq", PAGES)
+def test_zeros_beside_own_entries(kernel, B, hq):
+    """A prefix whose last pages and rows hold zeros, and own entries of another size behind it."""
+    if kernel == "decode":
+        pytest.skip("no prefix")
+    n = 200
+    K, V, q = plain(9, n, B, hq, size=1e-6)
+    V[::3], V[160:] = 0, 0
+    Entries(10, K, V, q, own=[(7 * b) % 20 for b in range(B)]).check(umim(), dev(), kernel)
+
+
+@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("low", [0, -300])
+def test_nothing_but_zeros(kernel, B, hq, low):
+    """No row holds a value: zeros, however low the scores."""
+    K, V, q = plain(11, 70, B, hq)
+    K[..., 0] = low
+    out = Entries(12, K, 0 * V, q).check(umim(), dev(), kernel)
+    assert (out == 0).all()
+
+
+@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("power", [0, -40])
+def test_a_page_that_is_not_there(kernel, B, hq, power):
+    """Its entries count with scores and values of zero, and set no unit for the others'."""
+    K, V, q = plain(13, 100, B, hq, size=2.0 ** power)
+    c = Entries(14, K, V, q)
+    c.missing = [int(c.table[0, 2])]
+    c.check(umim(), dev(), kernel, code=1)
+
+
+@pytest.mark.parametrize("kernel,B,hq", PAGES)
+def test_zeros_of_no_scale(kernel, B, hq):
+    """A V row of zeros whose scale is NaN is NaN, as 0 * NaN is."""
+    K, V, q = plain(15, 50, B, hq, heads=2)
+    V[20] = 0
+    c = Entries(16, K, V, q)
+    c.scales[0, c.table[0, 1], 1, 0, 4] = 255
+    got = c.run(umim(), dev(), kernel, 1.0).float().cpu().numpy()
+    assert np.isnan(got[:, :hq]).all() and np.isfinite(got[:, hq:]).all()
+
+
+@pytest.mark.parametrize("many", [False])
+def test_zero_scores_are_not_moved(many):
+    """A K row of zeros has a score of 0 beside keys of any size."""
+    B = 40 if many else 3
+    r = W.rng(17)
+    n, D = 64, 64
+    K, V = 2.0 ** -45 * r.standard_normal((n, 1, D)), r.standard_normal((n, 1, D))
+    K[::5] = 0
+    q = 2.0 ** 45 * r.standard_normal((B, 4, D)) / 4
+    Entries(18, K, V, q).check(umim(), dev(), "tensor cores" if many else "pages", scale=0.25)
