@@ -37,15 +37,16 @@
 // 8-bit pages: eight warps read e4m3 rows and make fp16 operands of them, code * 2^(e - E + 7) with E the largest e of the
 // page's 16 rows: 57344 at most, and multiples of 2^-24, so off by 2^-40 of the page's largest
 // at most; rows with e below E - 31 become zeros, which is 2^-31 of it at most.  (Converting
-// to value * 2^e in bf16 took twice the instructions, and they bound the kernel.)  q
+// to value * 2^e in bf16 took twice the instructions, and they bound the kernel.)  Rows that hold nothing but
+// zeros count for no largest e, whatever scale they are stored with, and pages that are not there neither.  q
 // becomes fp16 in place, below 2^15 by a power of two a row.  With r the row's and the page's
 // powers of two times the scale, and F the page's largest exponent of V's rows,
 //     w = 2^(r s + F - n + 7),   O = sum w v',   l = sum 2^(r s - m),   out = 2^(n - m - 14) O / l,
-// n the running maximum of r s + F and m that of r s: the weights that multiply V are at most 2^15 and are one
-// fp16 number each (2^-12 of themselves).  l has a maximum of its own, since a page may hold most of the weight and
+// n the running maximum of r s + F over rows of V that hold something, and m that of r s: the weights that
+// multiply V are at most 2^15 and are one fp16 number each (2^-12 of themselves).  l has a maximum of its own, since a page may hold most of the weight and
 // hardly any of the output: V's scales lie up to 2^220 apart.  A page's part of l is the sum of its w times 2^-(m + F - n + 7);
-// in a tile with a page whose w of a weight of 1 would be below 2^-26 (so that its fp16 weights are all 0), the
-// exponentials are taken once more against m.
+// in a tile with a page whose w of a weight of 1 would be below 2^-26 (so that its fp16 weights are all 0), or with
+// a row of V of zeros, whose w may be any number, the exponentials are taken once more against m.
 #include <cuda_fp16.h>
 
 #include "attention_pages.cuh"
@@ -128,6 +129,13 @@ __device__ __forceinline__ uint32_t ld_early_u8(const uint8_t *p) {
   return v;
 }
 
+// two fp32 numbers as fp16, those beyond its range as its largest
+__device__ __forceinline__ uint32_t half2_within(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 // a tile's 32 columns from x on whose positions lie in [lo, hi)
 __device__ __forceinline__ uint32_t columns_in(int x, int lo, int hi) {
   lo = max(lo - x, 0), hi = min(hi - x, 32);
@@ -147,6 +155,88 @@ __device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t smem_addr) {
 }
 constexpr uint32_t kBMnMajor = 1u << 16;   // instruction descriptor: B is MN-major
 
+// ---- a page of 8-bit rows of K and of V, as the warp that makes operands of it holds it: D / 8 lanes a key ----
+template <int D>
+struct Page8 {
+  static constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kSteps = kPageSize / kAtOnce;
+};
+
+struct PageScales {
+  // the largest codes of K's rows (in lanes 0-15) and of V's, and one more: 0 where no row counts, since those do not
+  // that are NaN, zeros or behind the end
+  uint32_t most, most_v;
+  uint32_t factor;   // this lane's key's (lanes 0-15 K's, 16-31 V's) in units of 2^-7 of that, packed twice; 0 behind the end
+  uint32_t zeros;    // the rows that are there and hold nothing: K's, from bit 16 on V's
+};
+
+// code: the scale of this lane's key
+__device__ __forceinline__ PageScales page_scales(uint32_t code, int rem, uint32_t zeros) {
+  const int lane = threadIdx.x & 31;
+  PageScales r;
+  const bool there = (lane & 15) < rem, zero = zeros >> lane & 1u;
+  r.zeros = zeros;
+  r.most = there && !zero && code != 255 ? code + 1 : 0;
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) r.most = max(r.most, __shfl_xor_sync(0xffffffffu, r.most, o));
+  r.most_v = __shfl_sync(0xffffffffu, r.most, 16);
+  const int down = (int)code + 1 - (int)r.most;   // 0 or less of the rows that count
+  const float scale = !there ? 0.f
+                      : code == 255 ? NAN
+                      : zero || down < -126 ? 0.f : __uint_as_float((uint32_t)(134 + down) << 23);
+  const __half2 scale2 = __floats2half2_rn(scale, scale);
+  r.factor = *reinterpret_cast<const uint32_t *>(&scale2);
+  return r;
+}
+
+// Rows to fp16 operands at the page's place in a tile; rows from `rem` on as zeros (V's, so that 0 * garbage makes no
+// NaN; K's scores are masked).  factor: of key i, in lane `first` + i.
+template <int D>
+__device__ __forceinline__ void convert_page(const uint2 (&in)[Page8<D>::kSteps], uint8_t *dst, uint32_t factor, int first,
+                                             int rem) {
+  constexpr int kLanes = Page8<D>::kLanes;
+  const int lane = threadIdx.x & 31, part = lane % kLanes;
+#pragma unroll
+  for (int i = 0; i < Page8<D>::kSteps; ++i) {
+    const int key = i * Page8<D>::kAtOnce + lane / kLanes;
+    const uint32_t f = __shfl_sync(0xffffffffu, factor, first + key);
+    const uint32_t x[2] = {key < rem ? in[i].x : 0u, key < rem ? in[i].y : 0u};
+    uint32_t out[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t h = f16x2_of_e4m3x2(x[e / 2] >> (e & 1) * 16);
+      const __half2 b = __hmul2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&f));
+      out[e] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    *reinterpret_cast<uint4 *>(dst + (part >> 3) * (kTcKeys * 128) + key * 128 + (((part & 7) ^ (key & 7)) << 4)) =
+        make_uint4(out[0], out[1], out[2], out[3]);
+  }
+}
+
+// A page that may hold rows of zeros: its scales without them, and K converted once more.  A call that reads everything
+// again, since it is seldom made: beside the others' code, its own took a tenth of the kernel's time.
+// row: K's first (values null: a page that is not there), V's rows_v further on.
+template <int D>
+__device__ __noinline__ PageScales page_again(const uint8_t *values, const uint8_t *scales, int64_t row, int rows_v, int rem,
+                                              uint8_t *dst) {
+  const int lane = threadIdx.x & 31;
+  const uint8_t *rows = values ? values + row * D : nullptr;
+  const uint32_t code = values ? scales[row + (lane >> 4) * rows_v + (lane & 15)] : 127u;
+  bool zero = (lane & 15) < rem;
+  if (zero && rows) {
+    const uint4 *p = reinterpret_cast<const uint4 *>(rows + ((int64_t)(lane >> 4) * rows_v + (lane & 15)) * D);
+    uint32_t any = 0;
+    for (int i = 0; i < D / 16; ++i) any |= p[i].x | p[i].y | p[i].z | p[i].w;
+    zero = !(any & 0x7f7f7f7f);
+  }
+  const PageScales r = page_scales(code, rem, __ballot_sync(0xffffffffu, zero));
+  uint2 k[Page8<D>::kSteps];
+#pragma unroll
+  for (int i = 0; i < Page8<D>::kSteps; ++i)
+    k[i] = rows ? *reinterpret_cast<const uint2 *>(rows + (i * 32 + lane) * 8) : make_uint2(0, 0);
+  convert_page<D>(k, dst, r.factor, 0, kPageSize);
+  return r;
+}
+
 template <int D, int BITS>
 __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     prefix_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap kv_map,
@@ -158,7 +248,9 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
   __shared__ __align__(8) uint64_t q_full[2], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2],
       p_full[2][2], pv_done[2], o_free[2], turn[2], mma_done[2],
       met[2][4], q_ready[2], scales_full[4];
-  __shared__ float2 s_scales[4][kTcKeys / kPageSize];   // 8-bit: of the last four key tiles' pages, 2^(E - 7), F
+  // 8-bit: of the last four key tiles' pages, 2^(E - 7), F, the same or -infinity where there are rows of V of
+  // zeros, and a bit for each of those
+  __shared__ float4 s_scales[4][kTcKeys / kPageSize];
   __shared__ float s_row[2][2][2][kTcRows];   // [tile's parity][slot][half]: a row's maximum, or sum
   __shared__ uint32_t tmem_base;
   __shared__ int s_abort, s_pages;
@@ -513,7 +605,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         };
         // 8-bit: of each page, the powers of two of K's and V's rows
-        const float2 *scale = s_scales[(pos + j - u.t0) & 3];
+        const float4 *scale = s_scales[(pos + j - u.t0) & 3];
         if constexpr (BITS == 8) {
           ok = wwait(&scales_full[(pos + j - u.t0) & 3], (uint32_t)((pos + j - u.t0) >> 2) & 1u);
           if (!ok) break;
@@ -535,7 +627,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
               }
               const float y = fmaxf(m2[0], m2[1]) * factor(2 * c + g);
               most = fmaxf(most, y);
-              low = fminf(low, scale[2 * c + g].y);
+              low = fminf(low, scale[2 * c + g].z);
               mx = fmaxf(mx, y + scale[2 * c + g].y);
             }
           } else {
@@ -545,6 +637,42 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         ok = exchange(mx, other, mx);
         if (!ok) break;
         mx = BITS == 8 ? mx : fmaxf(mx, other) * sl2;
+        float from = 0.f;   // 8-bit: a page's w times 2^(from - F) are its part of the row sum
+        bool apart = false;
+        if constexpr (BITS == 8) {
+          const float was = top;
+          top = fmaxf(top, most);
+          const float top0 = top == -INFINITY ? 0.f : top;   // (no finite score so far: a sum of NaN stays NaN)
+          l_run *= ex2_approx(was - top0);
+          const float n = mx > m_run + 8.f ? mx : m_run;   // (as below)
+          from = n == -INFINITY ? INFINITY : n - top0 - 7.f;
+          apart = __any_sync(0xffffffffu, live && !(from - low < 26.f));   // (one answer for the warp)
+          if (__builtin_expect(apart, 0)) {   // the row sum by itself, and the largest weight without the rows of zeros
+            const float2 m2 = make_float2(-top0, -top0);
+            mx = -INFINITY;
+#pragma unroll 1
+            for (int c = kKeys / 32 - 1; c >= 0; --c) {
+              tmem_ld_32x32b_x32(t_s + c * 32, s);
+              mask(s, c * 32);
+#pragma unroll
+              for (int g = 0; g < 2; ++g) {
+                const float k = factor(2 * c + g);
+                const uint32_t none = __float_as_uint(scale[2 * c + g].w);
+                float2 sum = make_float2(0.f, 0.f);
+                float y = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 16; x += 2) {
+                  const float2 z = make_float2(s[g * 16 + x], s[g * 16 + x + 1]);
+                  const float2 e = __ffma2_rn(z, make_float2(k, k), m2);
+                  sum = __fadd2_rn(sum, make_float2(ex2_approx(e.x), ex2_approx(e.y)));
+                  y = max3f(y, none >> x & 1u ? -INFINITY : z.x, none >> x & 2u ? -INFINITY : z.y);
+                }
+                l_run += sum.x + sum.y;
+                mx = fmaxf(mx, y * k + scale[2 * c + g].y);
+              }
+            }
+          }
+        }
         // move the running max only when it grows by more than 2^8
         const bool grow = mx > m_run + 8.f;
         float alpha = 1.f;
@@ -566,34 +694,6 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
           tmem_wait_st();
         }
         const float nm = (m_run == -INFINITY) ? 0.f : -m_run;
-        float top0 = 0.f, from = 0.f;   // 8-bit: a page's w times 2^(from - F) are its part of the row sum
-        if constexpr (BITS == 8) {
-          const float was = top;
-          top = fmaxf(top, most);
-          top0 = top == -INFINITY ? 0.f : top;   // (no finite score so far: a sum of NaN stays NaN)
-          l_run *= ex2_approx(was - top0);
-          from = m_run == -INFINITY ? INFINITY : m_run - top0 - 7.f;
-          if (__any_sync(0xffffffffu, live && !(from - low < 26.f))) {   // the row sum by itself, the whole warp's (seldom)
-            const float2 m2 = make_float2(-top0, -top0);
-#pragma unroll 1
-            for (int c = kKeys / 32 - 1; c >= 0; --c) {
-              tmem_ld_32x32b_x32(t_s + c * 32, s);
-              mask(s, c * 32);
-#pragma unroll
-              for (int g = 0; g < 2; ++g) {
-                const float k = factor(2 * c + g);
-                float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int x = 0; x < 16; x += 2) {
-                  const float2 y = __ffma2_rn(make_float2(s[g * 16 + x], s[g * 16 + x + 1]), make_float2(k, k), m2);
-                  sum = __fadd2_rn(sum, make_float2(ex2_approx(y.x), ex2_approx(y.y)));
-                }
-                l_run += sum.x + sum.y;
-              }
-            }
-            from = -INFINITY;
-          }
-        }
         const float2 minus = make_float2(-1.f, -1.f);
         float2 sl2x2 = make_float2(sl2, sl2), nm2 = make_float2(nm, nm), la = make_float2(0.f, 0.f), lb = la;
 #pragma unroll (H == 2 ? 2 : 1)   // (four chunks unrolled: their code is fetched over and over, and registers spill)
@@ -615,11 +715,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                 const float2 y = make_float2(ex2_approx(x.x), ex2_approx(x.y));   // masked (-inf): 0
                 if (c & 2) lb = __fadd2_rn(lb, y);
                 else la = __fadd2_rn(la, y);
-                const __half2 b = __floats2half2_rn(y.x, y.y);
-                p[g * 8 + c / 2] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&b));
+                p[g * 8 + c / 2] = __uint_as_float(half2_within(y.x, y.y));   // (a row of zeros: times 0)
               }
               const float2 lab = __fadd2_rn(la, lb);
-              l_run = fmaf(lab.x + lab.y, ex2_approx(from - f), l_run);
+              if (!apart) l_run = fmaf(lab.x + lab.y, ex2_approx(from - f), l_run);
             }
             // over S columns that have been read: 16 for each 32
             tmem_put_32x32b_x16(t_s + h * 16, p);
@@ -702,7 +801,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     // memory they left room for one stage of K, whose products then waited for its
     // conversion, and that for the products before ----
     if constexpr (BITS == 8) {
-      constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kSteps = kPageSize / kAtOnce;
+      constexpr int kLanes = Page8<D>::kLanes, kAtOnce = Page8<D>::kAtOnce, kSteps = Page8<D>::kSteps;
       static_assert(kConverters * kPageSize == kTcKeys, "a warp a page");
       const int w = warp - kConvert<BITS>, part = lane % kLanes;
       const int own = lane / kLanes * D + part * 8;   // this lane's place in a step's keys
@@ -734,74 +833,61 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         auto code_of = [&](int page) {   // a key's: lanes 0-15 K's, 16-31 V's
           return page >= 0 ? ld_early_u8(scales + row_at(page, lane >> 4) + (lane & 15)) : 127u;
         };
-        // of a tile's scales: the largest codes of the page's rows (those that are NaN or behind the end
-        // apart), and this lane's key's factor in the page's units, packed twice (0 behind the end)
-        uint32_t most, most_v, factor;
-        auto scales_of = [&](uint32_t code, int rem) {
-          const bool there = (lane & 15) < rem;
-          most = there && code != 255 ? code : 0;
+        // 0 where a row might be zeros: its first eight bytes say of most that they are not (lanes of part 0)
+        auto least_of = [&](const uint2 (&in)[kSteps]) {
+          uint32_t least = 0xffffffffu;
 #pragma unroll
-          for (int o = 1; o < 16; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-          const int down = (int)code - (int)most;   // 0 or less
-          const float scale = !there || down < -126 ? 0.f : code == 255 ? NAN : __uint_as_float((uint32_t)(134 + down) << 23);
-          const __half2 scale2 = __floats2half2_rn(scale, scale);
-          factor = *reinterpret_cast<const uint32_t *>(&scale2);
-          most_v = __shfl_sync(0xffffffffu, most, 16);
+          for (int i = 0; i < kSteps; ++i) least = min(least, (in[i].x | in[i].y) & 0x7f7f7f7f);
+          return least;
         };
         // The order below: a wait for one load is a wait for all loads before it, so what the short ones
         // bring is used before the next long ones are issued.
-        uint2 k[kSteps], v[kSteps];
+        uint2 k[kSteps], v[kSteps], v_next[kSteps];
         int page = checked(page_of(u.t0), u.t0);
         uint32_t code = code_of(page);
         load(k, page, 0);
         load(v, page, 1);
-        scales_of(code, u.len - (u.t0 * 8 + w) * kPageSize);
+        PageScales of = page_scales(code, u.len - (u.t0 * 8 + w) * kPageSize, 0);
         int next = checked(page_of(u.t0 + 1), u.t0 + 1);
         for (int j = u.t0; ok && j < u.t1; ++j, ++pos) {
           const int rem = u.len - (j * 8 + w) * kPageSize;   // keys from the page's first on
           const int s = pos % kTcStages;
           code = code_of(next);
           page = page_of(j + 2);
-          // rows from `rem` on as zeros: V's, so that 0 * garbage makes no NaN (K's scores are masked)
-          auto convert = [&](const uint2 (&in)[kSteps], uint8_t *dst, uint32_t factor, int first, int rem) {
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-              const int key = i * kAtOnce + lane / kLanes;
-              const uint32_t f = __shfl_sync(0xffffffffu, factor, first + key);
-              const uint32_t x[2] = {key < rem ? in[i].x : 0u, key < rem ? in[i].y : 0u};
-              uint32_t out[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t h = f16x2_of_e4m3x2(x[e / 2] >> (e & 1) * 16);
-                const __half2 b = __hmul2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&f));
-                out[e] = *reinterpret_cast<const uint32_t *>(&b);
-              }
-              *reinterpret_cast<uint4 *>(dst + (part >> 3) * (kTcKeys * 128) + (w * kPageSize + key) * 128 +
-                                         (((part & 7) ^ (key & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
-            }
-          };
           ok = wwait(&k_empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
           if (!ok) break;
+          uint8_t *const k_at = smem + L::kK + s * L::kTile + w * (kPageSize * 128);
+          convert_page<D>(k, k_at, of.factor, 0, kPageSize);
+          // (V is a tile ahead like K, so that both are looked at before the softmax warps need their scales)
+          const bool doubt = __any_sync(0xffffffffu, part == 0 && min(least_of(k), least_of(v)) == 0);
+          if (__builtin_expect(doubt && rem > 0, 0)) {
+            const int here = checked(page_of(j), j);
+            of = page_again<D>(here >= 0 ? values : nullptr, scales, here >= 0 ? row_at(here, 0) : 0, a.Hkv * kPageSize, rem, k_at);
+          }
           if (lane == 0) {   // (four tiles' scales: S of the tile two before is done, so the softmax of the one four before is)
-            // (a page behind the end: F beyond any other's, so that it takes no part in the tile's least)
-            s_scales[pos & 3][w] = make_float2(e8m0_value(most) * 0x1p-7f, rem > 0 ? (float)((int)most_v - 127) : 1e30f);
+            // (a page without values of V: F below any other's; one behind the end: above, so that it is not the tile's least)
+            const float f = rem <= 0 ? 1e30f : of.most_v ? (float)((int)of.most_v - 128) : -1e30f;
+            const uint32_t none = of.zeros >> 16;
+            s_scales[pos & 3][w] =
+                make_float4(e8m0_value(max(of.most, 1u) - 1) * 0x1p-7f, f, none ? -INFINITY : f, __uint_as_float(none));
             mbar_arrive(&scales_full[pos & 3]);
           }
-          convert(k, smem + L::kK + s * L::kTile, factor, 0, kPageSize);
           fence_proxy_async_smem();
           __syncwarp();
           if (elect_one()) mbar_arrive(&k_full[s]);
-          const uint32_t factor_v = factor;
-          scales_of(code, rem - kTcKeys);   // the next tile's
+          const uint32_t factor_v = of.factor;
+          of = page_scales(code, rem - kTcKeys, 0);   // the next tile's
           page = checked(page, j + 2);
           load(k, next, 0);
+          load(v_next, next, 1);
           ok = wwait(&v_empty[s], (uint32_t)(pos / kTcStages & 1) ^ 1u);
           if (!ok) break;
-          convert(v, smem + L::kV + s * L::kTile, factor_v, 16, rem);
+          convert_page<D>(v, smem + L::kV + s * L::kTile + w * (kPageSize * 128), factor_v, 16, rem);
           fence_proxy_async_smem();
           __syncwarp();
           if (elect_one()) mbar_arrive(&v_full[s]);
-          load(v, next, 1);
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i) v[i] = v_next[i];
           next = page;
         }
       }

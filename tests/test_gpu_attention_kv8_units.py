@@ -83,7 +83,6 @@ class Entries:
 # (kernel, sequences, query heads): "decode" is umim_decode_attention_kv8 with up to eight and with more query heads a KV
 # head; "pages" and "tensor cores" are the shared call's kernels
 FORMS = [("decode", 2, 4), ("decode", 2, 12), ("pages", 3, 4), ("tensor cores", 40, 4), ("tensor cores", 33, 1)]
-PAGES = FORMS[:3]
 
 
 def plain(seed, n, B, hq, D=64, heads=1, size=1.0):
@@ -121,7 +120,7 @@ def test_small_values_with_most_of_the_weight(kernel, B, hq, more):
     Entries(4, K, V, q).check(umim(), dev(), kernel)
 
 
-@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("kernel,B,hq", FORMS)
 @pytest.mark.parametrize("size", [1.0, 0.05, 1e-12])
 @pytest.mark.parametrize("share", [0, 7, 10, 13])
 def test_a_sink_without_a_value(kernel, B, hq, size, share):
@@ -133,7 +132,7 @@ def test_a_sink_without_a_value(kernel, B, hq, size, share):
     Entries(6, K, V, q).check(umim(), dev(), kernel)
 
 
-@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("kernel,B,hq", FORMS)
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("power", [0, -20, -40, -60])
 def test_rows_of_zeros(kernel, B, hq, D, power):
@@ -151,7 +150,21 @@ def test_rows_of_zeros(kernel, B, hq, D, power):
     Entries(8, K, V, q).check(umim(), dev(), kernel, scale=2.0 ** max(0, -power - 30))
 
 
-@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("kernel,B,hq", FORMS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_that_begin_with_zeros(kernel, B, hq, D):
+    """Rows that hold something behind zeros (of both signs), beside rows that hold nothing: over pages enough for every CTA
+    to have several tiles."""
+    n = 128 * 160 + 77 if kernel == "tensor cores" else 777
+    K, V, q = plain(21, n, B, hq, D, size=2.0 ** -30)
+    K[..., :D - 3], V[..., :D - 5] = 0, -0.0
+    q *= 4
+    V[5::97] = 0
+    K[7::89] = 0
+    Entries(22, K, V, q).check(umim(), dev(), kernel)
+
+
+@pytest.mark.parametrize("kernel,B,hq", FORMS)
 def test_zeros_beside_own_entries(kernel, B, hq):
     """A prefix whose last pages and rows hold zeros, and own entries of another size behind it."""
     if kernel == "decode":
@@ -162,7 +175,7 @@ def test_zeros_beside_own_entries(kernel, B, hq):
     Entries(10, K, V, q, own=[(7 * b) % 20 for b in range(B)]).check(umim(), dev(), kernel)
 
 
-@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("kernel,B,hq", FORMS)
 @pytest.mark.parametrize("low", [0, -300])
 def test_nothing_but_zeros(kernel, B, hq, low):
     """No row holds a value: zeros, however low the scores."""
@@ -172,7 +185,7 @@ def test_nothing_but_zeros(kernel, B, hq, low):
     assert (out == 0).all()
 
 
-@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("kernel,B,hq", FORMS)
 @pytest.mark.parametrize("power", [0, -40])
 def test_a_page_that_is_not_there(kernel, B, hq, power):
     """Its entries count with scores and values of zero, and set no unit for the others'."""
@@ -182,7 +195,7 @@ def test_a_page_that_is_not_there(kernel, B, hq, power):
     c.check(umim(), dev(), kernel, code=1)
 
 
-@pytest.mark.parametrize("kernel,B,hq", PAGES)
+@pytest.mark.parametrize("kernel,B,hq", FORMS)
 def test_zeros_of_no_scale(kernel, B, hq):
     """A V row of zeros whose scale is NaN is NaN, as 0 * NaN is."""
     K, V, q = plain(15, 50, B, hq, heads=2)
@@ -193,7 +206,7 @@ def test_zeros_of_no_scale(kernel, B, hq):
     assert np.isnan(got[:, :hq]).all() and np.isfinite(got[:, hq:]).all()
 
 
-@pytest.mark.parametrize("many", [False])
+@pytest.mark.parametrize("many", [False, True])
 def test_zero_scores_are_not_moved(many):
     """A K row of zeros has a score of 0 beside keys of any size."""
     B = 40 if many else 3
