@@ -116,8 +116,9 @@ typedef struct umim_paged_kv {
  * A row x is stored as e4m3(x / 2^e), rounded to nearest with ties to even, e
  * the smallest whole number with max |x| <= 448 * 2^e over the row's finite
  * values, kept within [-100, 120] (0 for a row without any but zeros).  NaN
- * and infinities are stored as NaN.  A stored value is off by at most 2^-4 of
- * itself, or by 2^-10 * 2^e where it is below 2^-6 * 2^e. */
+ * and infinities are stored as NaN, and finite magnitudes above 240 * 2^120 as
+ * that, so that what is finite stays finite.  A stored value is off by at most
+ * 2^-4 of itself, or by 2^-10 * 2^e where it is below 2^-6 * 2^e. */
 typedef struct umim_paged_kv8 {
   void *values;       /* device, 16-B aligned                          */
   void *scales;       /* device, 16-B aligned                          */

@@ -6,7 +6,8 @@ The paper keeps its cache in 16 bits; the format is this library's.  A row x of 
 values is stored as c_i = e4m3(x_i / 2^e), rounded to nearest, ties to even, with
 the smallest whole e such that max |x_i| <= 448 * 2^e over the finite x_i, kept in
 [-100, 120], and e = 0 for a row without any but zeros.  NaN and infinities are
-stored as NaN.  The e8m0 code of 2^e is e + 127.
+stored as NaN, finite magnitudes above 240 * 2^120 as that (256 * 2^120 is no
+bf16 number).  The e8m0 code of 2^e is e + 127.
 
 e4m3: sign, four exponent bits (bias 7), three fraction bits; no infinities, all
 ones is NaN, so the largest number is 1.75 * 2^8 = 448 and the smallest 2^-9.
@@ -64,7 +65,7 @@ def quantise(bits):
                 k += 1
             e[i] = k
     with np.errstate(invalid="ignore"):
-        y = np.where(finite, x, 0) / np.ldexp(1.0, e)[..., None]
+        y = np.clip(np.where(finite, x, 0), -240 * 2.0 ** 120, 240 * 2.0 ** 120) / np.ldexp(1.0, e)[..., None]
     return np.where(finite, _codes(y), 0x7f).astype(np.uint8), (e + 127).astype(np.uint8)
 
 

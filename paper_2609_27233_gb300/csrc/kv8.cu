@@ -83,15 +83,16 @@ __device__ __forceinline__ uint4 quantise(Row &r, uint32_t &code) {
   for (int i = 0; i < 8; ++i) m = __vmaxu2(m, r.x[i] & 0x7fff7fff);
   m = reduce(m);
   constexpr uint32_t kInf = 0x7f80;   // bf16 patterns from here on are infinite or NaN
-  if (__any_sync(0xffffffffu, m >= kInf)) {
-    // They have no part in the scale, and all become NaN: the conversion would make the
-    // largest number of an infinity.  (Selected value by value below: a call of 32 us took 36.)
+  if (__any_sync(0xffffffffu, m > kKv8Top)) {
+    // Those have no part in the scale, and all become NaN: the conversion would make the
+    // largest number of an infinity.  Finite numbers above the largest that is stored become that.
+    // (Selected value by value below: a call of 32 us took 36.)
     uint32_t f = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t a = r.x[i] & 0x7fff, b = r.x[i] >> 16 & 0x7fff;
       f = __vmaxu2(f, (a < kInf ? a : 0) | (b < kInf ? b : 0) << 16);
-      r.x[i] |= (a < kInf ? 0u : 0x7fffu) | (b < kInf ? 0u : 0x7fff0000u);
+      r.x[i] = (r.x[i] & 0x80008000u) | (a < kInf ? min(a, kKv8Top) : 0x7fffu) | (b < kInf ? min(b, kKv8Top) : 0x7fffu) << 16;
     }
     m = reduce(f);
   }
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(kRowThreads) kv8_read_kernel(RowsArgs a) {
     for (int i = 0; i < 8; ++i) {
       const uint32_t f = f16x2_of_e4m3x2(in[i / 2] >> (i & 1) * 16);
       const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&f));
-      // exact: four significant bits, and 2^-126 <= |x| for every scale that a write makes
+      // exact: four significant bits, and 2^-109 <= |x| <= 240 * 2^120 for what a write makes
       const __nv_bfloat162 y = __floats2bfloat162_rn(x.x * s, x.y * s);
       out[i] = *reinterpret_cast<const uint32_t *>(&y);
     }

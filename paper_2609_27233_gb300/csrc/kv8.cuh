@@ -11,6 +11,9 @@ namespace umim {
 // e stays within [-100, 120]: bf16's largest magnitude needs 120, and below -100
 // nothing is left of a row that any other row would not drown.
 constexpr int kKv8MinExp = -100, kKv8MaxExp = 120;
+// The bf16 bits of 240 * 2^120, the largest magnitude that is stored: the next e4m3 number up,
+// 256, times 2^120 is 2^128, which is finite neither in bf16 nor in fp32.
+constexpr uint32_t kKv8Top = 0x7f70;
 
 // e + 127 of a row whose largest magnitude has the bf16 bits `most` (finite):
 // 448 = 1.75 * 2^8, so a significand above 1.75 (fraction bits above 96) needs one more.
