@@ -147,6 +147,11 @@ def _pool_fields(pool):
     return pool.data_ptr(), layers, pages, heads, page_size, head_dim
 
 
+def _needs_float8():
+    if _E4M3 is None or _E8M0 is None:
+        raise RuntimeError("the 8-bit cache needs a torch with float8_e4m3fn and float8_e8m0fnu")
+
+
 class Kv8Pool:
     """An 8-bit paged cache: values torch.float8_e4m3fn [layers][pages][2][Hkv][16][D] and scales
     torch.float8_e8m0fnu [layers][pages][2][Hkv][16], an entry's value times its row's scale.  It holds the two
@@ -154,6 +159,7 @@ class Kv8Pool:
     __slots__ = ("values", "scales", "layers", "heads", "head_dim", "_c")
 
     def __init__(self, values, scales):
+        _needs_float8()
         shape = values.shape
         if values.dtype is not _E4M3 or len(shape) != 6 or shape[2] != 2 or not values.is_contiguous():
             raise ValueError("values must be contiguous float8_e4m3fn [layers][pages][2][Hkv][16][D]")
@@ -174,10 +180,11 @@ class Kv8Pool:
     @classmethod
     def zeros(cls, layers, pages, heads, head_dim, device, stream=None):
         """A cache of zeros (scales 1)."""
+        _needs_float8()
         shape = (layers, pages, 2, heads, PAGE_SIZE)
         values = _made(stream, torch.zeros, shape + (head_dim,), dtype=torch.uint8, device=device)
         scales = _made(stream, torch.full, shape, 127, dtype=torch.uint8, device=device)
-        return cls(values.view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu))
+        return cls(values.view(_E4M3), scales.view(_E8M0))
 
 
 def paged_kv(pool):
@@ -188,7 +195,8 @@ def paged_kv(pool):
 # the layouts of umim_paged_kv, umim_paged_kv8 and umim_merge_weights (native alignment)
 _pack_kv = struct.Struct("@P5i4x").pack
 _pack_kv8 = struct.Struct("@2P5i4x").pack
-_I32, _BF16, _E4M3, _E8M0 = torch.int32, torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
+_I32, _BF16 = torch.int32, torch.bfloat16
+_E4M3, _E8M0 = getattr(torch, "float8_e4m3fn", None), getattr(torch, "float8_e8m0fnu", None)   # (an older torch lacks them)
 _pack_weights = struct.Struct("@9P2if4x").pack
 _WEIGHTS = ("w_kv", "b_kv", "ln_kv_gamma", "ln_kv_beta", "query", "w_o", "b_o", "ln_o_gamma", "ln_o_beta")
 
