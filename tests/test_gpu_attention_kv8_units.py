@@ -8,7 +8,7 @@ import torch
 import oracle
 import workloads as W
 from helpers import dev, umim
-from kv8_helpers import PAGE, check_attention, i32, key_like, shared, tables, to_bf16, to_pool8
+from kv8_helpers import PAGE, attention_bound, check_attention, i32, key_like, shared, tables, to_bf16, to_pool8
 
 pytestmark = pytest.mark.gpu
 
@@ -216,3 +216,32 @@ def test_zero_scores_are_not_moved(many):
     K[::5] = 0
     q = 2.0 ** 45 * r.standard_normal((B, 4, D)) / 4
     Entries(18, K, V, q).check(umim(), dev(), "tensor cores" if many else "pages", scale=0.25)
+
+
+# the pages' kernel over 8-bit prefixes, held to what it keeps itself (not to the tensor cores' kernel's one fp16 number a
+# weight): 2^-17 of a weight and 2^-40 of the largest weight times its scale
+@pytest.mark.parametrize("hq,D,spread", [(4, 64, 0), (16, 128, 0), (7, 128, 10), (12, 64, 45)])
+def test_pages_kernel_keeps_its_own_bound(hq, D, spread):
+    r = W.rng(19 + hq)
+    n, B = 777, 5
+    K, V, q = plain(20 + hq, n, B, hq, D)
+    V *= np.exp2(r.integers(-spread, spread + 1, V.shape[:-1]))[..., None]
+    c = Entries(21, 4 * K, V, 4 * q, own=[0, 5, 16, 33, 1])
+    check_attention(c.run(umim(), dev(), "pages", 0.3), *c.want("pages", 0.3))
+
+
+@pytest.mark.parametrize("D,hq", [(64, 8), (128, 1), (128, 16)])
+def test_rows_of_a_page_far_apart_on_the_tensor_cores(D, hq):
+    """Rows of V in one page with scales up to 2^90 apart.  A row of scale f beside a largest scale of F is zeros where f is
+    below 2^-31 F, 448 f <= 448 * 2^-32 F at most, and off by 2^-25 units of 2^-7 F otherwise; their mean by weights that sum
+    up to 1 is off by no more than the largest of those."""
+    r = W.rng(23)
+    n, B = 333, 40
+    K, V, q = plain(24, n, B, hq, D)
+    V *= np.exp2(r.integers(-45, 46, V.shape[:-1]))[..., None]
+    c = Entries(25, K, V, q)
+    want, size, most, finest = c.want("tensor cores", 1.0)
+    got = c.run(umim(), dev(), "tensor cores", 1.0).double().cpu().numpy()
+    pages = c.table[0, :-(-n // PAGE)]
+    top = 2.0 ** (int(c.scales[0, pages, 1].max()) - 127)
+    assert (np.abs(got - want) <= attention_bound(want, size, most, finest, True) + 448 * 2.0 ** -32 * top).all()
