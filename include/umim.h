@@ -464,7 +464,10 @@ umim_status umim_kv8_append_merge(const umim_paged_kv8 *kv, int32_t *block_table
 
 /* ------------------------------------------------------------------------
  * umim_decode_attention over the 8-bit cache: K and V are value * 2^e, the
- * sums and the softmax fp32.
+ * sums and the softmax fp32.  What a weight adds to the output is kept down to
+ * 2^-40 of the largest weight times its V row's scale (rows of V that hold
+ * nothing but zeros apart, whatever their scale), and q down to 2^-40 of its
+ * row's largest value; the sum of the weights has no such limit.
  *
  * q             device bf16 [batch][n_q_heads][head_dim], 8-B aligned
  * out           device bf16 [batch][n_q_heads][head_dim]
@@ -512,10 +515,13 @@ umim_status umim_decode_attention_kv8(const void *q, int32_t n_q_heads, const um
  * n_kv_heads * (batch * max_pages + (n_prefixes + batch * n_q_heads /
  * n_kv_heads / 16) * max_prefix_pages) above 2^30, and the shapes that
  * umim_decode_attention does not support.
- * Over the 8-bit cache, with a prefix of more than 16 rows (sequence, query
- * head of one KV head), the entries of a page of K or of V may be rounded to
- * 2^-31 of the largest of them, and weights to 2^-12 of themselves or 2^-32 of
- * the largest (weights times the largest scale of their page of V).
+ * Over the 8-bit cache umim_decode_attention_kv8's limits hold, and with a
+ * prefix of more than 16 rows (sequence, query head of one KV head) the entries
+ * of a page of K or of V may be rounded to 2^-31 of the largest of them, and
+ * weights to 2^-12 of themselves or 2^-32 of the largest (weights times the
+ * largest scale of their page of V).  Rows of zeros and pages that are not
+ * there set neither limit, whatever scale they are stored with, and the sum of
+ * the weights is fp32 without them.
  * Device-side errors: UMIM_ERR_INVALID_ARG for a length outside its table (it counts as 0), an
  * offset that decreases (it counts as the largest before it) or leaves
  * [0, batch] (as 0), and a used page outside [0, n_pages) (it reads as

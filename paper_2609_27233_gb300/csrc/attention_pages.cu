@@ -34,10 +34,12 @@
 // copy (K and V, rows swizzled so that eight lanes' pieces meet no bank twice) and
 // one of its 32 scales.
 //
-// HBM bounds the 8-bit decode once it runs: 76800 entries of 64 sequences, 32/8 heads, D = 128
-// (158 MB) take 33.7 us, 27 of them the stream of pages (5.8 TB/s) and the rest what a call of one
-// short sequence takes too: lengths, table and first page one after the other, and the combine
-// kernel.  A page costs a warp some 440 instructions, 120 of them products, conversions and loads.
+// What bounds the 8-bit decode is what a page goes through in its warp, products, softmax and products one
+// after the other, with three warps a scheduler to cover that: DRAM and issue slots are half used.
+// 76800 entries of 64 sequences, 32/8 heads, D = 128 (158 MB) take 34.1 us on the device, 27 of them the
+// stream of pages (5.8 TB/s) and the rest what a call of one short sequence takes too: lengths, table and
+// first page one after the other, and the combine kernel; with 16 query heads a KV head 51.0.  A page costs a warp some 430
+// instructions, 120 of them products, conversions and loads.
 #include <cuda_fp16.h>
 
 #include "attention_pages.cuh"

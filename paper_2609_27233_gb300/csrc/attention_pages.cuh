@@ -61,8 +61,8 @@ inline int64_t tc_max_segments(int B, int n, int G) {
 }
 
 // CTAs of the pages' kernel, `ctas` for all.  Both kernels run at once where each has a fair part of the
-// work, the CTAs that this one leaves unused making room for the other's: 64 sequences behind 16000
-// entries, 16384 of their own, 32/8 heads, D = 128: 52.9 -> 44.4 us, 96 behind 4 x 4000 with 4000, 37.9 -> 34.3.  Below an
+// work, the CTAs that this one leaves unused making room for the other's: 64 sequences behind 16384
+// entries, 16384 of their own, 32/8 heads, D = 128: 51.4 -> 45.1 us on the device.  Below an
 // eighth they run one after the other on the whole GPU: few CTAs take their time over many
 // short sequences (64 of one page each beside 16384 entries: 41 -> 52 us).  A key tile of a row tile takes an SM
 // about as long as 12 (16 bits) or 15 pages of 16 rows.
