@@ -164,11 +164,9 @@ def test_rows_that_begin_with_zeros(kernel, B, hq, D):
     Entries(22, K, V, q).check(umim(), dev(), kernel)
 
 
-@pytest.mark.parametrize("kernel,B,hq", FORMS)
+@pytest.mark.parametrize("kernel,B,hq", FORMS[2:])
 def test_zeros_beside_own_entries(kernel, B, hq):
     """A prefix whose last pages and rows hold zeros, and own entries of another size behind it."""
-    if kernel == "decode":
-        pytest.skip("no prefix")
     n = 200
     K, V, q = plain(9, n, B, hq, size=1e-6)
     V[::3], V[160:] = 0, 0
